@@ -13,6 +13,10 @@ device every call raises.
     gemm(A, B, trans_a, trans_b, out=None)     C = op(A) .^ op(B) (float32 or bfloat16 A, B)
     bmm(A, B, trans_a, trans_b, out=None)      batched over the leading axis
     exact_grad(A, B, Mod, trans_a, out=None)   exact-derivative product (Table 1)
+    norm_rope, norm_rope_grad, append_kv, paged_attention
+                                               the attention side (``attention.py``): norms of queries and keys
+                                               with the position rotation, a paged key/value cache, PAM
+                                               attention over it
 
 Matrix arguments are float32 HIP tensors whose last dimension is contiguous
 (row stride = leading dimension).  Products that split K take their
@@ -29,7 +33,7 @@ import ctypes
 import os
 
 __all__ = ["mul", "pad", "palog2", "paexp2", "round_mantissa", "gemm", "bmm", "exact_grad", "plan",
-           "device_info", "library_path", "load", "PamError"]
+           "device_info", "library_path", "load", "PamError", "norm_rope", "norm_rope_grad", "append_kv", "paged_attention"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpam.so")
@@ -421,3 +425,6 @@ def device_info(device: int = 0) -> dict:
             "lanes_per_simd": info.lanes_per_simd, "clock_khz": info.clock_khz,
             "wavefront_size": info.wavefront_size, "valu_lane_ops_per_s": info.valu_lane_ops_per_s,
             "arch": info.arch.decode()}
+
+
+from .attention import append_kv, norm_rope, norm_rope_grad, paged_attention  # noqa: E402

@@ -1,0 +1,337 @@
+"""The attention-side operators of a PAM transformer: norms of queries and keys
+with the position rotation, a paged key/value cache, and PAM attention over it.
+
+Thin binding over ``include/pam_attention.h`` in the manner of the package's
+other calls: every step runs in the library's HIP kernels on the current
+stream, nothing waits for the GPU, and there is no CPU path.
+
+    norm_rope(q, k, positions, cos, sin, ...)        norm and rotation of queries and keys
+    norm_rope_grad(dq, dk, q, k, ...)                its gradient
+    append_kv(k, v, k_cache, v_cache, slots, ...)    keys and values into a paged cache
+    paged_attention(q, k_cache, v_cache, ...)        softmax(scale Q .^ K^T) .^ V over the cache
+
+Heads are (tokens, heads, d) tensors, float32 or bfloat16, with a contiguous
+last dimension and any strides (views of a projection's output); caches are
+(pages, page_size, heads, d) tensors, likewise.  Norm, rotation and softmax
+are ordinary float32 arithmetic (Sec. 3.2 replaces the products of the linear
+layers and of the attention), the attention's two products are PAM products.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+
+from . import _check, _launch, _require, _same_device, _torch, load
+
+__all__ = ["norm_rope", "norm_rope_grad", "append_kv", "paged_attention"]
+
+# Every symbol include/pam_attention.h declares.
+EXPORTS = ("pam_norm_rope", "pam_norm_rope_grad_workspace_size", "pam_norm_rope_grad", "pam_append_kv",
+           "pam_paged_attention_workspace_size", "pam_paged_attention")
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_token", ctypes.c_int64), ("stride_head", ctypes.c_int64),
+                ("heads", ctypes.c_int32), ("type", ctypes.c_int32)]
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_page", ctypes.c_int64), ("stride_slot", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("type", ctypes.c_int32)]
+
+
+class _Sequences(ctypes.Structure):
+    _fields_ = [("q_starts", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("tokens", ctypes.c_int64), ("batch", ctypes.c_int32),
+                ("table_width", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_kv", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+_bound = None
+
+
+def _library() -> ctypes.CDLL:
+    global _bound
+    if _bound is None:
+        lib = load()
+        i32, i64, vp, f32, sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float, ctypes.c_size_t
+        heads, rotation, cache = (ctypes.POINTER(t) for t in (_Heads, _Rotation, _Cache))
+        lib.pam_norm_rope.argtypes = [i64, i32, heads, vp, heads, heads, vp, heads, f32, rotation, vp]
+        lib.pam_norm_rope_grad_workspace_size.argtypes = [i64, i32, i32, i32, ctypes.POINTER(sz)]
+        lib.pam_norm_rope_grad.argtypes = [i64, i32, heads, vp, heads, heads, vp, heads, vp, heads, heads, vp, f32,
+                                           rotation, vp, sz, vp]
+        lib.pam_append_kv.argtypes = [i64, i32, heads, vp, heads, heads, vp, heads, f32, rotation, cache, cache, vp, vp]
+        lib.pam_paged_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+        lib.pam_paged_attention.argtypes = [i32, heads, cache, cache, ctypes.POINTER(_Sequences), heads, vp, sz, vp]
+        for name in EXPORTS:
+            getattr(lib, name).restype = i32
+        _bound = lib
+    return _bound
+
+
+def _is_bf16(t) -> int:
+    return int(t.dtype == _torch().bfloat16)
+
+
+def _heads(t):
+    return None if t is None else _Heads(t.data_ptr(), t.stride(0), t.stride(1), t.shape[1], _is_bf16(t))
+
+
+def _cache(t):
+    return _Cache(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2), t.shape[0], t.shape[1], t.shape[2], _is_bf16(t))
+
+
+def _ints(t, name: str, dtype, *shape):
+    """An index tensor of the given type and shape (None: any), contiguous."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != len(shape) or any(want is not None and have != want for have, want in zip(t.shape, shape)):
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _weight(w, name: str, d: int):
+    if w is not None:
+        _require(w, name, 1)
+        if w.shape[0] != d:
+            raise ValueError(f"{name} must have {d} values, got {w.shape[0]}")
+
+
+def _rotation(positions, cos, sin, interleaved: bool, tokens: int, d: int):
+    """The rotation's arguments, or None where there is none."""
+    torch = _torch()
+    given = [x is not None for x in (positions, cos, sin)]
+    if not any(given):
+        return None
+    if not all(given):
+        raise ValueError("positions, cos and sin must be given together")
+    _ints(positions, "positions", torch.int32, tokens)
+    for name, t in (("cos", cos), ("sin", sin)):
+        _require(t, name, 2)
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    if cos.shape != sin.shape:
+        raise ValueError(f"cos and sin differ in shape: {tuple(cos.shape)} and {tuple(sin.shape)}")
+    if 2 * cos.shape[1] > d:
+        raise ValueError(f"the tables turn {2 * cos.shape[1]} values, the heads have {d}")
+    return _Rotation(positions.data_ptr(), cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1],
+                     int(bool(interleaved)))
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _head_tensors(*named):
+    """Checks the (tokens, heads, d) tensors that are given; they agree in
+    tokens, d, type and device with the first."""
+    first = None
+    for name, t in named:
+        if t is None:
+            continue
+        _require(t, name, 3, bf16_ok=True)
+        if first is None:
+            first = (name, t)
+            continue
+        ref = first[1]
+        if t.shape[0] != ref.shape[0] or t.shape[2] != ref.shape[2]:
+            raise ValueError(f"{name} {tuple(t.shape)} and {first[0]} {tuple(ref.shape)} differ in tokens or head size")
+        if t.dtype != ref.dtype:
+            raise TypeError(f"{name} is {t.dtype}, {first[0]} {ref.dtype}")
+        _same_device(ref, (name, t))
+    if first is None:
+        raise ValueError("neither queries nor keys given")
+    return first[1]
+
+
+def norm_rope(q, k, positions=None, cos=None, sin=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+              interleaved: bool = False, out_dtype=None):
+    """Norm and position rotation of queries (tokens, heads, d) and keys (tokens,
+    key heads, d) in one pass; returns (q', k'), either input may be None.
+
+    With a weight (d float32 values) a head's values x become x * weight /
+    sqrt(mean(x^2) + eps).  ``cos`` and ``sin`` are float32 (rows, rot / 2)
+    tables, ``positions`` int32 (tokens): the first ``rot`` values of each head
+    are turned in pairs (p, p + rot / 2), or (2p, 2p + 1) if ``interleaved``,
+    by the angles of the token's position.  float32 arithmetic, rounded once to
+    ``out_dtype`` (the inputs' type)."""
+    torch = _torch()
+    ref = _head_tensors(("q", q), ("k", k))
+    tokens, _, d = ref.shape
+    _weight(q_weight, "q_weight", d)
+    _weight(k_weight, "k_weight", d)
+    rot = _rotation(positions, cos, sin, interleaved, tokens, d)
+    _same_device(ref, ("q_weight", q_weight), ("k_weight", k_weight), ("positions", positions), ("cos", cos),
+                 ("sin", sin))
+    dtype = ref.dtype if out_dtype is None else out_dtype
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"out_dtype must be float32 or bfloat16, got {dtype}")
+    qo, ko = (None if t is None else torch.empty(t.shape, dtype=dtype, device=ref.device) for t in (q, k))
+    _launch(ref, _library().pam_norm_rope, tokens, d, _ref(_heads(q)), _ptr(q_weight if q is not None else None),
+            _ref(_heads(qo)), _ref(_heads(k)), _ptr(k_weight if k is not None else None), _ref(_heads(ko)), float(eps),
+            _ref(rot))
+    return qo, ko
+
+
+def norm_rope_grad(dq, dk, q, k, positions=None, cos=None, sin=None, q_weight=None, k_weight=None,
+                   eps: float = 1e-6, interleaved: bool = False):
+    """Gradient of ``norm_rope``: from the gradients (dq, dk) of its outputs and
+    its inputs, (gradient of q, of k, of q_weight, of k_weight); None for what
+    was not given.  Gradients have their input's type, the weights' float32."""
+    torch = _torch()
+    if (dq is None) != (q is None) or (dk is None) != (k is None):
+        raise ValueError("q and dq, k and dk must be given together")
+    ref = _head_tensors(("q", q), ("dq", dq), ("k", k), ("dk", dk))
+    for x, dx, name in ((q, dq, "dq"), (k, dk, "dk")):
+        if x is not None and x.shape != dx.shape:
+            raise ValueError(f"{name} must have shape {tuple(x.shape)}, got {tuple(dx.shape)}")
+    tokens, _, d = ref.shape
+    if q is None:
+        q_weight = None
+    if k is None:
+        k_weight = None
+    _weight(q_weight, "q_weight", d)
+    _weight(k_weight, "k_weight", d)
+    rot = _rotation(positions, cos, sin, interleaved, tokens, d)
+    _same_device(ref, ("q_weight", q_weight), ("k_weight", k_weight), ("positions", positions), ("cos", cos),
+                 ("sin", sin))
+    gq, gk = (None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+    gqw, gkw = (None if w is None else torch.empty_like(w) for w in (q_weight, k_weight))
+    lib = _library()
+    keep = None
+    nbytes = 0
+    if gqw is not None or gkw is not None:
+        need = ctypes.c_size_t()
+        _check(lib.pam_norm_rope_grad_workspace_size(tokens, d, 0 if q is None else q.shape[1],
+                                                     0 if k is None else k.shape[1], ctypes.byref(need)))
+        nbytes = int(need.value)
+        keep = torch.empty(nbytes, dtype=torch.uint8, device=ref.device) if nbytes else None
+    _launch(ref, lib.pam_norm_rope_grad, tokens, d, _ref(_heads(q)), _ptr(q_weight), _ref(_heads(dq)),
+            _ref(_heads(gq)), _ptr(gqw), _ref(_heads(k)), _ptr(k_weight), _ref(_heads(dk)), _ref(_heads(gk)), _ptr(gkw),
+            float(eps), _ref(rot), _ptr(keep), nbytes)
+    del keep
+    return gq, gk, gqw, gkw
+
+
+def _caches(k_cache, v_cache):
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        _require(t, name, 4, bf16_ok=True)
+    if k_cache.shape != v_cache.shape:
+        raise ValueError(f"the caches differ in shape: {tuple(k_cache.shape)} and {tuple(v_cache.shape)}")
+    _same_device(k_cache, ("v_cache", v_cache))
+
+
+def append_kv(k, v, k_cache, v_cache, slots, positions=None, cos=None, sin=None, k_weight=None, q=None, q_weight=None,
+              eps: float = 1e-6, interleaved: bool = False):
+    """Writes the keys and values (tokens, key heads, d) of new tokens into the
+    paged caches (pages, page_size, key heads, d): token t to slot ``slots[t]``
+    (int64, page * page_size + place; outside the cache, as -1: not stored).
+    Keys are normed (``k_weight``) and rotated as by ``norm_rope`` on the way;
+    both are rounded to the cache's type.  With ``q``, the same tokens' queries
+    are normed (``q_weight``) and rotated in the same launch and returned in
+    q's type, else None."""
+    torch = _torch()
+    ref = _head_tensors(("k", k), ("v", v), ("q", q))
+    _caches(k_cache, v_cache)
+    tokens, heads, d = k.shape
+    if v.shape != k.shape or tuple(k_cache.shape[2:]) != (heads, d):
+        raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)} and caches {tuple(k_cache.shape)} do not agree")
+    _weight(q_weight, "q_weight", d)
+    _weight(k_weight, "k_weight", d)
+    _ints(slots, "slots", torch.int64, tokens)
+    rot = _rotation(positions, cos, sin, interleaved, tokens, d)
+    _same_device(ref, ("k_cache", k_cache), ("slots", slots), ("q_weight", q_weight), ("k_weight", k_weight),
+                 ("positions", positions), ("cos", cos), ("sin", sin))
+    qo = None if q is None else torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _launch(ref, _library().pam_append_kv, tokens, d, _ref(_heads(k)), _ptr(k_weight), _ref(_heads(v)),
+            _ref(_heads(q)), _ptr(q_weight if q is not None else None), _ref(_heads(qo)), float(eps), _ref(rot),
+            _ref(_cache(k_cache)), _ref(_cache(v_cache)), slots.data_ptr())
+    return qo
+
+
+# Workspace bytes of an attention call by its sizes, as the library reports them.
+_attention_bytes = {}
+
+
+def _attention_workspace(sizes: tuple) -> int:
+    nbytes = _attention_bytes.get(sizes)
+    if nbytes is None:
+        need = ctypes.c_size_t()
+        _check(_library().pam_paged_attention_workspace_size(*sizes, ctypes.byref(need)))
+        nbytes = int(need.value)
+        if len(_attention_bytes) >= 4096:
+            _attention_bytes.clear()
+        _attention_bytes[sizes] = nbytes
+    return nbytes
+
+
+def paged_attention(q, k_cache, v_cache, table, kv_lens, q_starts=None, max_q: int = 1, max_kv: int | None = None,
+                    scale: float | None = None, causal: bool = True, window: int = 0, out=None):
+    """softmax(scale Q .^ K^T) .^ V of new tokens over a paged cache, as float32
+    (tokens, heads, d).
+
+    ``q`` (tokens, heads, d) holds the new tokens of all sequences in order;
+    sequence b's are ``q_starts[b] : q_starts[b + 1]`` (int32, batch + 1
+    entries), at most ``max_q`` of them; without ``q_starts`` every sequence has
+    one.  ``kv_lens`` (int32) counts each sequence's cached keys, its new ones
+    among them as the last; ``table`` (int32, batch x pages a row) names their
+    pages.  ``max_kv`` (the table's whole reach) bounds ``kv_lens``: the nearer
+    it is, the better the work is cut.  A token sees its sequence's keys up to
+    its own position (all, without ``causal``), the last ``window`` of them
+    where that is positive; a token without keys gets zeros.  ``scale`` is 1 /
+    sqrt(d) if not given.  Tokens of no sequence are left unwritten."""
+    torch = _torch()
+    _require(q, "q", 3, bf16_ok=True)
+    _caches(k_cache, v_cache)
+    tokens, heads, d = q.shape
+    pages, page_size, kv_heads, cache_d = k_cache.shape
+    if k_cache.dtype != v_cache.dtype:
+        raise TypeError(f"the caches differ in type: {k_cache.dtype} and {v_cache.dtype}")
+    if cache_d != d:
+        raise ValueError(f"q has heads of {d} values, the caches of {cache_d}")
+    if not isinstance(kv_lens, torch.Tensor) or kv_lens.dim() != 1:
+        raise ValueError("kv_lens must be a one-dimensional tensor")
+    batch = kv_lens.shape[0]
+    _ints(kv_lens, "kv_lens", torch.int32, batch)
+    _ints(table, "table", torch.int32, batch, None)
+    if q_starts is not None:
+        _ints(q_starts, "q_starts", torch.int32, batch + 1)
+    elif tokens != batch:
+        raise ValueError(f"without q_starts q must have one token a sequence: {tokens} tokens, {batch} sequences")
+    else:
+        max_q = 1
+    if max_kv is None:
+        max_kv = table.shape[1] * page_size
+    if window < 0:
+        raise ValueError("window must be >= 0")
+    if out is None:
+        out = torch.empty((tokens, heads, d), dtype=torch.float32, device=q.device)
+    else:
+        _require(out, "out", 3)
+        if out.shape != q.shape:
+            raise ValueError(f"out must have shape {tuple(q.shape)}, got {tuple(out.shape)}")
+    _same_device(q, ("k_cache", k_cache), ("table", table), ("kv_lens", kv_lens), ("q_starts", q_starts), ("out", out))
+    max_q, max_kv = int(max_q), int(max_kv)
+    seq = _Sequences(_ptr(q_starts), kv_lens.data_ptr(), table.data_ptr(), table.shape[1], tokens, batch,
+                     table.shape[1], max_q, max_kv, int(bool(causal)), int(window),
+                     1.0 / math.sqrt(d) if scale is None else float(scale))
+    nbytes = _attention_workspace((d, heads, kv_heads, _is_bf16(k_cache), batch, max_q, max_kv))
+    keep = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
+    _launch(q, _library().pam_paged_attention, d, _ref(_heads(q)), _ref(_cache(k_cache)), _ref(_cache(v_cache)),
+            ctypes.byref(seq), _ref(_heads(out)), _ptr(keep), nbytes)
+    del keep
+    return out

@@ -735,6 +735,14 @@ pam_status_t run_exact_grad(pam_op_t transA, int64_t m, int64_t n, int64_t k, co
 
 }  // namespace
 
+namespace pamk {
+
+pam_status_t api_fail(pam_status_t status, const char *message) { return fail(status, message); }
+pam_status_t api_fail_hip(hipError_t error, const char *what) { return fail_hip(error, what); }
+pam_status_t api_check_device() { return check_device(); }
+
+}  // namespace pamk
+
 extern "C" {
 
 pam_status_t pam_mul(const float *a, const float *b, float *out, int64_t n, hipStream_t stream) {

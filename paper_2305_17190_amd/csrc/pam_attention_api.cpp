@@ -1,0 +1,504 @@
+// C ABI of the attention-side operators (pam_attention.h): argument
+// validation, the cut of an attention call into launches, workspaces.  The
+// arithmetic lives in pam_heads.hip and pam_attention.hip.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+
+#include "pam_attention.h"
+#include "pam_attention_internal.h"
+#include "pam_internal.h"
+
+namespace {
+
+using pamk::api_check_device;
+using pamk::api_fail;
+using pamk::api_fail_hip;
+
+pam_status_t invalid(const char *why) { return api_fail(PAM_ERROR_INVALID_VALUE, why); }
+
+pam_status_t invalid(const char *name, const char *why) {
+    char buf[160];
+    snprintf(buf, sizeof buf, "%s%s", name, why);
+    return invalid(buf);
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+constexpr int64_t kMaxRows = 0x7FFFFFFF;         // rows of a head launch, slots of a cache
+constexpr int64_t kMaxStride = (int64_t)1 << 48; // sums of strided offsets stay inside int64
+constexpr int64_t kMaxLaunchGroups = 16777215;   // workgroups of 256 threads: below 2^32 threads
+
+bool is_bf16(pam_type_t t) { return t == PAM_TYPE_BF16; }
+
+pam_status_t check_heads(const pam_heads_t &h, const char *name, int64_t tokens, bool must_have_data = true) {
+    if (h.type != PAM_TYPE_F32 && h.type != PAM_TYPE_BF16)
+        return invalid(name, ": type must be PAM_TYPE_F32 or PAM_TYPE_BF16");
+    if (h.heads < 1)
+        return invalid(name, ": heads must be at least 1");
+    if (h.stride_token < 0 || h.stride_head < 0 || h.stride_token > kMaxStride || h.stride_head > kMaxStride)
+        return invalid(name, ": strides must be in [0, 2^48]");
+    if (must_have_data && tokens > 0 && h.data == nullptr)
+        return invalid(name, ": data is NULL");
+    return PAM_SUCCESS;
+}
+
+// A written operand: its rows may not share memory.
+pam_status_t check_written(const pam_heads_t &h, const char *name, int64_t tokens, int32_t d) {
+    if ((tokens > 1 && h.stride_token < d) || (h.heads > 1 && h.stride_head < d))
+        return invalid(name, ": rows of a written operand overlap");
+    return check_heads(h, name, tokens);
+}
+
+pam_status_t check_cache(const pam_cache_t &c, const char *name, bool must_have_data) {
+    if (c.type != PAM_TYPE_F32 && c.type != PAM_TYPE_BF16)
+        return invalid(name, ": type must be PAM_TYPE_F32 or PAM_TYPE_BF16");
+    if (c.heads < 1 || c.page_size < 1 || c.pages < 0)
+        return invalid(name, ": heads and page_size must be at least 1, pages at least 0");
+    if (c.pages > kMaxRows / c.page_size)
+        return invalid(name, ": pages * page_size must be below 2^31");
+    if (c.stride_page < 0 || c.stride_slot < 0 || c.stride_head < 0 || c.stride_page > kMaxStride / (c.pages + 1) ||
+        c.stride_slot > kMaxStride || c.stride_head > kMaxStride)
+        return invalid(name, ": stride out of range");
+    if (must_have_data && c.pages > 0 && c.data == nullptr)
+        return invalid(name, ": data is NULL");
+    return PAM_SUCCESS;
+}
+
+pam_status_t check_dim(int64_t tokens, int32_t d, float eps) {
+    if (tokens < 0)
+        return invalid("tokens must be >= 0");
+    if (d < 2 || d > PAM_MAX_HEAD_DIM || d % 2 != 0)
+        return invalid("d must be even and in [2, 256]");
+    if (!(eps >= 0.0f) || !std::isfinite(eps))
+        return invalid("eps must be finite and >= 0");
+    return PAM_SUCCESS;
+}
+
+pam_status_t check_rotation(const pam_rotation_t *r, int64_t tokens, int32_t d) {
+    if (r == nullptr)
+        return PAM_SUCCESS;
+    if (r->rot < 0 || r->rot > d || r->rot % 2 != 0)
+        return invalid("rot must be even and in [0, d]");
+    if (r->rows < 0 || r->rows > kMaxRows)
+        return invalid("the rotation's rows must be in [0, 2^31)");
+    if (tokens > 0 && (r->positions == nullptr || (r->rows > 0 && r->rot > 0 && (r->cos == nullptr || r->sin == nullptr))))
+        return invalid("positions, cos and sin must be non-NULL");
+    return PAM_SUCCESS;
+}
+
+template <typename P> void set_rotation(P &p, const pam_rotation_t *r) {
+    if (r == nullptr || r->rot == 0) {
+        p.rot = 0;
+        p.interleaved = 0;
+        p.positions = nullptr;
+        p.cos = p.sin = nullptr;
+        p.rows = 0;
+        return;
+    }
+    p.rot = r->rot;
+    p.interleaved = r->interleaved != 0;
+    p.positions = r->positions;
+    p.cos = r->cos;
+    p.sin = r->sin;
+    p.rows = r->rows;
+}
+
+pam_status_t check_rows(int64_t tokens, int64_t heads) {
+    if (tokens > kMaxRows / heads)
+        return invalid("tokens times heads must be below 2^31");
+    return PAM_SUCCESS;
+}
+
+void add_part(pamk::HeadRowsParams &p, const pam_heads_t &in, const float *weight, bool rotate) {
+    pamk::HeadPart &part = p.part[p.parts++];
+    part = pamk::HeadPart{};
+    part.in = in.data;
+    part.weight = weight;
+    part.in_token = in.stride_token;
+    part.in_head = in.stride_head;
+    part.first = p.heads;
+    part.heads = in.heads;
+    part.rotate = rotate;
+    p.heads += in.heads;
+}
+
+void to_heads(pamk::HeadPart &part, const pam_heads_t &out) {
+    part.out = out.data;
+    part.out_token = out.stride_token;
+    part.out_head = out.stride_head;
+    part.out_bf16 = is_bf16(out.type);
+}
+
+void to_cache(pamk::HeadPart &part, const pam_cache_t &c) {
+    part.out = c.data;
+    part.out_token = c.stride_page;
+    part.out_slot = c.stride_slot;
+    part.out_head = c.stride_head;
+    part.out_bf16 = is_bf16(c.type);
+    part.paged = 1;
+}
+
+#define PAM_TRY(call)                                       \
+    do {                                                    \
+        if (pam_status_t st_ = (call); st_ != PAM_SUCCESS)  \
+            return st_;                                     \
+    } while (0)
+
+// Workgroups, and partial rows, of the two parts of a gradient: the budget
+// shared in proportion to the rows.
+void grad_budget(int64_t q_rows, int64_t k_rows, int (&most)[2]) {
+    const double all = (double)std::max<int64_t>(q_rows + k_rows, 1);
+    most[0] = std::max(1, (int)(pamk::kHeadGradGroups * ((double)q_rows / all)));
+    most[1] = std::max(1, (int)(pamk::kHeadGradGroups * ((double)k_rows / all)));
+}
+
+// How an attention call is cut.
+struct AttentionPlan {
+    int lanes;        // lanes a key in the kernels
+    int rows, row_blocks;
+    bool whole;
+    int splits, split_keys;
+    int64_t units;
+    size_t scores, stats, partial;   // workspace bytes of each
+    size_t bytes() const { return scores + stats + partial; }
+};
+
+constexpr int64_t kWholeScores = 16384;   // scores of a unit kept in LDS at most (64 KiB)
+
+AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool bf16, int32_t batch, int32_t max_q,
+                             int32_t max_kv) {
+    AttentionPlan a{};
+    const int per = bf16 ? 8 : 4;
+    a.lanes = 4;
+    while (a.lanes * per < d)
+        a.lanes *= 2;
+    const int64_t rows = (int64_t)max_q * (q_heads / kv_heads);
+    a.rows = rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
+    a.row_blocks = (int)ceil_div(std::max<int64_t>(rows, 1), a.rows);
+    a.units = (int64_t)batch * kv_heads * a.row_blocks;
+    a.whole = (int64_t)max_kv * a.rows <= kWholeScores && (a.units >= 256 || max_kv <= 512);
+    a.splits = 1;
+    if (a.whole || a.units == 0)
+        return a;
+    // About 2048 workgroups, of 256 to 1024 keys.
+    const int64_t keys = ceil_div((int64_t)max_kv * a.units, 2048);
+    a.split_keys = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(keys, 64) * 64, 256), 1024);
+    a.splits = (int)ceil_div(max_kv, a.split_keys);
+    const int64_t parts = a.units * a.splits;
+    a.scores = (size_t)(parts * a.split_keys * a.rows) * sizeof(float);
+    a.stats = (size_t)ceil_div(parts * 2 * a.rows, 4) * 16;
+    a.partial = (size_t)(parts * a.rows * d) * sizeof(float);
+    return a;
+}
+
+pam_status_t check_attention_sizes(int32_t d, int32_t q_heads, int32_t kv_heads, int32_t batch, int32_t max_q,
+                                   int32_t max_kv) {
+    if (d < 8 || d > PAM_MAX_HEAD_DIM || d % 8 != 0)
+        return invalid("d must be a multiple of 8 in [8, 256]");
+    if (q_heads < 1 || kv_heads < 1 || q_heads % kv_heads != 0)
+        return invalid("the query heads must be a multiple of the caches' heads");
+    if (batch < 0 || max_q < 0 || max_kv < 0)
+        return invalid("batch, max_q and max_kv must be >= 0");
+    const int64_t rows = (int64_t)max_q * q_heads;
+    if (rows > kMaxRows || (batch > 0 && ceil_div(rows, 1) * (max_kv / 256 + 1) > ((int64_t)1 << 40) / batch))
+        return invalid("too many rows (batch * max_q * heads * max_kv too large)");
+    return PAM_SUCCESS;
+}
+
+}  // namespace
+
+extern "C" {
+
+pam_status_t pam_norm_rope(int64_t tokens, int32_t d, const pam_heads_t *q_in, const float *q_weight,
+                           const pam_heads_t *q_out, const pam_heads_t *k_in, const float *k_weight,
+                           const pam_heads_t *k_out, float eps, const pam_rotation_t *rotation, hipStream_t stream) {
+    PAM_TRY(check_dim(tokens, d, eps));
+    if ((q_in == nullptr) != (q_out == nullptr) || (k_in == nullptr) != (k_out == nullptr))
+        return invalid("in and out must be given together");
+    if (q_in == nullptr && k_in == nullptr)
+        return invalid("neither queries nor keys given");
+    if (q_in != nullptr && k_in != nullptr && q_in->type != k_in->type)
+        return invalid("q_in and k_in must have one type");
+    pamk::HeadRowsParams p{};
+    const pam_heads_t *in[] = {q_in, k_in}, *out[] = {q_out, k_out};
+    const float *weight[] = {q_weight, k_weight};
+    const char *in_name[] = {"q_in", "k_in"}, *out_name[] = {"q_out", "k_out"};
+    for (int i = 0; i < 2; ++i) {
+        if (in[i] == nullptr)
+            continue;
+        PAM_TRY(check_heads(*in[i], in_name[i], tokens));
+        PAM_TRY(check_written(*out[i], out_name[i], tokens, d));
+        if (in[i]->heads != out[i]->heads)
+            return invalid(out_name[i], ": another count of heads than the input");
+        add_part(p, *in[i], weight[i], rotation != nullptr);
+        to_heads(p.part[p.parts - 1], *out[i]);
+    }
+    PAM_TRY(check_rotation(rotation, tokens, d));
+    PAM_TRY(check_rows(tokens, p.heads));
+    if (tokens == 0)
+        return PAM_SUCCESS;
+    PAM_TRY(api_check_device());
+    p.tokens = tokens;
+    p.d = d;
+    p.eps = eps;
+    set_rotation(p, rotation);
+    const bool bf16 = is_bf16(q_in != nullptr ? q_in->type : k_in->type);
+    const hipError_t e = pamk::launch_head_rows(bf16, p, stream);
+    return e == hipSuccess ? PAM_SUCCESS : api_fail_hip(e, "pam_norm_rope kernel launch");
+}
+
+pam_status_t pam_norm_rope_grad_workspace_size(int64_t tokens, int32_t d, int32_t q_heads, int32_t k_heads,
+                                               size_t *bytes) {
+    if (bytes == nullptr)
+        return invalid("bytes is NULL");
+    PAM_TRY(check_dim(tokens, d, 0.0f));
+    if (q_heads < 0 || k_heads < 0 || (q_heads == 0 && k_heads == 0))
+        return invalid("heads must be >= 0, and one of them positive");
+    PAM_TRY(check_rows(tokens, (int64_t)q_heads + k_heads));
+    int most[2];
+    grad_budget(tokens * q_heads, tokens * k_heads, most);
+    const int64_t rows = std::min<int64_t>(tokens * q_heads, most[0]) + std::min<int64_t>(tokens * k_heads, most[1]);
+    *bytes = (size_t)ceil_div(rows * d, 4) * 16;
+    return PAM_SUCCESS;
+}
+
+pam_status_t pam_norm_rope_grad(int64_t tokens, int32_t d, const pam_heads_t *q_in, const float *q_weight,
+                                const pam_heads_t *dq_out, const pam_heads_t *dq_in, float *dq_weight,
+                                const pam_heads_t *k_in, const float *k_weight, const pam_heads_t *dk_out,
+                                const pam_heads_t *dk_in, float *dk_weight, float eps,
+                                const pam_rotation_t *rotation, void *workspace, size_t workspace_bytes,
+                                hipStream_t stream) {
+    PAM_TRY(check_dim(tokens, d, eps));
+    if (q_in == nullptr && k_in == nullptr)
+        return invalid("neither queries nor keys given");
+    const pam_heads_t *x[] = {q_in, k_in}, *dz[] = {dq_out, dk_out}, *dx[] = {dq_in, dk_in};
+    const float *weight[] = {q_weight, k_weight};
+    float *dweight[] = {dq_weight, dk_weight};
+    const char *names[][3] = {{"q_in", "dq_out", "dq_in"}, {"k_in", "dk_out", "dk_in"}};
+    pamk::HeadGradParams p{};
+    pam_type_t type = q_in != nullptr ? q_in->type : k_in->type;
+    bool weights = false;
+    int64_t rows[2] = {0, 0};
+    for (int i = 0; i < 2; ++i) {
+        if ((x[i] == nullptr) != (dz[i] == nullptr) || (x[i] == nullptr) != (dx[i] == nullptr))
+            return invalid("an input and its two gradients must be given together");
+        if ((weight[i] == nullptr) != (dweight[i] == nullptr))
+            return invalid("a weight and its gradient must be given together");
+        if (x[i] == nullptr) {
+            if (weight[i] != nullptr)
+                return invalid("a weight without its input");
+            continue;
+        }
+        PAM_TRY(check_heads(*x[i], names[i][0], tokens));
+        PAM_TRY(check_heads(*dz[i], names[i][1], tokens));
+        PAM_TRY(check_written(*dx[i], names[i][2], tokens, d));
+        if (x[i]->heads != dz[i]->heads || x[i]->heads != dx[i]->heads)
+            return invalid(names[i][0], ": another count of heads than its gradients");
+        if (x[i]->type != type || dz[i]->type != type || dx[i]->type != type)
+            return invalid("inputs and gradients must have one type");
+        pamk::HeadGradPart &part = p.part[i];
+        part.x = x[i]->data;
+        part.dz = dz[i]->data;
+        part.dx = dx[i]->data;
+        part.weight = weight[i];
+        part.dweight = dweight[i];
+        part.x_token = x[i]->stride_token;
+        part.x_head = x[i]->stride_head;
+        part.dz_token = dz[i]->stride_token;
+        part.dz_head = dz[i]->stride_head;
+        part.dx_token = dx[i]->stride_token;
+        part.dx_head = dx[i]->stride_head;
+        part.heads = x[i]->heads;
+        rows[i] = tokens * x[i]->heads;
+        weights = weights || weight[i] != nullptr;
+    }
+    PAM_TRY(check_rotation(rotation, tokens, d));
+    PAM_TRY(check_rows(tokens, (int64_t)p.part[0].heads + p.part[1].heads));
+    if (tokens == 0 && !weights)
+        return PAM_SUCCESS;
+    p.tokens = tokens;
+    p.d = d;
+    p.eps = eps;
+    set_rotation(p, rotation);
+    const bool bf16 = is_bf16(type);
+    int most[2];
+    grad_budget(rows[0], rows[1], most);
+    for (int i = 0; i < 2; ++i)
+        p.part[i].groups = pamk::head_grad_groups(bf16, rows[i], d, p.rot, most[i]);
+    if (weights && tokens > 0) {
+        const size_t need = (size_t)((int64_t)(p.part[0].groups + p.part[1].groups) * d) * sizeof(float);
+        if (workspace == nullptr || workspace_bytes < need)
+            return invalid("workspace is NULL or smaller than pam_norm_rope_grad_workspace_size says");
+        if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0)
+            return invalid("workspace must be 16-byte aligned");
+        p.part[0].partial = static_cast<float *>(workspace);
+        p.part[1].partial = p.part[0].partial + (int64_t)p.part[0].groups * d;
+    }
+    PAM_TRY(api_check_device());
+    const hipError_t e = pamk::launch_head_grad(bf16, p, stream);
+    return e == hipSuccess ? PAM_SUCCESS : api_fail_hip(e, "pam_norm_rope_grad kernel launch");
+}
+
+pam_status_t pam_append_kv(int64_t tokens, int32_t d, const pam_heads_t *k, const float *k_weight,
+                           const pam_heads_t *v, const pam_heads_t *q_in, const float *q_weight,
+                           const pam_heads_t *q_out, float eps, const pam_rotation_t *rotation,
+                           const pam_cache_t *k_cache, const pam_cache_t *v_cache, const int64_t *slots,
+                           hipStream_t stream) {
+    PAM_TRY(check_dim(tokens, d, eps));
+    if (k == nullptr || v == nullptr || k_cache == nullptr || v_cache == nullptr)
+        return invalid("k, v, k_cache and v_cache must be non-NULL");
+    if ((q_in == nullptr) != (q_out == nullptr))
+        return invalid("q_in and q_out must be given together");
+    PAM_TRY(check_heads(*k, "k", tokens));
+    PAM_TRY(check_heads(*v, "v", tokens));
+    PAM_TRY(check_cache(*k_cache, "k_cache", tokens > 0));
+    PAM_TRY(check_cache(*v_cache, "v_cache", tokens > 0));
+    if (k->type != v->type || (q_in != nullptr && q_in->type != k->type))
+        return invalid("k, v and q_in must have one type");
+    if (k->heads != k_cache->heads || v->heads != v_cache->heads || k->heads != v->heads)
+        return invalid("k, v and the caches must have one count of heads");
+    if (k_cache->pages != v_cache->pages || k_cache->page_size != v_cache->page_size)
+        return invalid("the caches must have one count and size of pages");
+    PAM_TRY(check_rotation(rotation, tokens, d));
+    pamk::HeadRowsParams p{};
+    add_part(p, *k, k_weight, rotation != nullptr);
+    to_cache(p.part[0], *k_cache);
+    add_part(p, *v, nullptr, false);
+    to_cache(p.part[1], *v_cache);
+    if (q_in != nullptr) {
+        PAM_TRY(check_heads(*q_in, "q_in", tokens));
+        PAM_TRY(check_written(*q_out, "q_out", tokens, d));
+        if (q_in->heads != q_out->heads)
+            return invalid("q_out: another count of heads than the input");
+        add_part(p, *q_in, q_weight, rotation != nullptr);
+        to_heads(p.part[2], *q_out);
+    }
+    PAM_TRY(check_rows(tokens, p.heads));
+    if (tokens > 0 && slots == nullptr)
+        return invalid("slots is NULL");
+    if (tokens == 0)
+        return PAM_SUCCESS;
+    PAM_TRY(api_check_device());
+    p.tokens = tokens;
+    p.d = d;
+    p.eps = eps;
+    set_rotation(p, rotation);
+    p.slots = slots;
+    p.page_size = k_cache->page_size;
+    p.cache_slots = k_cache->pages * k_cache->page_size;
+    const hipError_t e = pamk::launch_head_rows(is_bf16(k->type), p, stream);
+    return e == hipSuccess ? PAM_SUCCESS : api_fail_hip(e, "pam_append_kv kernel launch");
+}
+
+pam_status_t pam_paged_attention_workspace_size(int32_t d, int32_t q_heads, int32_t kv_heads, pam_type_t kv_type,
+                                                int32_t batch, int32_t max_q, int32_t max_kv, size_t *bytes) {
+    if (bytes == nullptr)
+        return invalid("bytes is NULL");
+    if (kv_type != PAM_TYPE_F32 && kv_type != PAM_TYPE_BF16)
+        return invalid("kv_type must be PAM_TYPE_F32 or PAM_TYPE_BF16");
+    PAM_TRY(check_attention_sizes(d, q_heads, kv_heads, batch, max_q, max_kv));
+    *bytes = attention_plan(d, q_heads, kv_heads, is_bf16(kv_type), batch, max_q, max_kv).bytes();
+    return PAM_SUCCESS;
+}
+
+pam_status_t pam_paged_attention(int32_t d, const pam_heads_t *q, const pam_cache_t *k_cache,
+                                 const pam_cache_t *v_cache, const pam_sequences_t *sequences,
+                                 const pam_heads_t *out, void *workspace, size_t workspace_bytes,
+                                 hipStream_t stream) {
+    if (q == nullptr || k_cache == nullptr || v_cache == nullptr || sequences == nullptr || out == nullptr)
+        return invalid("q, k_cache, v_cache, sequences and out must be non-NULL");
+    const pam_sequences_t &s = *sequences;
+    if (s.tokens < 0)
+        return invalid("tokens must be >= 0");
+    PAM_TRY(check_attention_sizes(d, q->heads, k_cache->heads, s.batch, s.max_q, s.max_kv));
+    PAM_TRY(check_heads(*q, "q", s.tokens));
+    PAM_TRY(check_written(*out, "out", s.tokens, d));
+    if (out->type != PAM_TYPE_F32)
+        return invalid("out: must be PAM_TYPE_F32");
+    if (out->heads != q->heads)
+        return invalid("out: another count of heads than q");
+    PAM_TRY(check_cache(*k_cache, "k_cache", true));
+    PAM_TRY(check_cache(*v_cache, "v_cache", true));
+    if (k_cache->type != v_cache->type || k_cache->heads != v_cache->heads || k_cache->pages != v_cache->pages ||
+        k_cache->page_size != v_cache->page_size)
+        return invalid("the caches must agree in type, heads, pages and page_size");
+    if (s.table_width < 0 || s.table_stride < s.table_width || s.table_stride > kMaxStride)
+        return invalid("table_stride must be at least table_width, which must be >= 0");
+    if (s.max_kv > (int64_t)s.table_width * k_cache->page_size)
+        return invalid("max_kv must be at most table_width * page_size");
+    if (s.q_starts == nullptr && s.tokens < s.batch)
+        return invalid("without q_starts there must be one token a sequence");
+    if (!std::isfinite(s.scale))
+        return invalid("scale must be finite");
+    if (s.batch == 0 || s.tokens == 0 || s.max_q == 0)
+        return PAM_SUCCESS;
+    if (s.kv_lens == nullptr || (s.max_kv > 0 && s.table == nullptr))
+        return invalid("kv_lens and table must be non-NULL");
+    const bool bf16 = is_bf16(k_cache->type);
+    const AttentionPlan plan = attention_plan(d, q->heads, k_cache->heads, bf16, s.batch, s.max_q, s.max_kv);
+    if (plan.units * plan.splits > kMaxLaunchGroups)
+        return invalid("too many workgroups (batch * heads * rows * keys too large)");
+    if (plan.bytes() > 0) {
+        if (workspace == nullptr || workspace_bytes < plan.bytes())
+            return invalid("workspace is NULL or smaller than pam_paged_attention_workspace_size says");
+        if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0)
+            return invalid("workspace must be 16-byte aligned");
+    }
+    PAM_TRY(api_check_device());
+
+    pamk::AttentionParams p{};
+    p.q = q->data;
+    p.q_token = q->stride_token;
+    p.q_head = q->stride_head;
+    p.q_bf16 = is_bf16(q->type);
+    p.k = {k_cache->data, k_cache->stride_page, k_cache->stride_slot, k_cache->stride_head, k_cache->pages};
+    p.v = {v_cache->data, v_cache->stride_page, v_cache->stride_slot, v_cache->stride_head, v_cache->pages};
+    // key / page_size for key < 2^31 by a multiplication: with 2^l >= size,
+    // mul = 2^32 (2^l - size) / size + 1, (mulhi(key, mul) + key) >> l.
+    p.page_size = (uint32_t)k_cache->page_size;
+    while (((uint64_t)1 << p.page_shift) < p.page_size)
+        ++p.page_shift;
+    p.page_mul = (uint32_t)(((((uint64_t)1 << p.page_shift) - p.page_size) << 32) / p.page_size + 1);
+    p.q_starts = s.q_starts;
+    p.kv_lens = s.kv_lens;
+    p.table = s.table;
+    p.table_stride = s.table_stride;
+    p.out = static_cast<float *>(out->data);
+    p.out_token = out->stride_token;
+    p.out_head = out->stride_head;
+    p.tokens = s.tokens;
+    p.batch = s.batch;
+    p.kv_heads = k_cache->heads;
+    p.group = q->heads / k_cache->heads;
+    p.d = d;
+    p.max_q = s.q_starts == nullptr ? 1 : s.max_q;
+    p.max_kv = s.max_kv;
+    p.causal = s.causal;
+    p.window = s.window;
+    p.scale = (float)((double)s.scale * 1.4426950408889634);
+    p.rows = plan.rows;
+    p.row_blocks = plan.row_blocks;
+    p.splits = plan.splits;
+    p.split_keys = plan.split_keys;
+    p.scores = static_cast<float *>(workspace);
+    p.stats = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.scores);
+    p.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.scores + plan.stats);
+
+    hipError_t e;
+    if (plan.whole) {
+        e = pamk::launch_attention_whole(bf16, plan.lanes, p, stream);
+    } else {
+        e = pamk::launch_attention_scores(bf16, plan.lanes, p, stream);
+        if (e == hipSuccess)
+            e = pamk::launch_attention_values(bf16, plan.lanes, p, stream);
+        if (e == hipSuccess)
+            e = pamk::launch_attention_join(p, stream);
+    }
+    return e == hipSuccess ? PAM_SUCCESS : api_fail_hip(e, "pam_paged_attention kernel launch");
+}
+
+}  // extern "C"

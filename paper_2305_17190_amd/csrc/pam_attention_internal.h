@@ -1,0 +1,109 @@
+// Internal interface between the host layer of the attention-side operators
+// (pam_attention_api.cpp) and their HIP kernels (pam_heads.hip,
+// pam_attention.hip).
+#pragma once
+
+#include <stdint.h>
+#include <hip/hip_runtime_api.h>
+
+namespace pamk {
+
+// One operand of the head kernels: rows of d values at (token, head), written
+// to a tensor or, paged, to the slots of a cache.
+struct HeadPart {
+    const void *in;
+    void *out;
+    const float *weight;            // norm's weight, or nullptr: no norm
+    int64_t in_token, in_head;      // strides, elements
+    int64_t out_token, out_head;    // out_token: stride of a page where paged
+    int64_t out_slot;               // paged: stride of a slot
+    int32_t first, heads;           // heads first .. first + heads - 1 of a token's rows
+    int32_t out_bf16;
+    int32_t paged;
+    int32_t rotate;
+};
+
+struct HeadRowsParams {
+    HeadPart part[3];
+    int32_t parts;
+    int32_t heads;                  // of all parts
+    int64_t tokens;
+    int32_t d, rot, interleaved;
+    float eps;
+    const int32_t *positions;
+    const float *cos, *sin;
+    int64_t rows;                   // positions in the tables
+    const int64_t *slots;
+    int64_t cache_slots;            // pages * page_size
+    int32_t page_size;
+};
+
+// Norm and rotation of every part's rows, into tensors or cache slots.
+// bf16: the inputs are bfloat16.
+hipError_t launch_head_rows(bool bf16, const HeadRowsParams &p, hipStream_t stream);
+
+struct HeadGradPart {
+    const void *x, *dz;
+    void *dx;
+    const float *weight;
+    float *dweight;
+    float *partial;                 // [groups][d]
+    int64_t x_token, x_head, dz_token, dz_head, dx_token, dx_head;
+    int32_t heads;
+    int32_t groups;                 // workgroups of this part
+};
+
+struct HeadGradParams {
+    HeadGradPart part[2];
+    int64_t tokens;
+    int32_t d, rot, interleaved;
+    float eps;
+    const int32_t *positions;
+    const float *cos, *sin;
+    int64_t rows;
+};
+
+// About the most workgroups, and so rows of partial sums, of one gradient launch.
+constexpr int kHeadGradGroups = 1024;
+// How many workgroups `rows` rows keep busy, at most `most`.
+int head_grad_groups(bool bf16, int64_t rows, int d, int rot, int most);
+hipError_t launch_head_grad(bool bf16, const HeadGradParams &p, hipStream_t stream);
+
+// Keys or values of a paged cache.
+struct CacheView {
+    const void *data;
+    int64_t page, slot, head;       // strides, elements
+    int64_t pages;
+};
+
+// One PAM attention call.  A unit is (sequence, key head, row block): the rows
+// of a key head are its query heads of the sequence's new tokens, row =
+// token * group + query head in the group, `rows` of them a unit.
+struct AttentionParams {
+    const void *q;
+    int64_t q_token, q_head;
+    int32_t q_bf16;
+    CacheView k, v;
+    uint32_t page_size, page_mul, page_shift;   // key / page_size = (mulhi(key, mul) + key) >> shift
+    const int32_t *q_starts, *kv_lens, *table;
+    int64_t table_stride;
+    float *out;
+    int64_t out_token, out_head;
+    int64_t tokens;
+    int32_t batch, kv_heads, group, d;
+    int32_t max_q, max_kv, causal, window;
+    float scale;                    // times log2(e)
+    int32_t rows, row_blocks;
+    int32_t splits, split_keys;     // keys of a unit: splits of split_keys (a multiple of 64)
+    float *scores;                  // [unit][splits * split_keys][rows], in units of log2
+    float *stats;                   // [unit][split][2][rows]: maximum, sum of 2^(score - maximum)
+    float *partial;                 // [unit][split][rows][d]
+};
+
+// The kernels of pam_attention.hip, each for `lanes` lanes a key.
+hipError_t launch_attention_whole(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream);
+hipError_t launch_attention_scores(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream);
+hipError_t launch_attention_values(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream);
+hipError_t launch_attention_join(const AttentionParams &p, hipStream_t stream);
+
+}  // namespace pamk

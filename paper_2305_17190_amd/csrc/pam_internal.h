@@ -1,10 +1,13 @@
 // Internal interface between the C-ABI layer (pam_api.cpp) and the HIP
 // kernels (pam_gemm_dma.hip, pam_skinny.hip, pam_small.hip, pam_kernels.hip,
-// pa_ops.hip, pam_exact_grad.hip).  Not installed; not part of the public ABI.
+// pa_ops.hip, pam_exact_grad.hip).  The attention-side operators have theirs
+// in pam_attention_internal.h.  Not installed; not part of the public ABI.
 #pragma once
 
 #include <stdint.h>
 #include <hip/hip_runtime_api.h>
+
+#include "pam.h"
 
 namespace pamk {
 
@@ -39,6 +42,12 @@ struct GemmParams {
     const float *Mod;
     int64_t ldm;
 };
+
+// Error text and device check of the C entry points (pam_api.cpp), shared by
+// every host source.
+pam_status_t api_fail(pam_status_t status, const char *message);
+pam_status_t api_fail_hip(hipError_t error, const char *what);
+pam_status_t api_check_device();
 
 hipError_t launch_pam_mul(const float *a, const float *b, float *out, int64_t n, hipStream_t stream);
 
