@@ -27,119 +27,13 @@
 
 #include <algorithm>
 
-#include "pam_attention_internal.h"
-#include "pam_scalar.h"
+#include "pam_attention_device.h"
 
 namespace pamk {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr float kNegInf = -__builtin_inff();
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t u32x4a2 __attribute__((ext_vector_type(4), aligned(2)));
-
-// 16 bytes of cache elements: T is the element's storage.
-template <typename T> constexpr int kPer = 16 / sizeof(T);
-
-template <typename T> __device__ __forceinline__ u32x4 load16(const void *base, int64_t at) {
-    return *reinterpret_cast<const u32x4a2 *>(static_cast<const T *>(base) + at);
-}
-
-// Float32 encoding of element i of 16 loaded bytes.
-template <typename T> __device__ __forceinline__ uint32_t element(const u32x4 &w, int i) {
-    if constexpr (sizeof(T) == 4)
-        return w[i];
-    else
-        return i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16;
-}
-
-__device__ __forceinline__ uint32_t load_bits(const void *base, int64_t at, bool bf16) {
-    return bf16 ? (uint32_t) static_cast<const uint16_t *>(base)[at] << 16 : static_cast<const uint32_t *>(base)[at];
-}
-
-__device__ __forceinline__ float one_mantissa(uint32_t a) {
-    return __uint_as_float((a & kMant) | kBias);
-}
-__device__ __forceinline__ float power(uint32_t a) { return __uint_as_float(a & kSignExp); }
-
-// b' of an encoding: zeros and denormals as zero, NaN as inf.
-__device__ __forceinline__ uint32_t biased(uint32_t b) {
-    const uint32_t mag = b & kMag;
-    const uint32_t flushed = mag < kMinNormal ? 0u : mag > kInf ? kInf : mag;
-    return ((b & kSign) | flushed) - kBias;
-}
-
-__device__ __forceinline__ float pam_fma(float a1, float m, uint32_t b, float acc) {
-    return __builtin_fmaf(__uint_as_float(__float_as_uint(a1) + b), m, acc);
-}
-
-__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & kExpMask) != kExpMask; }
-
-// The unit a workgroup works on, and which keys its rows see.
-struct Unit {
-    int b, head, first_row, rows;   // rows of it that exist
-    int64_t first_token;            // token of row 0 of the sequence's block of new tokens
-    int64_t position;               // of the sequence's new token 0
-    int kv;                         // keys of the sequence, at most max_kv
-    int lo, hi;                     // keys any of the rows sees
-    const int32_t *table;
-
-    __device__ __forceinline__ Unit(const AttentionParams &p, int unit) {
-        const int block = unit % p.row_blocks;
-        const int bh = unit / p.row_blocks;
-        b = bh / p.kv_heads;
-        head = bh - b * p.kv_heads;
-        first_token = p.q_starts ? p.q_starts[b] : b;
-        const int64_t count = p.q_starts ? (int64_t)p.q_starts[b + 1] - first_token : 1;
-        const int64_t length = p.kv_lens[b];
-        kv = (int)std::min<int64_t>(std::max<int64_t>(length, 0), p.max_kv);
-        position = length - count;
-        table = p.table + (int64_t)b * p.table_stride;
-        first_row = block * p.rows;
-        int64_t live = std::min<int64_t>(count, p.max_q);
-        live = std::min<int64_t>(live, p.tokens - first_token);
-        if (first_token < 0)
-            live = 0;
-        rows = (int)std::min<int64_t>(std::max<int64_t>(live * p.group - first_row, 0), p.rows);
-        lo = hi = 0;
-        if (rows > 0) {
-            lo = row_lo(p, 0);
-            hi = row_hi(p, rows - 1);
-        }
-    }
-    __device__ __forceinline__ int token(const AttentionParams &p, int row) const { return (first_row + row) / p.group; }
-    // Keys lo <= j < hi are those the row sees (page permitting).
-    __device__ __forceinline__ int row_lo(const AttentionParams &p, int row) const {
-        if (p.window <= 0)
-            return 0;
-        const int64_t at = position + token(p, row) - p.window + 1;
-        return (int)std::min<int64_t>(std::max<int64_t>(at, 0), kv);
-    }
-    __device__ __forceinline__ int row_hi(const AttentionParams &p, int row) const {
-        if (!p.causal)
-            return kv;
-        return (int)std::min<int64_t>(std::max<int64_t>(position + token(p, row) + 1, 0), kv);
-    }
-    __device__ __forceinline__ int64_t q_at(const AttentionParams &p, int row) const {
-        const int i = token(p, row), g = first_row + row - i * p.group;
-        return (first_token + i) * p.q_token + (int64_t)(head * p.group + g) * p.q_head;
-    }
-    __device__ __forceinline__ int64_t out_at(const AttentionParams &p, int row) const {
-        const int i = token(p, row), g = first_row + row - i * p.group;
-        return (first_token + i) * p.out_token + (int64_t)(head * p.group + g) * p.out_head;
-    }
-    // Element offset of a key's row in a cache, or -1 where its page is not one.
-    __device__ __forceinline__ int64_t key_at(const AttentionParams &p, const CacheView &c, int key) const {
-        const uint32_t page = (__umulhi((uint32_t)key, p.page_mul) + (uint32_t)key) >> p.page_shift;
-        const int id = table[page];
-        if (id < 0 || id >= c.pages)
-            return -1;
-        return (int64_t)id * c.page + (int64_t)(key - (int)(page * p.page_size)) * c.slot + (int64_t)head * c.head;
-    }
-};
-
 // Scores of keys begin <= j < end (within the unit's lo .. hi) into
 // s[(j - begin) * R + row]; -inf where the row does not see the key.
 // `lanes` L lanes hold a key, 16 bytes each.
@@ -252,17 +146,6 @@ template <int R> __device__ __forceinline__ void row_sum(float (&l)[R], float *s
         for (int w = 0; w < (int)(blockDim.x >> 6); ++w)
             l[r] += scratch[w * R + r];
     }
-}
-
-// 2^(t - m); 0 for t = -inf also where the maximum is -inf.
-__device__ __forceinline__ float exp2_from(float t, float m) {
-    return __builtin_amdgcn_exp2f(t - (m == kNegInf ? 0.0f : m));
-}
-
-// A probability as b'; a row whose sum is NaN is set to NaN at the end.
-__device__ __forceinline__ uint32_t probability(float e, float inverse) {
-    const uint32_t bits = __float_as_uint(e * inverse);
-    return (bits < kMinNormal || bits >= kInf ? 0u : bits) - kBias;
 }
 
 // out[row][i] = sum over keys begin <= j < end of P .^ v, the probabilities'
@@ -505,18 +388,21 @@ __global__ void __launch_bounds__(kThreads) attention_values_kernel(const Attent
                         p.partial + ((int64_t)index * p.splits + split) * R * p.d);
 }
 
-// Third launch: a unit's outputs, the sums over its splits in order.
-__global__ void __launch_bounds__(kThreads) attention_join_kernel(const AttentionParams p) {
-    const Unit unit(p, blockIdx.x);
+// Third launch: the outputs, each the sum over its unit's splits in order; four
+// a thread.
+__global__ void __launch_bounds__(kThreads) attention_join_kernel(const AttentionParams p, int parts) {
+    const int index = blockIdx.x / parts;
+    const Unit unit(p, p.first_unit + index);
+    const int e = ((blockIdx.x % parts) * kThreads + threadIdx.x) * 4;
+    if (e >= unit.rows * p.d)
+        return;
     const int first = unit.lo / p.split_keys, last = unit.hi > unit.lo ? (unit.hi - 1) / p.split_keys : first - 1;
-    const float *partial = p.partial + (int64_t)blockIdx.x * p.splits * p.rows * p.d;
-    for (int e = threadIdx.x; e < unit.rows * p.d; e += blockDim.x) {
-        const int r = e / p.d, i = e - r * p.d;
-        float sum = 0.0f;
-        for (int j = first; j <= last; ++j)
-            sum += partial[(int64_t)j * p.rows * p.d + e];
-        p.out[unit.out_at(p, r) + i] = sum;
-    }
+    const float *partial = p.partial + (int64_t)index * p.splits * p.rows * p.d + e;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = first; j <= last; ++j)
+        sum += *reinterpret_cast<const f32x4 *>(partial + (int64_t)j * p.rows * p.d);
+    const int r = e / p.d;
+    *reinterpret_cast<f32x4 *>(p.out + unit.out_at(p, r) + (e - r * p.d)) = sum;
 }
 
 enum Which { kWhole, kScores, kValues };
@@ -566,9 +452,9 @@ hipError_t launch_attention_values(bool bf16, int lanes, const AttentionParams &
     return for_type(kValues, bf16, lanes, p, stream);
 }
 
-hipError_t launch_attention_join(const AttentionParams &p, hipStream_t stream) {
-    hipLaunchKernelGGL(attention_join_kernel, dim3((unsigned)(p.batch * p.kv_heads * p.row_blocks)), dim3(kThreads), 0,
-                       stream, p);
+hipError_t launch_attention_join(const AttentionParams &p, int units, hipStream_t stream) {
+    const int parts = (p.rows * p.d / 4 + kThreads - 1) / kThreads;
+    hipLaunchKernelGGL(attention_join_kernel, dim3((unsigned)(units * parts)), dim3(kThreads), 0, stream, p, parts);
     return hipGetLastError();
 }
 

@@ -157,17 +157,21 @@ void grad_budget(int64_t q_rows, int64_t k_rows, int (&most)[2]) {
 }
 
 // How an attention call is cut.
+enum class Form { whole, split, tiles };
 struct AttentionPlan {
-    int lanes;        // lanes a key in the kernels
+    Form form;
+    int lanes;        // lanes a key in the kernels for few rows
     int rows, row_blocks;
-    bool whole;
     int splits, split_keys;
     int64_t units;
-    size_t scores, stats, partial;   // workspace bytes of each
+    int64_t slab;     // units of one round of launches
+    size_t scores, stats, partial;   // workspace bytes of a slab
     size_t bytes() const { return scores + stats + partial; }
 };
 
 constexpr int64_t kWholeScores = 16384;   // scores of a unit kept in LDS at most (64 KiB)
+constexpr int64_t kTileRows = 24;         // fewest rows of a key head that run as tiles
+constexpr int64_t kSlabBytes = (int64_t)512 << 20;   // scores of one round of launches, about
 
 AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool bf16, int32_t batch, int32_t max_q,
                              int32_t max_kv) {
@@ -177,21 +181,36 @@ AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool 
     while (a.lanes * per < d)
         a.lanes *= 2;
     const int64_t rows = (int64_t)max_q * (q_heads / kv_heads);
-    a.rows = rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
+    if (rows >= kTileRows)
+        a.rows = rows <= 64 ? 64 : 128;
+    else
+        a.rows = rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
     a.row_blocks = (int)ceil_div(std::max<int64_t>(rows, 1), a.rows);
-    a.units = (int64_t)batch * kv_heads * a.row_blocks;
-    a.whole = (int64_t)max_kv * a.rows <= kWholeScores && (a.units >= 256 || max_kv <= 512);
+    a.units = a.slab = (int64_t)batch * kv_heads * a.row_blocks;
     a.splits = 1;
-    if (a.whole || a.units == 0)
+    a.form = rows >= kTileRows ? Form::tiles
+             : (int64_t)max_kv * a.rows <= kWholeScores && (a.units >= 256 || max_kv <= 512) ? Form::whole
+                                                                                            : Form::split;
+    if (a.form == Form::whole || a.units == 0)
         return a;
-    // About 2048 workgroups, of 256 to 1024 keys.
-    const int64_t keys = ceil_div((int64_t)max_kv * a.units, 2048);
-    a.split_keys = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(keys, 64) * 64, 256), 1024);
-    a.splits = (int)ceil_div(max_kv, a.split_keys);
-    const int64_t parts = a.units * a.splits;
+    if (a.form == Form::tiles) {
+        const int64_t keys = ceil_div(std::max(max_kv, 1), 128) * 128;
+        a.slab = std::min(a.units, std::max<int64_t>(kSlabBytes / (keys * a.rows * (int64_t)sizeof(float)), 1));
+        // Enough workgroups of the values for two a compute unit, of at least 256 keys.
+        const int64_t columns = d > 64 ? ceil_div(d, 128) : 1;
+        const int64_t want = ceil_div(512, a.slab * columns);
+        a.split_keys = (int)std::max<int64_t>(ceil_div(ceil_div(keys, want), 128) * 128, 256);
+    } else {
+        // About 2048 workgroups, of 256 to 1024 keys.
+        const int64_t keys = ceil_div((int64_t)max_kv * a.units, 2048);
+        a.split_keys = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(keys, 64) * 64, 256), 1024);
+    }
+    a.splits = (int)ceil_div(std::max(max_kv, 1), a.split_keys);
+    const int64_t parts = a.slab * a.splits;
+    const int64_t stats = parts * (a.form == Form::tiles ? a.split_keys / 128 : 1) * 2 * a.rows;
     a.scores = (size_t)(parts * a.split_keys * a.rows) * sizeof(float);
-    a.stats = (size_t)ceil_div(parts * 2 * a.rows, 4) * 16;
-    a.partial = (size_t)(parts * a.rows * d) * sizeof(float);
+    a.stats = (size_t)ceil_div(stats, 4) * 16;
+    a.partial = a.form == Form::tiles && a.splits == 1 ? 0 : (size_t)(parts * a.rows * d) * sizeof(float);
     return a;
 }
 
@@ -204,7 +223,7 @@ pam_status_t check_attention_sizes(int32_t d, int32_t q_heads, int32_t kv_heads,
     if (batch < 0 || max_q < 0 || max_kv < 0)
         return invalid("batch, max_q and max_kv must be >= 0");
     const int64_t rows = (int64_t)max_q * q_heads;
-    if (rows > kMaxRows || (batch > 0 && ceil_div(rows, 1) * (max_kv / 256 + 1) > ((int64_t)1 << 40) / batch))
+    if (rows > kMaxRows || (batch > 0 && rows > 0 && max_kv / 256 + 1 > ((int64_t)1 << 40) / batch / rows))
         return invalid("too many rows (batch * max_q * heads * max_kv too large)");
     return PAM_SUCCESS;
 }
@@ -440,7 +459,9 @@ pam_status_t pam_paged_attention(int32_t d, const pam_heads_t *q, const pam_cach
         return invalid("kv_lens and table must be non-NULL");
     const bool bf16 = is_bf16(k_cache->type);
     const AttentionPlan plan = attention_plan(d, q->heads, k_cache->heads, bf16, s.batch, s.max_q, s.max_kv);
-    if (plan.units * plan.splits > kMaxLaunchGroups)
+    const int64_t most_groups = plan.form == Form::tiles ? plan.slab * plan.splits * std::max(plan.split_keys / 128, 2)
+                                                         : plan.units * plan.splits;
+    if (plan.units > kMaxLaunchGroups || most_groups > kMaxLaunchGroups)
         return invalid("too many workgroups (batch * heads * rows * keys too large)");
     if (plan.bytes() > 0) {
         if (workspace == nullptr || workspace_bytes < plan.bytes())
@@ -488,15 +509,28 @@ pam_status_t pam_paged_attention(int32_t d, const pam_heads_t *q, const pam_cach
     p.stats = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.scores);
     p.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.scores + plan.stats);
 
-    hipError_t e;
-    if (plan.whole) {
+    if (plan.partial == 0)
+        p.partial = nullptr;
+
+    hipError_t e = hipSuccess;
+    if (plan.form == Form::whole) {
         e = pamk::launch_attention_whole(bf16, plan.lanes, p, stream);
-    } else {
+    } else if (plan.form == Form::split) {
         e = pamk::launch_attention_scores(bf16, plan.lanes, p, stream);
         if (e == hipSuccess)
             e = pamk::launch_attention_values(bf16, plan.lanes, p, stream);
         if (e == hipSuccess)
-            e = pamk::launch_attention_join(p, stream);
+            e = pamk::launch_attention_join(p, (int)plan.units, stream);
+    } else {
+        for (int64_t first = 0; first < plan.units && e == hipSuccess; first += plan.slab) {
+            const int units = (int)std::min(plan.slab, plan.units - first);
+            p.first_unit = (int32_t)first;
+            e = pamk::launch_tile_scores(bf16, p, units, stream);
+            if (e == hipSuccess)
+                e = pamk::launch_tile_values(bf16, p, units, stream);
+            if (e == hipSuccess && p.partial != nullptr)
+                e = pamk::launch_attention_join(p, units, stream);
+        }
     }
     return e == hipSuccess ? PAM_SUCCESS : api_fail_hip(e, "pam_paged_attention kernel launch");
 }

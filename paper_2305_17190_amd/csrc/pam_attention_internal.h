@@ -94,16 +94,22 @@ struct AttentionParams {
     int32_t max_q, max_kv, causal, window;
     float scale;                    // times log2(e)
     int32_t rows, row_blocks;
+    int32_t first_unit;             // of this launch; workspaces count units from it
     int32_t splits, split_keys;     // keys of a unit: splits of split_keys (a multiple of 64)
     float *scores;                  // [unit][splits * split_keys][rows], in units of log2
-    float *stats;                   // [unit][split][2][rows]: maximum, sum of 2^(score - maximum)
-    float *partial;                 // [unit][split][rows][d]
+    float *stats;                   // [unit][split, or tile of 128 keys][2][rows]: maximum, sum of 2^(score - maximum)
+    float *partial;                 // [unit][split][rows][d], or nullptr: one split, straight to the output
 };
 
-// The kernels of pam_attention.hip, each for `lanes` lanes a key.
+// Few rows a unit (pam_attention.hip), `lanes` lanes a key: one launch with
+// the scores in LDS, or two with the keys split.
 hipError_t launch_attention_whole(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream);
 hipError_t launch_attention_scores(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream);
 hipError_t launch_attention_values(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream);
-hipError_t launch_attention_join(const AttentionParams &p, hipStream_t stream);
+// Units of 64 or 128 rows (pam_attention_tile.hip); split_keys a multiple of 128.
+hipError_t launch_tile_scores(bool bf16, const AttentionParams &p, int units, hipStream_t stream);
+hipError_t launch_tile_values(bool bf16, const AttentionParams &p, int units, hipStream_t stream);
+// The outputs as the sums of the splits' parts, in order.
+hipError_t launch_attention_join(const AttentionParams &p, int units, hipStream_t stream);
 
 }  // namespace pamk
