@@ -26,34 +26,117 @@ namespace {
 
 constexpr int kStep = 16;             // k steps of a chunk
 constexpr int kPad = 4;               // words after each k step's row in LDS
-// Chunks whose sums a lane adds up before they join its totals: the float32
-// error of a sum grows with the length of its chain.
-constexpr int kChainChunks = 16;
+constexpr int kMaxSplit = 512;        // keys of a split at most
 
 // A lane's 8 rows or columns of a 64-wide block: two groups of four.
 __device__ __forceinline__ int place(int group, int i) { return (i / 4) * 32 + group * 4 + i % 4; }
 
-// acc[r][c] += b[k][row r] .^ a[k][column c] over one chunk in LDS.
-template <int BM, int BN>
-__device__ __forceinline__ void chunk_product(const float *a1, const float *m, const uint32_t *b, int row, int col,
+// One row of a k step, eight columns; the eight integer additions stand
+// together, then the eight float ones, so that neighbours are independent and
+// pair up with another wave's.  Plain: both encodings' exponent fields lie in
+// [64, 190], so a + b' is the encoding of their PAM itself.
+__device__ __forceinline__ void plain_row(float (&c)[8], uint32_t b, const uint32_t (&a)[8]) {
+    uint32_t t0, t1, t2, t3, t4, t5, t6, t7;
+    asm("v_add_u32 %[t0], %[a0], %[b]\n\tv_add_u32 %[t1], %[a1], %[b]\n\t"
+        "v_add_u32 %[t2], %[a2], %[b]\n\tv_add_u32 %[t3], %[a3], %[b]\n\t"
+        "v_add_u32 %[t4], %[a4], %[b]\n\tv_add_u32 %[t5], %[a5], %[b]\n\t"
+        "v_add_u32 %[t6], %[a6], %[b]\n\tv_add_u32 %[t7], %[a7], %[b]\n\t"
+        "v_add_f32 %[c0], %[c0], %[t0]\n\tv_add_f32 %[c1], %[c1], %[t1]\n\t"
+        "v_add_f32 %[c2], %[c2], %[t2]\n\tv_add_f32 %[c3], %[c3], %[t3]\n\t"
+        "v_add_f32 %[c4], %[c4], %[t4]\n\tv_add_f32 %[c5], %[c5], %[t5]\n\t"
+        "v_add_f32 %[c6], %[c6], %[t6]\n\tv_add_f32 %[c7], %[c7], %[t7]"
+        : [c0] "+v"(c[0]), [c1] "+v"(c[1]), [c2] "+v"(c[2]), [c3] "+v"(c[3]), [c4] "+v"(c[4]), [c5] "+v"(c[5]),
+          [c6] "+v"(c[6]), [c7] "+v"(c[7]), [t0] "=&v"(t0), [t1] "=&v"(t1), [t2] "=&v"(t2), [t3] "=&v"(t3),
+          [t4] "=&v"(t4), [t5] "=&v"(t5), [t6] "=&v"(t6), [t7] "=&v"(t7)
+        : [b] "v"(b), [a0] "v"(a[0]), [a1] "v"(a[1]), [a2] "v"(a[2]), [a3] "v"(a[3]), [a4] "v"(a[4]), [a5] "v"(a[5]),
+          [a6] "v"(a[6]), [a7] "v"(a[7]));
+}
+
+// acc[r][c] += b[k][row r] .^ a[k][column c] over one chunk in LDS: `plain` or,
+// for any values, with 1 + M and the power of two taken apart here.
+// FIX: b' is an encoding less the bias of any value, zeros and NaN among them.
+template <int BM, int BN, bool FIX>
+__device__ __forceinline__ void chunk_product(const uint32_t *a, const uint32_t *b, int row, int col, bool plain,
                                               float (&acc)[8][8]) {
-#pragma unroll 2
-    for (int k = 0; k < kStep; ++k) {
-        float x[8], y[8];
-        uint32_t z[8];
+    auto read = [](const uint32_t *from, uint32_t (&x)[8]) {
+        *reinterpret_cast<uint4 *>(x) = *reinterpret_cast<const uint4 *>(from);
+        *reinterpret_cast<uint4 *>(x + 4) = *reinterpret_cast<const uint4 *>(from + 32);
+    };
+    // Two loops one after the other, of which one runs, by a count the compiler
+    // cannot see through: as two branches the sums would be copied where they
+    // meet, in 64 more registers.
+    int first = __builtin_amdgcn_readfirstlane(plain ? kStep : 0);
+    asm("" : "+s"(first));
+    for (int k = 0; k < first; k += 2) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            *reinterpret_cast<float4 *>(x + 4 * h) = *reinterpret_cast<const float4 *>(a1 + k * (BN + kPad) + col + 32 * h);
-            *reinterpret_cast<float4 *>(y + 4 * h) = *reinterpret_cast<const float4 *>(m + k * (BN + kPad) + col + 32 * h);
-            *reinterpret_cast<uint4 *>(z + 4 * h) = *reinterpret_cast<const uint4 *>(b + k * (BM + kPad) + row + 32 * h);
+            uint32_t x[8], z[8];
+            read(a + (k + h) * (BN + kPad) + col, x);
+            read(b + (k + h) * (BM + kPad) + row, z);
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                plain_row(acc[r], z[r], x);
+        }
+    }
+#pragma unroll 1
+    for (int k = first; k < kStep; ++k) {
+        uint32_t x[8], z[8];
+        read(a + k * (BN + kPad) + col, x);
+        read(b + k * (BM + kPad) + row, z);
+        if constexpr (FIX) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                z[r] = biased(z[r] + kBias);
         }
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
+        for (int c = 0; c < 8; ++c) {
+            const float one = one_mantissa(x[c]), m = power(x[c]);
 #pragma unroll
-            for (int c = 0; c < 8; ++c)
-                acc[r][c] = pam_fma(x[c], y[c], z[r], acc[r][c]);
+            for (int r = 0; r < 8; ++r)
+                acc[r][c] = pam_fma(one, m, z[r], acc[r][c]);
+        }
     }
 }
+
+// Keeps track of whether an encoding's exponent field is outside [64, 190]: the
+// largest of 2 |x| - 2 * 2^(64 - 127)'s encoding, below which all are inside.
+struct Odd {
+    uint32_t most = 0, most16 = 0;
+    __device__ __forceinline__ void take(uint32_t x, uint32_t y) {
+        const uint32_t u = (x << 1) - (64u << 24), v = (y << 1) - (64u << 24);
+        most = max(max(most, u), v);
+    }
+    // Two bfloat16 values in one word.
+    __device__ __forceinline__ void take16(uint32_t w) {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        const u16x2 u = __builtin_bit_cast(u16x2, w) * (uint16_t)2 - (uint16_t)(64u << 8);
+        most16 = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, most16), u));
+    }
+    __device__ __forceinline__ bool any() const {
+        return most >= (127u << 24) || (most16 & 0xFFFFu) >= (127u << 8) || (most16 >> 16) >= (127u << 8);
+    }
+};
+
+// The sum or maximum over the 8 lanes that share a lane's rows.
+__device__ __forceinline__ float eight_max(float x) {
+    x = fmaxf(x, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0xB1, 0xF, 0xF, false)));   // lane ^ 1
+    x = fmaxf(x, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x4E, 0xF, 0xF, false)));   // lane ^ 2
+    return fmaxf(x, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x141, 0xF, 0xF, false)));   // 7 - lane
+}
+__device__ __forceinline__ float eight_sum(float x) {
+    x += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0xB1, 0xF, 0xF, false));
+    x += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x4E, 0xF, 0xF, false));
+    return x + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x141, 0xF, 0xF, false));
+}
+
+// The chunks' staging: two buffers in turn, and for each chunk a word that says
+// whether an element of it keeps it from the plain form; four of those words,
+// so that one is cleared two chunks before it is written.
+template <int BM, int BN> struct Buffers {
+    uint32_t a[2][kStep * (BN + kPad)];
+    uint32_t b[2][kStep * (BM + kPad)];
+    uint32_t odd[4];
+};
 
 __device__ __forceinline__ bool all_finite(const float (&acc)[8][8]) {
     float probe = 0.0f;                // NaN once any element is inf or NaN
@@ -98,19 +181,31 @@ struct Eight {
     __device__ __forceinline__ uint32_t operator()(int i, bool bf16) const {
         return bf16 ? element<uint16_t>(w[0], i) : w[i / 4][i % 4];
     }
+    // All eight as ones.
+    __device__ __forceinline__ void ones(bool bf16) {
+        const uint32_t one = bf16 ? kBias >> 16 | kBias : kBias;
+        w[0] = w[1] = u32x4{one, one, one, one};
+    }
+    __device__ __forceinline__ void check(Odd &odd, bool bf16) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (bf16)
+                odd.take16(w[0][i]);
+            else
+                odd.take(w[i / 2][i % 2 * 2], w[i / 2][i % 2 * 2 + 1]);
+    }
 };
 
 template <typename T, int WM, int WN, bool QB>
-__global__ void __launch_bounds__(64 * WM * WN) tile_scores_kernel(const AttentionParams p) {
+__global__ void __launch_bounds__(64 * WM * WN, 16 / (WM * WN)) tile_scores_kernel(const AttentionParams p) {
     constexpr int BM = 64 * WM, BN = 64 * WN, NT = 64 * WM * WN;
     constexpr int KI = 2 / WM > 0 ? 2 / WM : 1;    // key items of 8 values a lane and chunk
     constexpr int QI = 2 / WN > 0 ? 2 / WN : 1;    // query items
     constexpr bool KB = sizeof(T) == 2;
-    __shared__ float a1[kStep * (BN + kPad)], am[kStep * (BN + kPad)];
-    __shared__ uint32_t qb[kStep * (BM + kPad)];
+    __shared__ Buffers<BM, BN> buf;
     __shared__ int lo[BM], hi[BM];
     __shared__ int valid[BN];
-    __shared__ float across[WN][BM];
+    __shared__ float across[2][WN][BM];
 
     const int tiles = p.splits * (p.split_keys / BN);
     const int tile = blockIdx.x % tiles, index = blockIdx.x / tiles;
@@ -126,56 +221,72 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_scores_kernel(const Attenti
         lo[r] = r < unit.rows ? unit.row_lo(p, r) : 0;
         hi[r] = r < unit.rows ? unit.row_hi(p, r) : 0;
     }
+    // Keys that every row sees, page permitting.
+    const int most_lo = unit.rows == BM ? unit.row_lo(p, BM - 1) : p.max_kv, least_hi = unit.row_hi(p, 0);
     // The lane's keys and queries: one row each for all chunks.
     int64_t k_from[KI], q_from[QI];
+    bool missing = false;
 #pragma unroll
     for (int i = 0; i < KI; ++i) {
         const int item = tid + i * NT, j = item % BN, key = begin + j;
         k_from[i] = key >= unit.lo && key < unit.hi ? unit.key_at(p, p.k, key) : -1;
         if (item / BN == 0)
             valid[j] = k_from[i] >= 0;
+        missing = missing || k_from[i] < 0;
     }
+    const bool none_missing = !__syncthreads_or(missing);
 #pragma unroll
     for (int i = 0; i < QI; ++i) {
         const int r = (tid + i * NT) % BM;
         q_from[i] = r < unit.rows ? unit.q_at(p, r) : -1;
     }
 
+    // Keys and rows that do not exist hold ones: nothing of them is kept, and
+    // the chunk stays plain.
     Eight kw[KI], qw[QI];
     auto fetch = [&](int d0) {
 #pragma unroll
         for (int i = 0; i < KI; ++i) {
             const int at = d0 + (tid + i * NT) / BN * 8;
-            kw[i].clear();
-            if (k_from[i] >= 0 && at < p.d)
+            if (k_from[i] < 0)
+                kw[i].ones(KB);
+            else if (at < p.d)
                 kw[i].load(p.k.data, k_from[i] + at, KB);
+            else
+                kw[i].clear();
         }
 #pragma unroll
         for (int i = 0; i < QI; ++i) {
             const int at = d0 + (tid + i * NT) / BM * 8;
-            qw[i].clear();
-            if (q_from[i] >= 0 && at < p.d)
+            if (q_from[i] < 0)
+                qw[i].ones(QB);
+            else if (at < p.d)
                 qw[i].load(p.q, q_from[i] + at, QB);
+            else
+                qw[i].clear();
         }
     };
-    auto stage = [&]() {
+    auto stage = [&](int chunk) {
+        uint32_t *a = buf.a[chunk & 1], *b = buf.b[chunk & 1];
+        Odd odd;
 #pragma unroll
         for (int i = 0; i < KI; ++i) {
             const int item = tid + i * NT, j = item % BN, k = item / BN * 8;
+            kw[i].check(odd, KB);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t a = kw[i](e, KB);
-                a1[(k + e) * (BN + kPad) + j] = one_mantissa(a);
-                am[(k + e) * (BN + kPad) + j] = power(a);
-            }
+            for (int e = 0; e < 8; ++e)
+                a[(k + e) * (BN + kPad) + j] = kw[i](e, KB);
         }
 #pragma unroll
         for (int i = 0; i < QI; ++i) {
             const int item = tid + i * NT, r = item % BM, k = item / BM * 8;
+            qw[i].check(odd, QB);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                qb[(k + e) * (BM + kPad) + r] = biased(qw[i](e, QB));
+                b[(k + e) * (BM + kPad) + r] = qw[i](e, QB) - kBias;
         }
+        if (odd.any())
+            buf.odd[chunk & 3] = 1;
     };
 
     float acc[8][8];
@@ -184,14 +295,21 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_scores_kernel(const Attenti
 #pragma unroll
         for (int c = 0; c < 8; ++c)
             acc[r][c] = 0.0f;
+    if (tid < 4)
+        buf.odd[tid] = 0;
     fetch(0);
-    for (int d0 = 0; d0 < p.d; d0 += kStep) {
+    __syncthreads();
+    stage(0);
+    const int chunks = (p.d + kStep - 1) / kStep;
+    for (int c = 0; c < chunks; ++c) {
+        if (c + 1 < chunks)
+            fetch((c + 1) * kStep);
         __syncthreads();
-        stage();
-        __syncthreads();
-        if (d0 + kStep < p.d)
-            fetch(d0 + kStep);
-        chunk_product<BM, BN>(a1, am, qb, row0, col0, acc);
+        if (tid == 0)
+            buf.odd[(c + 2) & 3] = 0;
+        chunk_product<BM, BN, true>(buf.a[c & 1], buf.b[c & 1], row0, col0, buf.odd[c & 3] == 0, acc);
+        if (c + 1 < chunks)
+            stage(c + 1);
     }
 
     if (!all_finite(acc))
@@ -209,25 +327,38 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_scores_kernel(const Attenti
             return sum;
         });
 
-    // Scaled scores, -inf where the row does not see the key; the rows' maxima.
+    // Scaled scores, -inf where the row does not see the key and 0 in rows that
+    // do not exist; the rows' maxima and sums.
     float *scores = p.scores + ((int64_t)index * tiles * BN + begin) * BM;
-    float best[8];
+    float best[8], sum[8];
+    const bool inside = begin >= most_lo && begin + BN <= least_hi && none_missing;
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
-        const int row = row0 + place(0, r);
         best[r] = kNegInf;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            const int j = col0 + place(0, c);
-            const bool sees = valid[j] && begin + j >= lo[row] && begin + j < hi[row];
-            acc[r][c] = sees ? acc[r][c] * p.scale : kNegInf;
-            best[r] = fmaxf(best[r], acc[r][c]);
-        }
+        for (int c = 0; c < 8; ++c)
+            acc[r][c] *= p.scale;
+    }
+    if (!inside) {
 #pragma unroll
-        for (int x = 1; x < 8; x *= 2)
-            best[r] = fmaxf(best[r], __shfl_xor(best[r], x));
+        for (int r = 0; r < 8; ++r) {
+            const int row = row0 + place(0, r);
+            const int low = lo[row] - begin, high = hi[row] - begin;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const int j = col0 + place(0, c);
+                acc[r][c] = row >= unit.rows ? 0.0f : valid[j] && j >= low && j < high ? acc[r][c] : kNegInf;
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+            best[r] = fmaxf(best[r], acc[r][c]);
+        best[r] = eight_max(best[r]);
         if (tx == 0)
-            across[wave / WM][row] = best[r];
+            across[0][wave / WM][row0 + place(0, r)] = best[r];
     }
 #pragma unroll
     for (int c = 0; c < 8; ++c)
@@ -236,26 +367,21 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_scores_kernel(const Attenti
             *reinterpret_cast<float4 *>(scores + (int64_t)(col0 + place(0, c)) * BM + row0 + 32 * h) =
                 make_float4(acc[4 * h][c], acc[4 * h + 1][c], acc[4 * h + 2][c], acc[4 * h + 3][c]);
     __syncthreads();
-    float sum[8];
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
         const int row = row0 + place(0, r);
 #pragma unroll
         for (int w = 0; w < WN; ++w)
-            best[r] = fmaxf(best[r], across[w][row]);
+            best[r] = fmaxf(best[r], across[0][w][row]);
+        const float m = best[r] == kNegInf ? 0.0f : best[r];
         sum[r] = 0.0f;
 #pragma unroll
         for (int c = 0; c < 8; ++c)
-            sum[r] += exp2_from(acc[r][c], best[r]);
-#pragma unroll
-        for (int x = 1; x < 8; x *= 2)
-            sum[r] += __shfl_xor(sum[r], x);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < 8; ++r)
+            sum[r] += __builtin_amdgcn_exp2f(acc[r][c] - m);
+        sum[r] = eight_sum(sum[r]);
         if (tx == 0)
-            across[wave / WM][row0 + place(0, r)] = sum[r];
+            across[1][wave / WM][row] = sum[r];
+    }
     __syncthreads();
     float *stats = p.stats + ((int64_t)index * tiles + tile) * 2 * BM;
 #pragma unroll
@@ -265,14 +391,14 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_scores_kernel(const Attenti
             float total = 0.0f;
 #pragma unroll
             for (int w = 0; w < WN; ++w)
-                total += across[w][row];
+                total += across[1][w][row];
             stats[row] = best[r];
             stats[BM + row] = total;
         }
 }
 
 template <typename T, int WM, int WN>
-__global__ void __launch_bounds__(64 * WM * WN) tile_values_kernel(const AttentionParams p) {
+__global__ void __launch_bounds__(64 * WM * WN, 16 / (WM * WN)) tile_values_kernel(const AttentionParams p) {
     constexpr int BM = 64 * WM, BN = 64 * WN, NT = 64 * WM * WN;
     constexpr int E = kPer<T>;
     constexpr int SI = kStep * BM / 4 / NT;        // score items of 4 rows a lane and chunk
@@ -280,10 +406,9 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_values_kernel(const Attenti
     constexpr int SK = NT / (BM / 4);              // keys between a lane's score items
     constexpr int VK = NT / (BN / E);              // and between its value items
     constexpr bool VB = sizeof(T) == 2;
-    __shared__ float a1[kStep * (BN + kPad)], am[kStep * (BN + kPad)];
-    __shared__ uint32_t pb[kStep * (BM + kPad)];
+    __shared__ Buffers<BM, BN> buf;
     __shared__ float row_max[BM], row_sum[BM];
-    __shared__ int lo[BM], hi[BM];
+    __shared__ int64_t from[kMaxSplit];            // the split's keys, -1: none
 
     const int dtiles = (p.d + BN - 1) / BN;
     const int col_tile = blockIdx.x % dtiles;
@@ -308,11 +433,16 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_values_kernel(const Attenti
             m = fmaxf(m, stats[(int64_t)t * 2 * BM + r]);
         for (int t = first; t <= last; ++t)
             l += stats[(int64_t)t * 2 * BM + BM + r] * exp2_from(stats[(int64_t)t * 2 * BM + r], m);
-        row_max[r] = m;
+        row_max[r] = m == kNegInf ? 0.0f : m;
         row_sum[r] = l;
-        lo[r] = r < unit.rows ? unit.row_lo(p, r) : 0;
-        hi[r] = r < unit.rows ? unit.row_hi(p, r) : 0;
     }
+    const int start = begin / kStep * kStep;
+    for (int j = tid; j < p.split_keys; j += NT) {
+        const int key = start + j;
+        from[j] = key >= begin && key < end ? unit.key_at(p, p.v, key) : -1;
+    }
+    if (tid < 4)
+        buf.odd[tid] = 0;
     __syncthreads();
     const int my_row = tid % (BM / 4) * 4;
     float m4[4], inverse4[4];
@@ -320,116 +450,101 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_values_kernel(const Attenti
     for (int i = 0; i < 4; ++i) {
         m4[i] = row_max[my_row + i];
         const float l = row_sum[my_row + i];
-        inverse4[i] = l > 0.0f ? 1.0f / l : 0.0f;
+        inverse4[i] = my_row + i >= unit.rows ? 1.0f : l > 0.0f ? 1.0f / l : 0.0f;
     }
 
     const float *scores = p.scores + (int64_t)index * tiles * kTile * BM;
     const int col = tid % (BN / E) * E, column = col_tile * BN + col;
+    // Columns that do not exist hold ones, as rows do.
+    const uint32_t none = column < p.d ? 0u : VB ? kBias >> 16 | kBias : kBias;
     float4 sw[SI];
     u32x4 vw[VI];
-    int64_t v_from[VI];
-    auto locate = [&](int k0) {
-#pragma unroll
-        for (int i = 0; i < VI; ++i) {
-            const int key = k0 + tid / (BN / E) + i * VK;
-            v_from[i] = key >= begin && key < end && column < p.d ? unit.key_at(p, p.v, key) : -1;
-        }
-    };
     auto fetch = [&](int k0) {
 #pragma unroll
         for (int i = 0; i < SI; ++i)
             sw[i] = *reinterpret_cast<const float4 *>(scores + (int64_t)(k0 + tid / (BM / 4) + i * SK) * BM + my_row);
 #pragma unroll
         for (int i = 0; i < VI; ++i) {
-            vw[i] = u32x4{0, 0, 0, 0};
-            if (v_from[i] >= 0)
-                vw[i] = load16<T>(p.v.data, v_from[i] + column);
+            const int64_t at = from[k0 - start + tid / (BN / E) + i * VK];
+            if (at >= 0 && column < p.d)
+                vw[i] = load16<T>(p.v.data, at + column);
+            else
+                vw[i] = u32x4{none, none, none, none};
         }
     };
-    auto stage = [&](int k0) {
+    // Scores outside the split's keys are -inf, those of rows that do not exist
+    // 0: probabilities 0 and 1.  A NaN row's probabilities are anything.
+    auto stage = [&](int chunk) {
+        uint32_t *a = buf.a[chunk & 1], *b = buf.b[chunk & 1];
+        Odd odd;
+        float least = 1.0f;
 #pragma unroll
         for (int i = 0; i < SI; ++i) {
             const int k = tid / (BM / 4) + i * SK;
-            const bool mine = k0 + k >= begin && k0 + k < end;
             const float t[4] = {sw[i].x, sw[i].y, sw[i].z, sw[i].w};
-            uint32_t b[4];
+            uint32_t x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                b[e] = mine ? probability(exp2_from(t[e], m4[e]), inverse4[e]) : 0u - kBias;
-            *reinterpret_cast<uint4 *>(pb + k * (BM + kPad) + my_row) = make_uint4(b[0], b[1], b[2], b[3]);
+            for (int e = 0; e < 4; ++e) {
+                const float pr = __builtin_amdgcn_exp2f(t[e] - m4[e]) * inverse4[e];
+                least = fminf(least, pr);
+                x[e] = __float_as_uint(pr) - kBias;
+            }
+            *reinterpret_cast<uint4 *>(b + k * (BM + kPad) + my_row) = make_uint4(x[0], x[1], x[2], x[3]);
         }
 #pragma unroll
         for (int i = 0; i < VI; ++i) {
             const int at = (tid / (BN / E) + i * VK) * (BN + kPad) + col;
 #pragma unroll
-            for (int e = 0; e < E; e += 4) {
-                float x[4], y[4];
+            for (int e = 0; e < 4; ++e)
+                if (VB)
+                    odd.take16(vw[i][e]);
+                else if (e % 2 == 0)
+                    odd.take(vw[i][e], vw[i][e + 1]);
 #pragma unroll
-                for (int f = 0; f < 4; ++f) {
-                    const uint32_t a = element<T>(vw[i], e + f);
-                    x[f] = one_mantissa(a);
-                    y[f] = power(a);
-                }
-                *reinterpret_cast<float4 *>(a1 + at + e) = make_float4(x[0], x[1], x[2], x[3]);
-                *reinterpret_cast<float4 *>(am + at + e) = make_float4(y[0], y[1], y[2], y[3]);
-            }
+            for (int e = 0; e < E; e += 4)
+                *reinterpret_cast<uint4 *>(a + at + e) =
+                    make_uint4(element<T>(vw[i], e), element<T>(vw[i], e + 1), element<T>(vw[i], e + 2),
+                               element<T>(vw[i], e + 3));
         }
+        if (odd.any() || least < 0x1p-63f)
+            buf.odd[chunk & 3] = 1;
     };
 
-    float acc[8][8], total[8][8];
+    float acc[8][8];
 #pragma unroll
     for (int r = 0; r < 8; ++r)
 #pragma unroll
         for (int c = 0; c < 8; ++c)
-            acc[r][c] = total[r][c] = 0.0f;
-    const int start = begin / kStep * kStep;
-    if (begin < end) {
-        locate(start);
+            acc[r][c] = 0.0f;
+    const int chunks = begin < end ? (end - start + kStep - 1) / kStep : 0;
+    if (chunks > 0) {
         fetch(start);
-        if (start + kStep < end)
-            locate(start + kStep);
+        stage(0);
     }
-    int chain = 0;
-    for (int k0 = start; k0 < end; k0 += kStep) {
+    for (int c = 0; c < chunks; ++c) {
+        if (c + 1 < chunks)
+            fetch(start + (c + 1) * kStep);
         __syncthreads();
-        stage(k0);
-        __syncthreads();
-        if (k0 + kStep < end) {
-            fetch(k0 + kStep);
-            if (k0 + 2 * kStep < end)
-                locate(k0 + 2 * kStep);
-        }
-        chunk_product<BM, BN>(a1, am, pb, row0, col0, acc);
-        if (++chain == kChainChunks) {
-            chain = 0;
-#pragma unroll
-            for (int r = 0; r < 8; ++r)
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    total[r][c] += acc[r][c];
-                    acc[r][c] = 0.0f;
-                }
-        }
+        if (tid == 0)
+            buf.odd[(c + 2) & 3] = 0;
+        chunk_product<BM, BN, false>(buf.a[c & 1], buf.b[c & 1], row0, col0, buf.odd[c & 3] == 0, acc);
+        if (c + 1 < chunks)
+            stage(c + 1);
     }
-#pragma unroll
-    for (int r = 0; r < 8; ++r)
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-            total[r][c] += acc[r][c];
 
-    if (!all_finite(total))
-        sum_again(total, [&](int r, int c, float value) {
+    if (!all_finite(acc))
+        sum_again(acc, [&](int r, int c, float value) {
             const int row = row0 + place(0, r), i = col_tile * BN + col0 + place(0, c);
-            if (row >= unit.rows || i >= p.d)
+            if (row >= unit.rows || i >= p.d || !(row_sum[row] > 0.0f))
                 return value;
-            const float m = row_max[row], inverse = row_sum[row] > 0.0f ? 1.0f / row_sum[row] : 0.0f;
+            const float m = row_max[row], inverse = 1.0f / row_sum[row];
             float sum = 0.0f;
-            for (int key = max(begin, lo[row]); key < min(end, hi[row]); ++key) {
-                const int64_t from = unit.key_at(p, p.v, key);
-                if (from < 0)
+            for (int key = max(begin, unit.row_lo(p, row)); key < min(end, unit.row_hi(p, row)); ++key) {
+                const int64_t at = from[key - start];
+                if (at < 0)
                     continue;
                 const uint32_t b = probability(exp2_from(scores[(int64_t)key * BM + row], m), inverse);
-                sum += __uint_as_float(pam_full(b + kBias, load_bits(p.v.data, from + i, VB)));
+                sum += __uint_as_float(pam_full(b + kBias, load_bits(p.v.data, at + i, VB)));
             }
             return sum;
         });
@@ -446,7 +561,7 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_values_kernel(const Attenti
             const int i = col_tile * BN + col0 + 32 * h;
             if (i >= p.d)
                 continue;
-            f32x4 v = {total[r][4 * h], total[r][4 * h + 1], total[r][4 * h + 2], total[r][4 * h + 3]};
+            f32x4 v = {acc[r][4 * h], acc[r][4 * h + 1], acc[r][4 * h + 2], acc[r][4 * h + 3]};
             if (!(l > 0.0f))               // no weight, or a NaN score
                 v = f32x4{l, l, l, l};
             *reinterpret_cast<f32x4 *>(to + i) = v;
