@@ -1,31 +1,30 @@
-// PAM attention over a paged key/value cache for gfx950 (Kosson & Jaggi, Sec.
-// 3.2: the attention's products Q K^T and P V are PAM products, the softmax
-// between them is ordinary).
+// PAM attention of few rows over a paged key/value cache for gfx950 (Kosson &
+// Jaggi, Sec. 3.2: the attention's products Q K^T and P V are PAM products, the
+// softmax between them is ordinary): single tokens, and the few tokens of a
+// short chunk.
 //
 //   s_j = scale sum_i q_i .^ k_ji,  P_j = exp(s_j - max s) / sum exp(s - max s),
 //   out_i = sum_j P_j .^ v_ji
 //
 // The sum of the exponentials is known before the second product: PAM
 // commutes with powers of two only, so P V cannot be rescaled afterwards, and
-// each unit of work (a key head of a sequence and some of its rows) first
+// each unit of work (a key head of a sequence and up to 8 of its rows) first
 // scores all its keys, then reads the values.
 //
-// PAM on float hardware: for a = 2^E (1 + M) let a1 be the encoding of 1 + M
-// and m = a with its mantissa cleared (+-2^E; +-0 for zeros and denormals),
-// and b' = b's encoding less one bias.  a1 + b' as integers is the encoding of
-// PAM(1 + M, b), and times m it is PAM(a, b) wherever that is a normal number:
-// an integer addition and a float fma a term.  Keys and values are `a`, made
-// once for all rows; queries and probabilities are `b`, where a zero's sum
-// stays below the normal range and reads as zero.  A value with exponent
-// field 255 has m = +-inf, and b = NaN is given inf's encoding, so that any
-// NaN, inf or product past the range leaves a non-finite sum: such sums are
-// computed again term by term from the complete definition, over the keys the
-// row sees only.
-
-#include <hip/hip_runtime.h>
-#include <stdint.h>
-
-#include <algorithm>
+// A wave takes 64 keys at a time.  Lane i looks up key i's page; then every
+// load of a wave fetches 64 / L whole keys, L neighbouring lanes 16 bytes each,
+// so that a cache line is used by the lanes of one load, and all L loads of the
+// 64 keys are on their way before the first is used.  Scores: a lane has the
+// partial sums of its 16 bytes of each key; adding them up over the L lanes
+// halves the number of sums a lane holds with each step (one half goes to the
+// lane's partner, the other half comes), so that lane i ends with one key's
+// whole sums after L - 1 additions a row instead of L log2 L.  Values: a lane
+// keeps its 16 bytes' worth of outputs over all keys, the probabilities come
+// from LDS, where lane i put key i's.
+//
+// Bound by memory for up to about 4 rows, by the vector ALU beyond: for each
+// bfloat16 value read, 2 full-rate ops a row and 2.5 half-rate ones to take it
+// apart.
 
 #include "pam_attention_device.h"
 
@@ -33,40 +32,146 @@ namespace pamk {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
-// Scores of keys begin <= j < end (within the unit's lo .. hi) into
-// s[(j - begin) * R + row]; -inf where the row does not see the key.
-// `lanes` L lanes hold a key, 16 bytes each.
-template <typename T, int L, int R>
-__device__ __forceinline__ void score_keys(const AttentionParams &p, const Unit &unit, int begin, int end, float *s,
-                                           const int *lo, const int *hi) {
-    constexpr int E = kPer<T>;
-    constexpr int K = 64 / L;         // keys of one load of a wave
-    constexpr int U = 4;              // loads in flight
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int at = (lane % L) * E;
-    const bool holds = at < p.d;
-    uint32_t q[R][E];
+constexpr int kMostWaves = 8;
+constexpr int kGroup = 64;            // keys a wave takes at a time
+
+__device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x); }
+__device__ __forceinline__ float real(uint32_t x) { return __uint_as_float(x); }
+
+template <int CTRL> __device__ __forceinline__ float dpp(float x) {
+    return real(__builtin_amdgcn_mov_dpp(bits(x), CTRL, 0xF, 0xF, false));
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140, kRotate8 = 0x128;
+
+// The sums of a (lanes with bit BIT of their number clear) and of b (set) over
+// the two lanes of a pair.  Pairs differ in BIT, and in lower bits at will: the
+// steps run from the highest bit down.
+template <int BIT> __device__ __forceinline__ float merge(float a, float b, int lane) {
+    if constexpr (BIT >= 4) {
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        const u32x2 s = BIT == 5 ? __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(bits(a), bits(b), false, false))
+                                 : __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(bits(a), bits(b), false, false));
+        return real(s.x) + real(s.y);
+    } else {
+        constexpr int ctrl = BIT == 3 ? kMirror : BIT == 2 ? kHalfMirror : BIT == 1 ? kXor2 : kXor1;
+        const bool high = lane >> BIT & 1;
+        return (high ? b : a) + dpp<ctrl>(high ? a : b);
+    }
+}
+
+// Over the wave, in all lanes.
+__device__ __forceinline__ float wave_max(float x) {
+    x = fmaxf(x, dpp<kXor1>(x));
+    x = fmaxf(x, dpp<kXor2>(x));
+    x = fmaxf(x, dpp<kHalfMirror>(x));
+    x = fmaxf(x, dpp<kMirror>(x));
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+    x += dpp<kXor1>(x);
+    x += dpp<kXor2>(x);
+    x += dpp<kHalfMirror>(x);
+    x += dpp<kMirror>(x);
+    x = merge<4>(x, x, 0);
+    return merge<5>(x, x, 0);
+}
+
+constexpr int log2_of(int x) { return x <= 1 ? 0 : 1 + log2_of(x / 2); }
+
+// What a wave keeps in LDS of its 64 keys.
+template <int R> struct Area {
+    int64_t from[kGroup];             // offsets in the cache, -1: none
+    uint32_t pr[kGroup * R];          // probabilities, as b'
+};
+
+// A unit's rows: which keys they see, where their queries are.
+template <int R> struct Rows {
+    int lo[R], hi[R];
+    __device__ __forceinline__ Rows(const AttentionParams &p, const Unit &unit) {
+        const int lane = threadIdx.x & 63;
+        const bool live = lane < unit.rows;
+        const int low = live ? unit.row_lo(p, lane) : 0, high = live ? unit.row_hi(p, lane) : 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            lo[r] = __builtin_amdgcn_readlane(low, r);
+            hi[r] = __builtin_amdgcn_readlane(high, r);
+        }
+    }
+};
+
+// Orders a wave's LDS writes before its other lanes' reads.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// The b' of the rows' queries, E of them from element `at` on.
+template <int E, int R>
+__device__ __forceinline__ void load_queries(const AttentionParams &p, const Unit &unit, int at, uint32_t (&q)[R][E]) {
+    const int lane = threadIdx.x & 63;
+    const int64_t mine = lane < unit.rows ? unit.q_at(p, lane) : 0;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int64_t row = r < unit.rows ? unit.q_at(p, r) : 0;
+        const int64_t from = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), r) << 32) |
+                                       (uint32_t)__builtin_amdgcn_readlane((int)mine, r)) + at;
+        u32x4 w[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+        if (r < unit.rows && at < p.d) {
+            if (p.q_bf16) {
+                typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+                if constexpr (E == 8) {
+                    w[0] = load16<uint16_t>(p.q, from);
+                } else {
+                    const u32x2 h = *reinterpret_cast<const u32x2 *>(static_cast<const uint16_t *>(p.q) + from);
+                    w[0].x = h.x;
+                    w[0].y = h.y;
+                }
+            } else {
 #pragma unroll
-        for (int i = 0; i < E; ++i)
-            q[r][i] = biased(holds && r < unit.rows ? load_bits(p.q, row + at + i, p.q_bf16) : 0u);
-    }
-    for (int first = begin + wave * U * K; first < end; first += waves * U * K) {
-        u32x4 w[U];
-        int64_t from[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int key = first + u * K + lane / L;
-            from[u] = key < end ? unit.key_at(p, p.k, key) : -1;
-            w[u] = u32x4{0, 0, 0, 0};
-            if (from[u] >= 0 && holds)
-                w[u] = load16<T>(p.k.data, from[u] + at);
+                for (int h = 0; h < E / 4; ++h)
+                    w[h] = load16<float>(p.q, from + 4 * h);
+            }
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int i = 0; i < E; ++i)
+            q[r][i] = biased(p.q_bf16 ? element<uint16_t>(w[0], i) : w[i / 4][i % 4]);
+    }
+}
+
+// The scores, in units of log2, of keys first .. first + 63 (those below end):
+// lane i's are key first + own_key(i)'s, -inf where a row does not see it.
+template <int L> __device__ __forceinline__ int own_key(int lane) {
+    const int u = L == 1 ? 0 : (int)(__brev((uint32_t)(lane % L)) >> (32 - log2_of(L)));
+    return u * (64 / L) + lane / L;
+}
+
+template <typename T, int L, int R>
+__device__ __forceinline__ void score_group(const AttentionParams &p, const Unit &unit, const Rows<R> &rows, int first,
+                                            int end, const uint32_t (&q)[R][kPer<T>], Area<R> &area, float (&t)[R]) {
+    constexpr int E = kPer<T>;
+    constexpr int K = 64 / L;
+    constexpr int B = L < 16 ? L : 16;   // loads in flight
+    constexpr int S = log2_of(L);
+    const int lane = threadIdx.x & 63;
+    const int at = (lane % L) * E;
+    const bool holds = at < p.d;
+    wave_sync();
+    area.from[lane] = first + lane < end ? unit.key_at(p, p.k, first + lane) : -1;
+    wave_sync();
+    float v[S + 1][R];
+#pragma unroll
+    for (int u0 = 0; u0 < L; u0 += B) {
+        u32x4 w[B];
+#pragma unroll
+        for (int u = 0; u < B; ++u) {
+            const int64_t from = area.from[(u0 + u) * K + lane / L];
+            w[u] = u32x4{0, 0, 0, 0};
+            if (from >= 0 && holds)
+                w[u] = load16<T>(p.k.data, from + at);
+        }
+#pragma unroll
+        for (int u = 0; u < B; ++u) {
             float sum[R];
 #pragma unroll
             for (int r = 0; r < R; ++r)
@@ -74,134 +179,204 @@ __device__ __forceinline__ void score_keys(const AttentionParams &p, const Unit 
 #pragma unroll
             for (int i = 0; i < E; ++i) {
                 const uint32_t a = element<T>(w[u], i);
-                const float a1 = one_mantissa(a), m = power(a);
+                const float one = one_mantissa(a), m = power(a);
 #pragma unroll
                 for (int r = 0; r < R; ++r)
-                    sum[r] = pam_fma(a1, m, q[r][i], sum[r]);
+                    sum[r] = pam_fma(one, m, q[r][i], sum[r]);
             }
+            // Merge with the equal-sized sums before it: bit j of the load's
+            // number goes with bit S - 1 - j of the lane's.
+            const int n = u0 + u;
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int x = 1; x < L; x *= 2)
-                    sum[r] += __shfl_xor(sum[r], x);
-            const int key = first + u * K + lane / L;
-            if (lane % L == 0 && key < end) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    float t = kNegInf;
-                    if (r < unit.rows && from[u] >= 0 && key >= lo[r] && key < hi[r]) {
-                        if (!finite(sum[r])) {
-                            sum[r] = 0.0f;
-                            const int64_t row = unit.q_at(p, r);
-                            for (int i = 0; i < p.d; ++i)
-                                sum[r] += __uint_as_float(pam_full(load_bits(p.q, row + i, p.q_bf16),
-                                                                   load_bits(p.k.data, from[u] + i, sizeof(T) == 2)));
+            for (int r = 0; r < R; ++r) {
+                float x = sum[r];
+                if constexpr (S > 0) if ((n & 1) == 1) {
+                    x = merge<S - 1>(v[0][r], x, lane);
+                    if constexpr (S > 1) if ((n & 3) == 3) {
+                        x = merge<(S > 1 ? S - 2 : 0)>(v[1][r], x, lane);
+                        if constexpr (S > 2) if ((n & 7) == 7) {
+                            x = merge<(S > 2 ? S - 3 : 0)>(v[2][r], x, lane);
+                            if constexpr (S > 3) if ((n & 15) == 15) {
+                                x = merge<(S > 3 ? S - 4 : 0)>(v[3][r], x, lane);
+                                if constexpr (S > 4) if ((n & 31) == 31) {
+                                    x = merge<(S > 4 ? S - 5 : 0)>(v[4][r], x, lane);
+                                    if constexpr (S > 5) if ((n & 63) == 63)
+                                        x = merge<0>(v[5][r], x, lane);
+                                }
+                            }
                         }
-                        t = sum[r] * p.scale;
                     }
-                    s[(key - begin) * R + r] = t;
                 }
+                int level = 0;
+#pragma unroll
+                for (int j = 0; j < S; ++j)
+                    level += (n & ((2 << j) - 1)) == (2 << j) - 1;
+                v[level][r] = x;
             }
+        }
+    }
+    const int own = own_key<L>(lane), key = first + own;
+    const int64_t from = area.from[own];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float sum = v[S][r];
+        const bool sees = from >= 0 && key >= rows.lo[r] && key < rows.hi[r];
+        if (sees && !finite(sum)) {
+            sum = 0.0f;
+            const int64_t row = unit.q_at(p, r);
+            for (int i = 0; i < p.d; ++i)
+                sum += real(pam_full(load_bits(p.q, row + i, p.q_bf16), load_bits(p.k.data, from + i, sizeof(T) == 2)));
+        }
+        t[r] = sees ? sum * p.scale : kNegInf;
+    }
+}
+
+template <int R> __device__ __forceinline__ void put(float *to, const float (&t)[R]) {
+    constexpr int W = R == 4 || R == 8 ? 4 : R % 2 == 0 ? 2 : 1;
+    if constexpr (W == 1) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            to[r] = t[r];
+    } else {
+        typedef float vec __attribute__((ext_vector_type(W), aligned(4)));
+#pragma unroll
+        for (int r = 0; r < R; r += W) {
+            vec v;
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+                v[i] = t[r + i];
+            *reinterpret_cast<vec *>(to + r) = v;
         }
     }
 }
 
-// Maximum of the rows' scores s[0 .. keys * R) over the workgroup.
-template <int R> __device__ __forceinline__ void row_max(const float *s, int keys, float (&m)[R], float *scratch) {
+template <int R> __device__ __forceinline__ void get(const float *from, float (&t)[R]) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
-        m[r] = kNegInf;
-    for (int j = threadIdx.x; j < keys; j += blockDim.x)
+        t[r] = from[r];
+}
+
+// A running maximum and sum of 2^(t - maximum).
+template <int R> struct Running {
+    float m[R], l[R];
+    __device__ __forceinline__ Running() {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            m[r] = kNegInf;
+            l[r] = 0.0f;
+        }
+    }
+    // Takes in `sum` with maximum `top`, row r; a NaN sum stays one.
+    __device__ __forceinline__ void take(int r, float top, float sum) {
+        const float to = fmaxf(m[r], top);
+        l[r] = l[r] * exp2_from(m[r], to) + sum * exp2_from(top, to);
+        m[r] = to;
+    }
+    __device__ __forceinline__ void score(const float (&t)[R]) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            m[r] = fmaxf(m[r], s[j * R + r]);
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        for (int x = 1; x < 64; x *= 2)
-            m[r] = fmaxf(m[r], __shfl_xor(m[r], x));
-        if ((threadIdx.x & 63) == 0)
-            scratch[(threadIdx.x >> 6) * R + r] = m[r];
+            take(r, t[r], 1.0f);
     }
-    __syncthreads();
+    __device__ __forceinline__ void over_wave() {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-        for (int w = 0; w < (int)(blockDim.x >> 6); ++w)
-            m[r] = fmaxf(m[r], scratch[w * R + r]);
-}
+        for (int r = 0; r < R; ++r) {
+            const float to = wave_max(m[r]);
+            l[r] = wave_sum(l[r] * exp2_from(m[r], to));
+            m[r] = to;
+        }
+    }
+    // Over the workgroup, in all lanes; scratch: two arrays of waves x R.
+    __device__ __forceinline__ void over_group(float (&top)[kMostWaves][R], float (&sum)[kMostWaves][R]) {
+        over_wave();
+        const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                top[wave][r] = m[r];
+                sum[wave][r] = l[r];
+            }
+        }
+        __syncthreads();
+        *this = Running();
+        for (int w = 0; w < waves; ++w)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                take(r, top[w][r], sum[w][r]);
+    }
+};
 
-template <int R> __device__ __forceinline__ void row_sum(float (&l)[R], float *scratch) {
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        for (int x = 1; x < 64; x *= 2)
-            l[r] += __shfl_xor(l[r], x);
-        if ((threadIdx.x & 63) == 0)
-            scratch[(threadIdx.x >> 6) * R + r] = l[r];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        l[r] = 0.0f;
-        for (int w = 0; w < (int)(blockDim.x >> 6); ++w)
-            l[r] += scratch[w * R + r];
-    }
-}
-
-// out[row][i] = sum over keys begin <= j < end of P .^ v, the probabilities'
-// b' in pr[(j - begin) * R + row]; to out's rows (partial == nullptr) or
-// partial[row * d + i].  scratch: waves * R * L * 16 / sizeof(T) floats.
+// out[row][i] = sum over keys begin <= j < end of P .^ v, the scores at
+// scores[(j - origin) * R + row]; to out's rows (partial == nullptr) or
+// partial[row * d + i].
 template <typename T, int L, int R>
 __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit &unit, int begin, int end,
-                                           const uint32_t *pr, float *scratch, const int *lo, const int *hi,
-                                           const float *sums, float *partial) {
+                                           const float *scores, const Running<R> &row, Area<R> *areas, float *scratch,
+                                           float *partial) {
     constexpr int E = kPer<T>;
     constexpr int K = 64 / L;
-    constexpr int U = 4;
+    constexpr int B = L < 16 ? L : 16;
     constexpr int D = L * E;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int at = (lane % L) * E;
     const bool holds = at < p.d;
-    float acc[R][E];
+    Area<R> &area = areas[wave];
+    float inverse[R], acc[R][E];
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) {
+        inverse[r] = row.l[r] > 0.0f ? 1.0f / row.l[r] : 0.0f;
 #pragma unroll
         for (int i = 0; i < E; ++i)
             acc[r][i] = 0.0f;
-    for (int first = begin + wave * U * K; first < end; first += waves * U * K) {
-        u32x4 w[U];
+    }
+    for (int first = begin + wave * kGroup; first < end; first += waves * kGroup) {
+        wave_sync();
+        const int mine = first + lane;
+        area.from[lane] = mine < end ? unit.key_at(p, p.v, mine) : -1;
+        float t[R];
+        get<R>(scores + (int64_t)(min(mine, end - 1) - begin) * R, t);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int key = first + u * K + lane / L;
-            const int64_t from = key < end ? unit.key_at(p, p.v, key) : -1;
-            w[u] = u32x4{0, 0, 0, 0};
-            if (from >= 0 && holds)
-                w[u] = load16<T>(p.v.data, from + at);
-        }
+        for (int r = 0; r < R; ++r)
+            t[r] = real(probability(mine < end ? exp2_from(t[r], row.m[r]) : 0.0f, inverse[r]));
+        put<R>(reinterpret_cast<float *>(area.pr) + lane * R, t);
+        wave_sync();
+#pragma unroll 1
+        for (int u0 = 0; u0 < L; u0 += B) {
+            u32x4 w[B];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int key = min(first + u * K + lane / L, end - 1);
-            uint32_t b[R];
+            for (int u = 0; u < B; ++u) {
+                const int64_t from = area.from[(u0 + u) * K + lane / L];
+                w[u] = u32x4{0, 0, 0, 0};
+                if (from >= 0 && holds)
+                    w[u] = load16<T>(p.v.data, from + at);
+            }
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-                b[r] = pr[(key - begin) * R + r];
+            for (int u = 0; u < B; ++u) {
+                float b[R];
+                get<R>(reinterpret_cast<const float *>(area.pr) + ((u0 + u) * K + lane / L) * R, b);
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const uint32_t a = element<T>(w[u], i);
-                const float a1 = one_mantissa(a), m = power(a);
+                for (int i = 0; i < E; ++i) {
+                    const uint32_t a = element<T>(w[u], i);
+                    const float one = one_mantissa(a), m = power(a);
 #pragma unroll
-                for (int r = 0; r < R; ++r)
-                    acc[r][i] = pam_fma(a1, m, b[r], acc[r][i]);
+                    for (int r = 0; r < R; ++r)
+                        acc[r][i] = pam_fma(one, m, bits(b[r]), acc[r][i]);
+                }
             }
         }
     }
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int i = 0; i < E; ++i)
-#pragma unroll
-            for (int x = L; x < 64; x *= 2)
-                acc[r][i] += __shfl_xor(acc[r][i], x);
+        for (int i = 0; i < E; ++i) {
+            if constexpr (L <= 4)
+                acc[r][i] += __shfl_xor(acc[r][i], 4);
+            if constexpr (L <= 8)
+                acc[r][i] += dpp<kRotate8>(acc[r][i]);
+            if constexpr (L <= 16)
+                acc[r][i] = merge<4>(acc[r][i], acc[r][i], lane);
+            if constexpr (L <= 32)
+                acc[r][i] = merge<5>(acc[r][i], acc[r][i], lane);
+        }
     if (lane < L) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -214,21 +389,28 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
         const int r = e / D, i = e % D;
         if (r >= unit.rows || i >= p.d)
             continue;
+        float m = 0.0f, l = 0.0f;
+#pragma unroll
+        for (int x = 0; x < R; ++x)
+            if (x == r) {
+                m = row.m[x];
+                l = row.l[x];
+            }
         float sum = 0.0f;
         for (int w = 0; w < waves; ++w)
             sum += scratch[w * R * D + e];
-        if (!finite(sum)) {
+        if (!(l > 0.0f)) {                 // no weight, or a NaN score
+            sum = l;
+        } else if (!finite(sum)) {
             // Term by term, over the keys the row sees.
             sum = 0.0f;
-            for (int key = max(begin, lo[r]); key < min(end, hi[r]); ++key) {
+            for (int key = max(begin, unit.row_lo(p, r)); key < min(end, unit.row_hi(p, r)); ++key) {
                 const int64_t from = unit.key_at(p, p.v, key);
                 if (from >= 0)
-                    sum += __uint_as_float(pam_full(pr[(key - begin) * R + r] + kBias,
-                                                    load_bits(p.v.data, from + i, sizeof(T) == 2)));
+                    sum += real(pam_full(probability(exp2_from(scores[(int64_t)(key - begin) * R + r], m), 1.0f / l) + kBias,
+                                         load_bits(p.v.data, from + i, sizeof(T) == 2)));
             }
         }
-        if (!(sums[r] > 0.0f))      // no weight, or a NaN score
-            sum = sums[r];
         if (partial != nullptr)
             partial[r * p.d + i] = sum;
         else
@@ -236,94 +418,65 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
     }
 }
 
-template <int R>
-__device__ __forceinline__ void row_ranges(const AttentionParams &p, const Unit &unit, int *lo, int *hi) {
-    if (threadIdx.x < R) {
-        const int r = threadIdx.x;
-        lo[r] = r < unit.rows ? unit.row_lo(p, r) : 0;
-        hi[r] = r < unit.rows ? unit.row_hi(p, r) : 0;
-    }
-    __syncthreads();
-}
-
 // A unit in one workgroup: its scores stay in LDS.
 template <typename T, int L, int R>
-__global__ void __launch_bounds__(kThreads) attention_whole_kernel(const AttentionParams p) {
+__global__ void __launch_bounds__(kMostWaves * 64) attention_whole_kernel(const AttentionParams p) {
     extern __shared__ float s[];
-    __shared__ float scratch[kWaves * R * L * kPer<T>];
-    __shared__ int lo[R], hi[R];
-    __shared__ float sums[R];
+    __shared__ Area<R> areas[kMostWaves];
+    __shared__ float top[kMostWaves][R], sum[kMostWaves][R];
     const Unit unit(p, blockIdx.x);
     if (unit.rows == 0)
         return;
-    row_ranges<R>(p, unit, lo, hi);
-    score_keys<T, L, R>(p, unit, unit.lo, unit.hi, s, lo, hi);
-    __syncthreads();
-    const int keys = max(unit.hi - unit.lo, 0);
-    float m[R], l[R];
-    row_max<R>(s, keys, m, scratch);
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-        l[r] = 0.0f;
-    for (int j = threadIdx.x; j < keys; j += blockDim.x)
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const float e = exp2_from(s[j * R + r], m[r]);
-            l[r] += e;
-            s[j * R + r] = e;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    float *scratch = s + (int64_t)p.max_kv * R;
+    Running<R> row;
+    {
+        const Rows<R> rows(p, unit);
+        uint32_t q[R][kPer<T>];
+        load_queries<kPer<T>, R>(p, unit, (lane % L) * kPer<T>, q);
+        for (int first = unit.lo + wave * kGroup; first < unit.hi; first += waves * kGroup) {
+            float t[R];
+            score_group<T, L, R>(p, unit, rows, first, unit.hi, q, areas[wave], t);
+            row.score(t);
+            const int key = first + own_key<L>(lane);
+            if (key < unit.hi)
+                put<R>(s + (key - unit.lo) * R, t);
         }
-    row_sum<R>(l, scratch);
-    float inverse[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        inverse[r] = l[r] > 0.0f ? 1.0f / l[r] : 0.0f;
-        if (threadIdx.x == 0)
-            sums[r] = l[r];
     }
-    for (int j = threadIdx.x; j < keys; j += blockDim.x)
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            s[j * R + r] = __uint_as_float(probability(s[j * R + r], inverse[r]));
-    __syncthreads();
-    value_keys<T, L, R>(p, unit, unit.lo, unit.hi, reinterpret_cast<const uint32_t *>(s), scratch, lo, hi, sums,
-                        nullptr);
+    row.over_group(top, sum);
+    value_keys<T, L, R>(p, unit, unit.lo, unit.hi, s, row, areas, scratch, nullptr);
 }
 
 // Long contexts, first launch: scores of one split of a unit's keys, with the
 // split's maximum and sum for each row.
 template <typename T, int L, int R>
 __global__ void __launch_bounds__(kThreads) attention_scores_kernel(const AttentionParams p) {
-    extern __shared__ float s[];
-    __shared__ float scratch[kWaves * R];
-    __shared__ int lo[R], hi[R];
+    __shared__ Area<R> areas[kThreads / 64];
+    __shared__ float top[kMostWaves][R], sum[kMostWaves][R];
     const int split = blockIdx.x % p.splits, index = blockIdx.x / p.splits;
     const Unit unit(p, index);
     const int begin = max(unit.lo, split * p.split_keys), end = min(unit.hi, (split + 1) * p.split_keys);
     if (unit.rows == 0 || begin >= end)
         return;
-    row_ranges<R>(p, unit, lo, hi);
-    score_keys<T, L, R>(p, unit, begin, end, s, lo, hi);
-    __syncthreads();
-    float m[R], l[R];
-    row_max<R>(s, end - begin, m, scratch);
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-        l[r] = 0.0f;
-    float *to = p.scores + ((int64_t)index * p.splits * p.split_keys + begin) * R;
-    for (int j = threadIdx.x; j < end - begin; j += blockDim.x)
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            l[r] += exp2_from(s[j * R + r], m[r]);
-            to[(int64_t)j * R + r] = s[j * R + r];
-        }
-    row_sum<R>(l, scratch);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Running<R> row;
+    const Rows<R> rows(p, unit);
+    uint32_t q[R][kPer<T>];
+    load_queries<kPer<T>, R>(p, unit, (lane % L) * kPer<T>, q);
+    float *scores = p.scores + (int64_t)index * p.splits * p.split_keys * R;
+    for (int first = begin + wave * kGroup; first < end; first += kThreads) {
+        float t[R];
+        score_group<T, L, R>(p, unit, rows, first, end, q, areas[wave], t);
+        row.score(t);
+        const int key = first + own_key<L>(lane);
+        if (key < end)
+            put<R>(scores + (int64_t)key * R, t);
+    }
+    row.over_group(top, sum);
     if (threadIdx.x == 0) {
         float *stats = p.stats + ((int64_t)index * p.splits + split) * 2 * R;
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            stats[r] = m[r];
-            stats[R + r] = l[r];
-        }
+        put<R>(stats, row.m);
+        put<R>(stats + R, row.l);
     }
 }
 
@@ -331,78 +484,61 @@ __global__ void __launch_bounds__(kThreads) attention_scores_kernel(const Attent
 // split's part of P V.
 template <typename T, int L, int R>
 __global__ void __launch_bounds__(kThreads) attention_values_kernel(const AttentionParams p) {
-    extern __shared__ float s[];
-    __shared__ float scratch[kWaves * R * L * kPer<T>];
-    __shared__ int lo[R], hi[R];
-    __shared__ float sums[R];
+    __shared__ Area<R> areas[kThreads / 64];
+    __shared__ float scratch[kThreads / 64 * R * L * kPer<T>];
     const int split = blockIdx.x % p.splits, index = blockIdx.x / p.splits;
     const Unit unit(p, index);
     const int begin = max(unit.lo, split * p.split_keys), end = min(unit.hi, (split + 1) * p.split_keys);
     if (unit.rows == 0 || begin >= end)
         return;
-    row_ranges<R>(p, unit, lo, hi);
     const int first = unit.lo / p.split_keys, last = (unit.hi - 1) / p.split_keys;
     const float *stats = p.stats + (int64_t)index * p.splits * 2 * R;
-    float m[R], l[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-        m[r] = kNegInf;
-    for (int j = first + threadIdx.x; j <= last; j += blockDim.x)
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            m[r] = fmaxf(m[r], stats[j * 2 * R + r]);
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        for (int x = 1; x < 64; x *= 2)
-            m[r] = fmaxf(m[r], __shfl_xor(m[r], x));
-        if ((threadIdx.x & 63) == 0)
-            scratch[(threadIdx.x >> 6) * R + r] = m[r];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        for (int w = 0; w < kWaves; ++w)
-            m[r] = fmaxf(m[r], scratch[w * R + r]);
-        l[r] = 0.0f;
-    }
-    for (int j = first + threadIdx.x; j <= last; j += blockDim.x)
+    Running<R> row;
+    for (int j = first + (threadIdx.x & 63); j <= last; j += 64) {
+        float m[R], l[R];
+        get<R>(stats + j * 2 * R, m);
+        get<R>(stats + j * 2 * R + R, l);
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            l[r] += stats[j * 2 * R + R + r] * exp2_from(stats[j * 2 * R + r], m[r]);
-    row_sum<R>(l, scratch);
-    float inverse[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        inverse[r] = l[r] > 0.0f ? 1.0f / l[r] : 0.0f;
-        if (threadIdx.x == 0)
-            sums[r] = l[r];
+            row.take(r, m[r], l[r]);
     }
-    const float *from = p.scores + ((int64_t)index * p.splits * p.split_keys + begin) * R;
-    for (int j = threadIdx.x; j < end - begin; j += blockDim.x)
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            s[j * R + r] = __uint_as_float(probability(exp2_from(from[(int64_t)j * R + r], m[r]), inverse[r]));
-    __syncthreads();
-    value_keys<T, L, R>(p, unit, begin, end, reinterpret_cast<const uint32_t *>(s), scratch, lo, hi, sums,
-                        p.partial + ((int64_t)index * p.splits + split) * R * p.d);
+    row.over_wave();
+    value_keys<T, L, R>(p, unit, begin, end, p.scores + ((int64_t)index * p.splits * p.split_keys + begin) * R, row,
+                        areas, scratch, p.partial + ((int64_t)index * p.splits + split) * R * p.d);
 }
 
-// Third launch: the outputs, each the sum over its unit's splits in order; four
-// a thread.
+// Third launch: the outputs, each the sum over its unit's splits; four a thread.
+// GROUPS threads share an output's splits, each in order, then their sums in
+// order.
+template <int GROUPS>
 __global__ void __launch_bounds__(kThreads) attention_join_kernel(const AttentionParams p, int parts) {
+    constexpr int items = kThreads / GROUPS;
+    __shared__ f32x4 sums[GROUPS][items];
     const int index = blockIdx.x / parts;
     const Unit unit(p, p.first_unit + index);
-    const int e = ((blockIdx.x % parts) * kThreads + threadIdx.x) * 4;
-    if (e >= unit.rows * p.d)
-        return;
+    const int item = threadIdx.x % items, group = threadIdx.x / items;
+    const int e = ((blockIdx.x % parts) * items + item) * 4;
+    const bool live = e < unit.rows * p.d;
     const int first = unit.lo / p.split_keys, last = unit.hi > unit.lo ? (unit.hi - 1) / p.split_keys : first - 1;
-    const float *partial = p.partial + (int64_t)index * p.splits * p.rows * p.d + e;
+    const int64_t step = (int64_t)p.rows * p.d;
+    const float *partial = p.partial + (int64_t)index * p.splits * step + e;
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int j = first; j <= last; ++j)
-        sum += *reinterpret_cast<const f32x4 *>(partial + (int64_t)j * p.rows * p.d);
-    const int r = e / p.d;
-    *reinterpret_cast<f32x4 *>(p.out + unit.out_at(p, r) + (e - r * p.d)) = sum;
+    if (live)
+#pragma unroll 4
+        for (int j = first + group; j <= last; j += GROUPS)
+            sum += *reinterpret_cast<const f32x4 *>(partial + j * step);
+    if constexpr (GROUPS > 1) {
+        sums[group][item] = sum;
+        __syncthreads();
+        if (group > 0)
+            return;
+        for (int g = 1; g < GROUPS; ++g)
+            sum += sums[g][item];
+    }
+    if (live) {
+        const int r = e / p.d;
+        *reinterpret_cast<f32x4 *>(p.out + unit.out_at(p, r) + (e - r * p.d)) = sum;
+    }
 }
 
 enum Which { kWhole, kScores, kValues };
@@ -413,17 +549,20 @@ hipError_t launch(Which which, const AttentionParams &p, hipStream_t stream) {
     const void *kernel = which == kWhole    ? (const void *)attention_whole_kernel<T, L, R>
                          : which == kScores ? (const void *)attention_scores_kernel<T, L, R>
                                             : (const void *)attention_values_kernel<T, L, R>;
-    const size_t lds = (size_t)(which == kWhole ? p.max_kv : p.split_keys) * R * sizeof(float);
+    const int threads = which == kWhole ? whole_waves(p.max_kv) * 64 : kThreads;
+    const size_t lds = which == kWhole ? ((size_t)p.max_kv + threads / 64 * L * kPer<T>) * R * sizeof(float) : 0;
     const unsigned grid = which == kWhole ? units : units * (unsigned)p.splits;
     void *args[] = {const_cast<AttentionParams *>(&p)};
-    return hipLaunchKernel(kernel, dim3(grid), dim3(kThreads), args, lds, stream);
+    return hipLaunchKernel(kernel, dim3(grid), dim3((unsigned)threads), args, lds, stream);
 }
 
 template <typename T, int L> hipError_t for_rows(Which which, const AttentionParams &p, hipStream_t stream) {
     switch (p.rows) {
     case 1: return launch<T, L, 1>(which, p, stream);
     case 2: return launch<T, L, 2>(which, p, stream);
+    case 3: return launch<T, L, 3>(which, p, stream);
     case 4: return launch<T, L, 4>(which, p, stream);
+    case 6: return launch<T, L, 6>(which, p, stream);
     default: return launch<T, L, 8>(which, p, stream);
     }
 }
@@ -453,8 +592,14 @@ hipError_t launch_attention_values(bool bf16, int lanes, const AttentionParams &
 }
 
 hipError_t launch_attention_join(const AttentionParams &p, int units, hipStream_t stream) {
-    const int parts = (p.rows * p.d / 4 + kThreads - 1) / kThreads;
-    hipLaunchKernelGGL(attention_join_kernel, dim3((unsigned)(units * parts)), dim3(kThreads), 0, stream, p, parts);
+    // Many splits of few outputs: 16 threads an output.
+    const bool shared = p.splits > 8 && (int64_t)units * p.rows * p.d <= 1 << 17;
+    const int items = shared ? kThreads / 16 : kThreads;
+    const int parts = (p.rows * p.d / 4 + items - 1) / items;
+    if (shared)
+        hipLaunchKernelGGL(attention_join_kernel<16>, dim3((unsigned)(units * parts)), dim3(kThreads), 0, stream, p, parts);
+    else
+        hipLaunchKernelGGL(attention_join_kernel<1>, dim3((unsigned)(units * parts)), dim3(kThreads), 0, stream, p, parts);
     return hipGetLastError();
 }
 

@@ -169,8 +169,7 @@ struct AttentionPlan {
     size_t bytes() const { return scores + stats + partial; }
 };
 
-constexpr int64_t kWholeScores = 16384;   // scores of a unit kept in LDS at most (64 KiB)
-constexpr int64_t kTileRows = 24;         // fewest rows of a key head that run as tiles
+constexpr int64_t kTileRows = 33;         // fewest rows of a key head that run as tiles
 constexpr int64_t kSlabBytes = (int64_t)512 << 20;   // scores of one round of launches, about
 
 AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool bf16, int32_t batch, int32_t max_q,
@@ -181,15 +180,20 @@ AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool 
     while (a.lanes * per < d)
         a.lanes *= 2;
     const int64_t rows = (int64_t)max_q * (q_heads / kv_heads);
-    if (rows >= kTileRows)
-        a.rows = rows <= 64 ? 64 : 128;
-    else
-        a.rows = rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
+    if (rows >= kTileRows) {
+        // 128 rows a unit where that leaves two rounds of score tiles, four
+        // workgroups a compute unit; else 64, which waste less.
+        const int64_t tiles = (int64_t)batch * kv_heads * ceil_div(rows, 128) * ceil_div(max_kv, 128);
+        a.rows = rows > 64 && tiles >= 2048 ? 128 : 64;
+    } else {
+        const int64_t blocks = ceil_div(std::max<int64_t>(rows, 1), 8), each = ceil_div(std::max<int64_t>(rows, 1), blocks);
+        a.rows = (int)(each <= 4 ? each : each <= 6 ? 6 : 8);
+    }
     a.row_blocks = (int)ceil_div(std::max<int64_t>(rows, 1), a.rows);
     a.units = a.slab = (int64_t)batch * kv_heads * a.row_blocks;
     a.splits = 1;
     a.form = rows >= kTileRows ? Form::tiles
-             : (int64_t)max_kv * a.rows <= kWholeScores && (a.units >= 256 || max_kv <= 512) ? Form::whole
+             : pamk::whole_lds(max_kv, a.rows, a.lanes, bf16) <= pamk::kWholeLds && (a.units >= 256 || max_kv <= 256) ? Form::whole
                                                                                             : Form::split;
     if (a.form == Form::whole || a.units == 0)
         return a;
@@ -203,9 +207,9 @@ AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool 
         const int64_t per = ceil_div(keys * a.slab * columns * waves, 4096);
         a.split_keys = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(per, 128) * 128, 128), 512);
     } else {
-        // About 2048 workgroups, of 256 to 1024 keys.
-        const int64_t keys = ceil_div((int64_t)max_kv * a.units, 2048);
-        a.split_keys = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(keys, 64) * 64, 256), 1024);
+        // About 1024 workgroups, of 256 to 1024 keys.
+        const int64_t keys = ceil_div((int64_t)max_kv * a.units, 1024);
+        a.split_keys = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(keys, 256) * 256, 256), 1024);
     }
     a.splits = (int)ceil_div(std::max(max_kv, 1), a.split_keys);
     const int64_t parts = a.slab * a.splits;

@@ -26,7 +26,6 @@ namespace {
 
 constexpr int kStep = 16;             // k steps of a chunk
 constexpr int kPad = 4;               // words after each k step's row in LDS
-constexpr int kMaxSplit = 512;        // keys of a split at most
 
 // A lane's 8 rows or columns of a 64-wide block: two groups of four.
 __device__ __forceinline__ int place(int group, int i) { return (i / 4) * 32 + group * 4 + i % 4; }
@@ -129,12 +128,14 @@ __device__ __forceinline__ float eight_sum(float x) {
     return x + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x141, 0xF, 0xF, false));
 }
 
-// The chunks' staging: two buffers in turn, and for each chunk a word that says
-// whether an element of it keeps it from the plain form; four of those words,
-// so that one is cleared two chunks before it is written.
-template <int BM, int BN> struct Buffers {
-    uint32_t a[2][kStep * (BN + kPad)];
-    uint32_t b[2][kStep * (BM + kPad)];
+// The chunks' staging: two buffers in turn, or one with a second barrier a chunk;
+// and for each chunk a word that says whether an element of it keeps it from the
+// plain form, four of them, so that one is cleared two chunks before it is
+// written.
+template <int BM, int BN, int COUNT> struct Buffers {
+    static constexpr int kCount = COUNT;
+    uint32_t a[kCount][kStep * (BN + kPad)];
+    uint32_t b[kCount][kStep * (BM + kPad)];
     uint32_t odd[4];
 };
 
@@ -197,12 +198,14 @@ struct Eight {
 };
 
 template <typename T, int WM, int WN, bool QB>
-__global__ void __launch_bounds__(64 * WM * WN, 16 / (WM * WN)) tile_scores_kernel(const AttentionParams p) {
+__global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(4, 4))) tile_scores_kernel(const AttentionParams p) {
     constexpr int BM = 64 * WM, BN = 64 * WN, NT = 64 * WM * WN;
     constexpr int KI = 2 / WM > 0 ? 2 / WM : 1;    // key items of 8 values a lane and chunk
     constexpr int QI = 2 / WN > 0 ? 2 / WN : 1;    // query items
     constexpr bool KB = sizeof(T) == 2;
-    __shared__ Buffers<BM, BN> buf;
+    // One buffer lets a compute unit hold 16 waves of the small workgroups (many
+    // 64-row tiles of 128 values a head: 447 -> 373 us with one).
+    __shared__ Buffers<BM, BN, WM == 2 ? 2 : 1> buf;
     __shared__ int lo[BM], hi[BM];
     __shared__ int valid[BN];
     __shared__ float across[2][WN][BM];
@@ -267,7 +270,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 16 / (WM * WN)) tile_scores_kern
         }
     };
     auto stage = [&](int chunk) {
-        uint32_t *a = buf.a[chunk & 1], *b = buf.b[chunk & 1];
+        uint32_t *a = buf.a[chunk % buf.kCount], *b = buf.b[chunk % buf.kCount];
         Odd odd;
 #pragma unroll
         for (int i = 0; i < KI; ++i) {
@@ -307,9 +310,12 @@ __global__ void __launch_bounds__(64 * WM * WN, 16 / (WM * WN)) tile_scores_kern
         __syncthreads();
         if (tid == 0)
             buf.odd[(c + 2) & 3] = 0;
-        chunk_product<BM, BN, true>(buf.a[c & 1], buf.b[c & 1], row0, col0, buf.odd[c & 3] == 0, acc);
-        if (c + 1 < chunks)
+        chunk_product<BM, BN, true>(buf.a[c % buf.kCount], buf.b[c % buf.kCount], row0, col0, buf.odd[c & 3] == 0, acc);
+        if (c + 1 < chunks) {
+            if (buf.kCount == 1)
+                __syncthreads();
             stage(c + 1);
+        }
     }
 
     if (!all_finite(acc))
@@ -398,7 +404,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 16 / (WM * WN)) tile_scores_kern
 }
 
 template <typename T, int WM, int WN>
-__global__ void __launch_bounds__(64 * WM * WN, 16 / (WM * WN)) tile_values_kernel(const AttentionParams p) {
+__global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(4, 4))) tile_values_kernel(const AttentionParams p) {
     constexpr int BM = 64 * WM, BN = 64 * WN, NT = 64 * WM * WN;
     constexpr int E = kPer<T>;
     constexpr int SI = kStep * BM / 4 / NT;        // score items of 4 rows a lane and chunk
@@ -406,9 +412,9 @@ __global__ void __launch_bounds__(64 * WM * WN, 16 / (WM * WN)) tile_values_kern
     constexpr int SK = NT / (BM / 4);              // keys between a lane's score items
     constexpr int VK = NT / (BN / E);              // and between its value items
     constexpr bool VB = sizeof(T) == 2;
-    __shared__ Buffers<BM, BN> buf;
+    __shared__ Buffers<BM, BN, 2> buf;
     __shared__ float row_max[BM], row_sum[BM];
-    __shared__ int64_t from[kMaxSplit];            // the split's keys, -1: none
+    extern __shared__ int64_t from[];              // the split's keys, -1: none
 
     const int dtiles = (p.d + BN - 1) / BN;
     const int col_tile = blockIdx.x % dtiles;
@@ -475,7 +481,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 16 / (WM * WN)) tile_values_kern
     // Scores outside the split's keys are -inf, those of rows that do not exist
     // 0: probabilities 0 and 1.  A NaN row's probabilities are anything.
     auto stage = [&](int chunk) {
-        uint32_t *a = buf.a[chunk & 1], *b = buf.b[chunk & 1];
+        uint32_t *a = buf.a[chunk % buf.kCount], *b = buf.b[chunk % buf.kCount];
         Odd odd;
         float least = 1.0f;
 #pragma unroll
@@ -527,9 +533,12 @@ __global__ void __launch_bounds__(64 * WM * WN, 16 / (WM * WN)) tile_values_kern
         __syncthreads();
         if (tid == 0)
             buf.odd[(c + 2) & 3] = 0;
-        chunk_product<BM, BN, false>(buf.a[c & 1], buf.b[c & 1], row0, col0, buf.odd[c & 3] == 0, acc);
-        if (c + 1 < chunks)
+        chunk_product<BM, BN, false>(buf.a[c % buf.kCount], buf.b[c % buf.kCount], row0, col0, buf.odd[c & 3] == 0, acc);
+        if (c + 1 < chunks) {
+            if (buf.kCount == 1)
+                __syncthreads();
             stage(c + 1);
+        }
     }
 
     if (!all_finite(acc))
@@ -580,15 +589,16 @@ template <typename T, bool QB> hipError_t scores_launch(const AttentionParams &p
 
 template <typename T> hipError_t values_launch(const AttentionParams &p, int units, hipStream_t stream) {
     const int wide = p.d > 64;
+    const size_t keys = (size_t)p.split_keys * sizeof(int64_t);
     const unsigned grid = (unsigned)(units * p.splits * (wide ? (p.d + 127) / 128 : 1));
     if (p.rows == 128 && wide)
-        hipLaunchKernelGGL((tile_values_kernel<T, 2, 2>), dim3(grid), dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((tile_values_kernel<T, 2, 2>), dim3(grid), dim3(256), keys, stream, p);
     else if (p.rows == 128)
-        hipLaunchKernelGGL((tile_values_kernel<T, 2, 1>), dim3(grid), dim3(128), 0, stream, p);
+        hipLaunchKernelGGL((tile_values_kernel<T, 2, 1>), dim3(grid), dim3(128), keys, stream, p);
     else if (wide)
-        hipLaunchKernelGGL((tile_values_kernel<T, 1, 2>), dim3(grid), dim3(128), 0, stream, p);
+        hipLaunchKernelGGL((tile_values_kernel<T, 1, 2>), dim3(grid), dim3(128), keys, stream, p);
     else
-        hipLaunchKernelGGL((tile_values_kernel<T, 1, 1>), dim3(grid), dim3(64), 0, stream, p);
+        hipLaunchKernelGGL((tile_values_kernel<T, 1, 1>), dim3(grid), dim3(64), keys, stream, p);
     return hipGetLastError();
 }
 
