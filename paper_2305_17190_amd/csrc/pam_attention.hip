@@ -14,7 +14,9 @@
 // A wave takes 64 keys at a time.  Lane i looks up key i's page; then every
 // load of a wave fetches 64 / L whole keys, L neighbouring lanes 16 bytes each,
 // so that a cache line is used by the lanes of one load, and all L loads of the
-// 64 keys are on their way before the first is used.  Scores: a lane has the
+// 64 keys are on their way before the first is used.  Lanes past a head's end
+// and keys that are none read something that is there instead, and count for
+// nothing afterwards.  Scores: a lane has the
 // partial sums of its 16 bytes of each key; adding them up over the L lanes
 // halves the number of sums a lane holds with each step (one half goes to the
 // lane's partner, the other half comes), so that lane i ends with one key's
@@ -81,7 +83,7 @@ constexpr int log2_of(int x) { return x <= 1 ? 0 : 1 + log2_of(x / 2); }
 
 // What a wave keeps in LDS of its 64 keys.
 template <int R> struct Area {
-    int64_t from[kGroup];             // offsets in the cache, -1: none
+    int64_t from[kGroup];             // offsets in the cache (0 where there is none)
     uint32_t pr[kGroup * R];          // probabilities, as b'
 };
 
@@ -154,10 +156,11 @@ __device__ __forceinline__ void score_group(const AttentionParams &p, const Unit
     constexpr int B = L < 16 ? L : 16;   // loads in flight
     constexpr int S = log2_of(L);
     const int lane = threadIdx.x & 63;
-    const int at = (lane % L) * E;
-    const bool holds = at < p.d;
+    const int at = (lane % L) * E < p.d ? (lane % L) * E : 0;
     wave_sync();
-    area.from[lane] = first + lane < end ? unit.key_at(p, p.k, first + lane) : -1;
+    const int64_t place = first + lane < end ? unit.key_at(p, p.k, first + lane) : -1;
+    const uint64_t there = __ballot(place >= 0);
+    area.from[lane] = place >= 0 ? place : 0;
     wave_sync();
     float v[S + 1][R];
 #pragma unroll
@@ -165,10 +168,7 @@ __device__ __forceinline__ void score_group(const AttentionParams &p, const Unit
         u32x4 w[B];
 #pragma unroll
         for (int u = 0; u < B; ++u) {
-            const int64_t from = area.from[(u0 + u) * K + lane / L];
-            w[u] = u32x4{0, 0, 0, 0};
-            if (from >= 0 && holds)
-                w[u] = load16<T>(p.k.data, from + at);
+            w[u] = load16<T>(p.k.data, area.from[(u0 + u) * K + lane / L] + at);
         }
 #pragma unroll
         for (int u = 0; u < B; ++u) {
@@ -216,14 +216,14 @@ __device__ __forceinline__ void score_group(const AttentionParams &p, const Unit
         }
     }
     const int own = own_key<L>(lane), key = first + own;
-    const int64_t from = area.from[own];
+    const bool exists = there >> own & 1;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         float sum = v[S][r];
-        const bool sees = from >= 0 && key >= rows.lo[r] && key < rows.hi[r];
+        const bool sees = exists && key >= rows.lo[r] && key < rows.hi[r];
         if (sees && !finite(sum)) {
             sum = 0.0f;
-            const int64_t row = unit.q_at(p, r);
+            const int64_t row = unit.q_at(p, r), from = area.from[own];
             for (int i = 0; i < p.d; ++i)
                 sum += real(pam_full(load_bits(p.q, row + i, p.q_bf16), load_bits(p.k.data, from + i, sizeof(T) == 2)));
         }
@@ -317,8 +317,7 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
     constexpr int B = L < 16 ? L : 16;
     constexpr int D = L * E;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int at = (lane % L) * E;
-    const bool holds = at < p.d;
+    const int at = (lane % L) * E, reads = at < p.d ? at : 0;
     Area<R> &area = areas[wave];
     float inverse[R], acc[R][E];
 #pragma unroll
@@ -331,12 +330,13 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
     for (int first = begin + wave * kGroup; first < end; first += waves * kGroup) {
         wave_sync();
         const int mine = first + lane;
-        area.from[lane] = mine < end ? unit.key_at(p, p.v, mine) : -1;
+        const int64_t place = mine < end ? unit.key_at(p, p.v, mine) : -1;
+        area.from[lane] = place >= 0 ? place : 0;
         float t[R];
         get<R>(scores + (int64_t)(min(mine, end - 1) - begin) * R, t);
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            t[r] = real(probability(mine < end ? exp2_from(t[r], row.m[r]) : 0.0f, inverse[r]));
+            t[r] = real(probability(place >= 0 ? exp2_from(t[r], row.m[r]) : 0.0f, inverse[r]));
         put<R>(reinterpret_cast<float *>(area.pr) + lane * R, t);
         wave_sync();
 #pragma unroll 1
@@ -344,10 +344,7 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
             u32x4 w[B];
 #pragma unroll
             for (int u = 0; u < B; ++u) {
-                const int64_t from = area.from[(u0 + u) * K + lane / L];
-                w[u] = u32x4{0, 0, 0, 0};
-                if (from >= 0 && holds)
-                    w[u] = load16<T>(p.v.data, from + at);
+                w[u] = load16<T>(p.v.data, area.from[(u0 + u) * K + lane / L] + reads);
             }
 #pragma unroll
             for (int u = 0; u < B; ++u) {
@@ -447,13 +444,17 @@ __global__ void __launch_bounds__(kMostWaves * 64) attention_whole_kernel(const 
     value_keys<T, L, R>(p, unit, unit.lo, unit.hi, s, row, areas, scratch, nullptr);
 }
 
+// Consecutive workgroups, which go to the chip's eight dies in turn, take one
+// split of consecutive units: with the splits of a unit in a row, sequences of
+// different lengths left the dies of the last splits idle.
+//
 // Long contexts, first launch: scores of one split of a unit's keys, with the
 // split's maximum and sum for each row.
 template <typename T, int L, int R>
 __global__ void __launch_bounds__(kThreads) attention_scores_kernel(const AttentionParams p) {
     __shared__ Area<R> areas[kThreads / 64];
     __shared__ float top[kMostWaves][R], sum[kMostWaves][R];
-    const int split = blockIdx.x % p.splits, index = blockIdx.x / p.splits;
+    const int units = gridDim.x / p.splits, split = blockIdx.x / units, index = blockIdx.x - split * units;
     const Unit unit(p, index);
     const int begin = max(unit.lo, split * p.split_keys), end = min(unit.hi, (split + 1) * p.split_keys);
     if (unit.rows == 0 || begin >= end)
@@ -486,7 +487,7 @@ template <typename T, int L, int R>
 __global__ void __launch_bounds__(kThreads) attention_values_kernel(const AttentionParams p) {
     __shared__ Area<R> areas[kThreads / 64];
     __shared__ float scratch[kThreads / 64 * R * L * kPer<T>];
-    const int split = blockIdx.x % p.splits, index = blockIdx.x / p.splits;
+    const int units = gridDim.x / p.splits, split = blockIdx.x / units, index = blockIdx.x - split * units;
     const Unit unit(p, index);
     const int begin = max(unit.lo, split * p.split_keys), end = min(unit.hi, (split + 1) * p.split_keys);
     if (unit.rows == 0 || begin >= end)

@@ -81,6 +81,8 @@ struct Unit {
         live = std::min<int64_t>(live, p.tokens - first_token);
         if (first_token < 0)
             live = 0;
+        if (p.k.pages <= 0)
+            kv = 0;
         rows = (int)std::min<int64_t>(std::max<int64_t>(live * p.group - first_row, 0), p.rows);
         lo = hi = 0;
         if (rows > 0) {
