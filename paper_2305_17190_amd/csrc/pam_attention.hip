@@ -36,6 +36,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMostWaves = 8;
 constexpr int kGroup = 64;            // keys a wave takes at a time
+constexpr int kLoads = 4;             // loads of a batch at most; a wave has one to two batches in flight
 
 __device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x); }
 __device__ __forceinline__ float real(uint32_t x) { return __uint_as_float(x); }
@@ -81,11 +82,50 @@ __device__ __forceinline__ float wave_sum(float x) {
 
 constexpr int log2_of(int x) { return x <= 1 ? 0 : 1 + log2_of(x / 2); }
 
-// What a wave keeps in LDS of its 64 keys.
+// What a wave keeps in LDS of its 64 keys, and of the next 64.
 template <int R> struct Area {
-    int64_t from[kGroup];             // offsets in the cache (0 where there is none)
-    uint32_t pr[kGroup * R];          // probabilities, as b'
+    int64_t from[2][kGroup];          // offsets in the cache (0 where there is none)
+    uint32_t pr[2][kGroup * R];       // probabilities, as b'
 };
+
+// A wave's loads of its keys, groups first, first + step, ... below end, in
+// batches of B: while one batch is used the next is on its way, the next
+// group's first at the end of a group, so that the memory always has work of
+// the wave.  next(first) starts to fetch what the group from `first` on needs,
+// keep(buffer) puts it where load(buffer, n) finds load n's offset; use(buffer,
+// n, words) takes load n, done(buffer, first) closes a group.
+template <typename T, int L, typename Next, typename Keep, typename From, typename Use, typename Done>
+__device__ __forceinline__ void stream_keys(const void *data, int first, int end, int step, Next next, Keep keep,
+                                            From from, Use use, Done done) {
+    constexpr int B = L / 2 < kLoads ? L / 2 : kLoads;
+    constexpr int N = L / B;
+    if (first >= end)
+        return;
+    u32x4 w[2][B];
+    next(first);
+    keep(0);
+#pragma unroll
+    for (int u = 0; u < B; ++u)
+        w[0][u] = load16<T>(data, from(0, u));
+    for (int buffer = 0; first < end; first += step, buffer ^= 1) {
+        next(first + step);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bool last = i + 1 == N;
+            if (last)
+                keep(buffer ^ 1);
+#pragma unroll
+            for (int u = 0; u < B; ++u)
+                w[(i + 1) & 1][u] = load16<T>(data, last ? from(buffer ^ 1, u) : from(buffer, (i + 1) * B + u));
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < B; ++u)
+                use(buffer, i * B + u, w[i & 1][u]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        done(buffer, first);
+    }
+}
 
 // A unit's rows: which keys they see, where their queries are.
 template <int R> struct Rows {
@@ -141,44 +181,42 @@ __device__ __forceinline__ void load_queries(const AttentionParams &p, const Uni
     }
 }
 
-// The scores, in units of log2, of keys first .. first + 63 (those below end):
-// lane i's are key first + own_key(i)'s, -inf where a row does not see it.
-template <int L> __device__ __forceinline__ int own_key(int lane) {
-    const int u = L == 1 ? 0 : (int)(__brev((uint32_t)(lane % L)) >> (32 - log2_of(L)));
-    return u * (64 / L) + lane / L;
-}
-
-template <typename T, int L, int R>
-__device__ __forceinline__ void score_group(const AttentionParams &p, const Unit &unit, const Rows<R> &rows, int first,
-                                            int end, const uint32_t (&q)[R][kPer<T>], Area<R> &area, float (&t)[R]) {
+// Scores, in units of log2, of the wave's keys first, first + step, ... below end, 64 at a time:
+// take(key, t) gets a key's scores, -inf
+// where a row does not see it.
+template <typename T, int L, int R, typename Take>
+__device__ __forceinline__ void score_keys(const AttentionParams &p, const Unit &unit, int first, int end, int step,
+                                           Area<R> &area, Take take) {
     constexpr int E = kPer<T>;
     constexpr int K = 64 / L;
-    constexpr int B = L < 16 ? L : 16;   // loads in flight
     constexpr int S = log2_of(L);
     const int lane = threadIdx.x & 63;
-    const int at = (lane % L) * E < p.d ? (lane % L) * E : 0;
-    wave_sync();
-    const int64_t place = first + lane < end ? unit.key_at(p, p.k, first + lane) : -1;
-    const uint64_t there = __ballot(place >= 0);
-    area.from[lane] = place >= 0 ? place : 0;
-    wave_sync();
+    const int at = (lane % L) * E, reads = at < p.d ? at : 0;
+    const Rows<R> rows(p, unit);
+    uint32_t q[R][E];
+    load_queries<E, R>(p, unit, at, q);
+    int64_t place = -1;
+    uint64_t there[2] = {0, 0};
     float v[S + 1][R];
-#pragma unroll
-    for (int u0 = 0; u0 < L; u0 += B) {
-        u32x4 w[B];
-#pragma unroll
-        for (int u = 0; u < B; ++u) {
-            w[u] = load16<T>(p.k.data, area.from[(u0 + u) * K + lane / L] + at);
-        }
-#pragma unroll
-        for (int u = 0; u < B; ++u) {
+    stream_keys<T, L>(
+        p.k.data, first, end, step,
+        [&](int from) { place = from + lane < end ? unit.key_at(p, p.k, from + lane) : -1; },
+        [&](int buffer) {
+            wave_sync();
+            there[0] = there[1];
+            there[1] = __ballot(place >= 0);
+            area.from[buffer][lane] = place >= 0 ? place : 0;
+            wave_sync();
+        },
+        [&](int buffer, int n) { return area.from[buffer][n * K + lane / L] + reads; },
+        [&](int, int n, const u32x4 &w) {
             float sum[R];
 #pragma unroll
             for (int r = 0; r < R; ++r)
                 sum[r] = 0.0f;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const uint32_t a = element<T>(w[u], i);
+                const uint32_t a = element<T>(w, i);
                 const float one = one_mantissa(a), m = power(a);
 #pragma unroll
                 for (int r = 0; r < R; ++r)
@@ -186,49 +224,54 @@ __device__ __forceinline__ void score_group(const AttentionParams &p, const Unit
             }
             // Merge with the equal-sized sums before it: bit j of the load's
             // number goes with bit S - 1 - j of the lane's.
-            const int n = u0 + u;
+            int level = 0;
+#pragma unroll
+            for (int j = 0; j < S; ++j)
+                level += (n & ((2 << j) - 1)) == (2 << j) - 1;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float x = sum[r];
-                if constexpr (S > 0) if ((n & 1) == 1) {
+                if (level > 0)
                     x = merge<S - 1>(v[0][r], x, lane);
-                    if constexpr (S > 1) if ((n & 3) == 3) {
-                        x = merge<(S > 1 ? S - 2 : 0)>(v[1][r], x, lane);
-                        if constexpr (S > 2) if ((n & 7) == 7) {
-                            x = merge<(S > 2 ? S - 3 : 0)>(v[2][r], x, lane);
-                            if constexpr (S > 3) if ((n & 15) == 15) {
-                                x = merge<(S > 3 ? S - 4 : 0)>(v[3][r], x, lane);
-                                if constexpr (S > 4) if ((n & 31) == 31) {
-                                    x = merge<(S > 4 ? S - 5 : 0)>(v[4][r], x, lane);
-                                    if constexpr (S > 5) if ((n & 63) == 63)
-                                        x = merge<0>(v[5][r], x, lane);
-                                }
-                            }
-                        }
-                    }
-                }
-                int level = 0;
-#pragma unroll
-                for (int j = 0; j < S; ++j)
-                    level += (n & ((2 << j) - 1)) == (2 << j) - 1;
+                if constexpr (S > 1)
+                    if (level > 1)
+                        x = merge<S - 2>(v[1][r], x, lane);
+                if constexpr (S > 2)
+                    if (level > 2)
+                        x = merge<S - 3>(v[2][r], x, lane);
+                if constexpr (S > 3)
+                    if (level > 3)
+                        x = merge<S - 4>(v[3][r], x, lane);
+                if constexpr (S > 4)
+                    if (level > 4)
+                        x = merge<S - 5>(v[4][r], x, lane);
+                if constexpr (S > 5)
+                    if (level > 5)
+                        x = merge<0>(v[5][r], x, lane);
                 v[level][r] = x;
             }
-        }
-    }
-    const int own = own_key<L>(lane), key = first + own;
-    const bool exists = there >> own & 1;
+        },
+        [&](int buffer, int from) {
+            // The lane's own key: its number's bits from the loads' are the
+            // lane's in reverse.
+            const int own = (int)(__brev((uint32_t)(lane % L)) >> (32 - S)) * K + lane / L, key = from + own;
+            const bool exists = there[0] >> own & 1;
+            float t[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        float sum = v[S][r];
-        const bool sees = exists && key >= rows.lo[r] && key < rows.hi[r];
-        if (sees && !finite(sum)) {
-            sum = 0.0f;
-            const int64_t row = unit.q_at(p, r), from = area.from[own];
-            for (int i = 0; i < p.d; ++i)
-                sum += real(pam_full(load_bits(p.q, row + i, p.q_bf16), load_bits(p.k.data, from + i, sizeof(T) == 2)));
-        }
-        t[r] = sees ? sum * p.scale : kNegInf;
-    }
+            for (int r = 0; r < R; ++r) {
+                float sum = v[S][r];
+                const bool sees = exists && key >= rows.lo[r] && key < rows.hi[r];
+                if (sees && !finite(sum)) {
+                    sum = 0.0f;
+                    const int64_t row = unit.q_at(p, r), k = area.from[buffer][own];
+                    for (int i = 0; i < p.d; ++i)
+                        sum += real(pam_full(load_bits(p.q, row + i, p.q_bf16), load_bits(p.k.data, k + i, sizeof(T) == 2)));
+                }
+                t[r] = sees ? sum * p.scale : kNegInf;
+            }
+            if (key < end)
+                take(key, t);
+        });
 }
 
 template <int R> __device__ __forceinline__ void put(float *to, const float (&t)[R]) {
@@ -314,7 +357,6 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
                                            float *partial) {
     constexpr int E = kPer<T>;
     constexpr int K = 64 / L;
-    constexpr int B = L < 16 ? L : 16;
     constexpr int D = L * E;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int at = (lane % L) * E, reads = at < p.d ? at : 0;
@@ -327,40 +369,38 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
         for (int i = 0; i < E; ++i)
             acc[r][i] = 0.0f;
     }
-    for (int first = begin + wave * kGroup; first < end; first += waves * kGroup) {
-        wave_sync();
-        const int mine = first + lane;
-        const int64_t place = mine < end ? unit.key_at(p, p.v, mine) : -1;
-        area.from[lane] = place >= 0 ? place : 0;
-        float t[R];
-        get<R>(scores + (int64_t)(min(mine, end - 1) - begin) * R, t);
+    int64_t place = -1;
+    float t[R];
+    stream_keys<T, L>(
+        p.v.data, begin + wave * kGroup, end, waves * kGroup,
+        [&](int from) {
+            const int mine = from + lane;
+            place = mine < end ? unit.key_at(p, p.v, mine) : -1;
+            get<R>(scores + (int64_t)(min(mine, end - 1) - begin) * R, t);
+        },
+        [&](int buffer) {
+            wave_sync();
+            area.from[buffer][lane] = place >= 0 ? place : 0;
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            t[r] = real(probability(place >= 0 ? exp2_from(t[r], row.m[r]) : 0.0f, inverse[r]));
-        put<R>(reinterpret_cast<float *>(area.pr) + lane * R, t);
-        wave_sync();
-#pragma unroll 1
-        for (int u0 = 0; u0 < L; u0 += B) {
-            u32x4 w[B];
+            for (int r = 0; r < R; ++r)
+                t[r] = real(probability(place >= 0 ? exp2_from(t[r], row.m[r]) : 0.0f, inverse[r]));
+            put<R>(reinterpret_cast<float *>(area.pr[buffer]) + lane * R, t);
+            wave_sync();
+        },
+        [&](int buffer, int n) { return area.from[buffer][n * K + lane / L] + reads; },
+        [&](int buffer, int n, const u32x4 &w) {
+            float b[R];
+            get<R>(reinterpret_cast<const float *>(area.pr[buffer]) + (n * K + lane / L) * R, b);
 #pragma unroll
-            for (int u = 0; u < B; ++u) {
-                w[u] = load16<T>(p.v.data, area.from[(u0 + u) * K + lane / L] + reads);
+            for (int i = 0; i < E; ++i) {
+                const uint32_t a = element<T>(w, i);
+                const float one = one_mantissa(a), m = power(a);
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    acc[r][i] = pam_fma(one, m, bits(b[r]), acc[r][i]);
             }
-#pragma unroll
-            for (int u = 0; u < B; ++u) {
-                float b[R];
-                get<R>(reinterpret_cast<const float *>(area.pr) + ((u0 + u) * K + lane / L) * R, b);
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    const uint32_t a = element<T>(w[u], i);
-                    const float one = one_mantissa(a), m = power(a);
-#pragma unroll
-                    for (int r = 0; r < R; ++r)
-                        acc[r][i] = pam_fma(one, m, bits(b[r]), acc[r][i]);
-                }
-            }
-        }
-    }
+        },
+        [](int, int) {});
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -424,22 +464,14 @@ __global__ void __launch_bounds__(kMostWaves * 64) attention_whole_kernel(const 
     const Unit unit(p, blockIdx.x);
     if (unit.rows == 0)
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     float *scratch = s + (int64_t)p.max_kv * R;
     Running<R> row;
-    {
-        const Rows<R> rows(p, unit);
-        uint32_t q[R][kPer<T>];
-        load_queries<kPer<T>, R>(p, unit, (lane % L) * kPer<T>, q);
-        for (int first = unit.lo + wave * kGroup; first < unit.hi; first += waves * kGroup) {
-            float t[R];
-            score_group<T, L, R>(p, unit, rows, first, unit.hi, q, areas[wave], t);
-            row.score(t);
-            const int key = first + own_key<L>(lane);
-            if (key < unit.hi)
-                put<R>(s + (key - unit.lo) * R, t);
-        }
-    }
+    score_keys<T, L, R>(p, unit, unit.lo + wave * kGroup, unit.hi, waves * kGroup, areas[wave],
+                        [&](int key, const float (&t)[R]) {
+                            row.score(t);
+                            put<R>(s + (key - unit.lo) * R, t);
+                        });
     row.over_group(top, sum);
     value_keys<T, L, R>(p, unit, unit.lo, unit.hi, s, row, areas, scratch, nullptr);
 }
@@ -459,20 +491,14 @@ __global__ void __launch_bounds__(kThreads) attention_scores_kernel(const Attent
     const int begin = max(unit.lo, split * p.split_keys), end = min(unit.hi, (split + 1) * p.split_keys);
     if (unit.rows == 0 || begin >= end)
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wave = threadIdx.x >> 6;
     Running<R> row;
-    const Rows<R> rows(p, unit);
-    uint32_t q[R][kPer<T>];
-    load_queries<kPer<T>, R>(p, unit, (lane % L) * kPer<T>, q);
     float *scores = p.scores + (int64_t)index * p.splits * p.split_keys * R;
-    for (int first = begin + wave * kGroup; first < end; first += kThreads) {
-        float t[R];
-        score_group<T, L, R>(p, unit, rows, first, end, q, areas[wave], t);
-        row.score(t);
-        const int key = first + own_key<L>(lane);
-        if (key < end)
-            put<R>(scores + (int64_t)key * R, t);
-    }
+    score_keys<T, L, R>(p, unit, begin + wave * kGroup, end, kThreads, areas[wave],
+                        [&](int key, const float (&t)[R]) {
+                            row.score(t);
+                            put<R>(scores + (int64_t)key * R, t);
+                        });
     row.over_group(top, sum);
     if (threadIdx.x == 0) {
         float *stats = p.stats + ((int64_t)index * p.splits + split) * 2 * R;

@@ -109,7 +109,7 @@ inline int whole_waves(int max_kv) { return max_kv <= 256 ? 4 : 8; }
 // 64 keys it works on.
 inline int64_t whole_lds(int64_t max_kv, int64_t rows, int lanes, bool bf16) {
     const int64_t waves = 8;
-    return 4 * rows * (max_kv + waves * lanes * (bf16 ? 8 : 4)) + waves * 64 * (8 + 4 * rows) + 512;
+    return 4 * rows * (max_kv + waves * lanes * (bf16 ? 8 : 4)) + waves * 128 * (8 + 4 * rows) + 512;
 }
 constexpr int64_t kWholeLds = 65536;   // at most
 hipError_t launch_attention_whole(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream);
