@@ -10,7 +10,8 @@
  *
  * The conventions of pam.h hold: device pointers, strides in elements, every
  * call asynchronous on `stream`, no allocation, arguments validated before
- * anything is launched.  What lies in device memory (positions, slots,
+ * anything is launched.  A call's arguments are one structure, read before the
+ * call returns: the pointers, then the layouts and sizes.  What lies in device memory (positions, slots,
  * lengths, page tables) cannot be validated by the host: each call says what
  * a value out of range does, and none makes a kernel leave its buffers as
  * long as the arrays have the stated sizes.
@@ -35,25 +36,23 @@ typedef enum { PAM_TYPE_F32 = 0, PAM_TYPE_BF16 = 1 } pam_type_t;
 #define PAM_MAX_HEAD_DIM 256
 
 /* Values x[t][h][i] = data[t*stride_token + h*stride_head + i] of `heads`
- * heads: views into a projection's output are such. */
+ * heads: views into a projection's output are such.  heads == 0: the operand
+ * is not given. */
 typedef struct {
-    void *data;
     int64_t stride_token, stride_head;
     int32_t heads;
     pam_type_t type;
 } pam_heads_t;
 
 /*
- * The position rotation: the first `rot` values of a head (even, 0..d) are
+ * The position rotation: the first `rot` values of a head (even, 0 .. d) are
  * pairs p = 0 .. rot/2 - 1, values (p, p + rot/2), or (2p, 2p + 1) where
  * interleaved != 0.  A token at position n turns pair p by the angle whose
  * cosine and sine are cos[n*rot/2 + p] and sin[n*rot/2 + p]; the tables have
  * `rows` positions.  positions: one int32 a token.  A position outside
- * [0, rows) gives NaN in the rotated values.
+ * [0, rows) gives NaN in the rotated values.  rot == 0: no rotation.
  */
 typedef struct {
-    const int32_t *positions;
-    const float *cos, *sin;
     int64_t rows;
     int32_t rot;
     int32_t interleaved;
@@ -66,12 +65,12 @@ typedef struct {
  * < 2^31.
  */
 typedef struct {
-    void *data;
     int64_t stride_page, stride_slot, stride_head;
     int64_t pages;
     int32_t page_size;
     int32_t heads;
     pam_type_t type;
+    int32_t reserved;
 } pam_cache_t;
 
 /*
@@ -81,14 +80,26 @@ typedef struct {
  *   out[t][h] = rotation of y at the token's position
  * in float32, rounded once to out's type (nearest even).  d even, 2 .. 256.
  * q and k are each a pair of in and out with equal head counts (out may be
- * in); both or one of them given (NULL in and out: none).  q_in and k_in
- * have one type.  rotation NULL: no rotation.  tokens == 0 launches nothing.
- * eps >= 0 and finite.
+ * in); both or one of them given.  q_in and k_in have one type.  tokens == 0
+ * launches nothing.  eps >= 0 and finite.
  */
-pam_status_t pam_norm_rope(int64_t tokens, int32_t d, const pam_heads_t *q_in, const float *q_weight,
-                           const pam_heads_t *q_out, const pam_heads_t *k_in, const float *k_weight,
-                           const pam_heads_t *k_out, float eps, const pam_rotation_t *rotation,
-                           hipStream_t stream);
+typedef struct {
+    const void *q_in;
+    void *q_out;
+    const float *q_weight;
+    const void *k_in;
+    void *k_out;
+    const float *k_weight;
+    const int32_t *positions;
+    const float *cos, *sin;
+    pam_heads_t q_in_heads, q_out_heads, k_in_heads, k_out_heads;
+    pam_rotation_t rotation;
+    int64_t tokens;
+    int32_t d;
+    float eps;
+} pam_norm_rope_t;
+
+pam_status_t pam_norm_rope(const pam_norm_rope_t *args, hipStream_t stream);
 
 /*
  * Its gradient.  With dz = grad_out[t][h] and g = dz rotated back:
@@ -99,34 +110,67 @@ pam_status_t pam_norm_rope(int64_t tokens, int32_t d, const pam_heads_t *q_in, c
  * non-NULL exactly where the weight is).  The same for k; one of the two may
  * be left out.  The three heads of q and of k have one type.  The sums over
  * tokens run in a fixed order over partial sums in `workspace`
- * (pam_norm_rope_grad_workspace_size bytes, 16-byte aligned; 0 without
- * weights).  tokens == 0 writes zeros to the weights' gradients.
+ * (pam_norm_rope_grad_workspace_size bytes, 16-byte aligned; none needed
+ * without weights).  tokens == 0 writes zeros to the weights' gradients.
  */
+typedef struct {
+    const void *q_in;
+    const float *q_weight;
+    const void *dq_out;
+    void *dq_in;
+    float *dq_weight;
+    const void *k_in;
+    const float *k_weight;
+    const void *dk_out;
+    void *dk_in;
+    float *dk_weight;
+    const int32_t *positions;
+    const float *cos, *sin;
+    void *workspace;
+    pam_heads_t q_in_heads, dq_out_heads, dq_in_heads, k_in_heads, dk_out_heads, dk_in_heads;
+    pam_rotation_t rotation;
+    int64_t tokens;
+    int64_t workspace_bytes;
+    int32_t d;
+    float eps;
+} pam_norm_rope_grad_t;
+
 pam_status_t pam_norm_rope_grad_workspace_size(int64_t tokens, int32_t d, int32_t q_heads, int32_t k_heads,
                                                size_t *bytes);
 
-pam_status_t pam_norm_rope_grad(int64_t tokens, int32_t d, const pam_heads_t *q_in, const float *q_weight,
-                                const pam_heads_t *dq_out, const pam_heads_t *dq_in, float *dq_weight,
-                                const pam_heads_t *k_in, const float *k_weight, const pam_heads_t *dk_out,
-                                const pam_heads_t *dk_in, float *dk_weight, float eps,
-                                const pam_rotation_t *rotation, void *workspace, size_t workspace_bytes,
-                                hipStream_t stream);
+pam_status_t pam_norm_rope_grad(const pam_norm_rope_grad_t *args, hipStream_t stream);
 
 /*
  * Appends the keys and values of `tokens` tokens to a paged cache: token t
  * goes to slot slots[t] % page_size of page slots[t] / page_size; a slot
  * outside [0, pages * page_size) is not stored (padding tokens carry -1).
- * Keys are normed (k_weight non-NULL) and rotated (rotation non-NULL) on the
- * way as in pam_norm_rope, values stored as they are; both are rounded to the
- * cache's type (nearest even).  q_in / q_out (NULL: none): the same tokens'
- * queries, normed and rotated in the same launch.  k, v and q_in have one
- * type, k and v as many heads as the caches.  Two tokens with one slot race.
+ * Keys are normed (k_weight non-NULL) and rotated (rot > 0) on the way as in
+ * pam_norm_rope, values stored as they are; both are rounded to the cache's
+ * type (nearest even).  q_in / q_out (optional): the same tokens' queries,
+ * normed and rotated in the same launch.  k, v and q_in have one type, k and
+ * v as many heads as the caches.  Two tokens with one slot race.
  */
-pam_status_t pam_append_kv(int64_t tokens, int32_t d, const pam_heads_t *k, const float *k_weight,
-                           const pam_heads_t *v, const pam_heads_t *q_in, const float *q_weight,
-                           const pam_heads_t *q_out, float eps, const pam_rotation_t *rotation,
-                           const pam_cache_t *k_cache, const pam_cache_t *v_cache, const int64_t *slots,
-                           hipStream_t stream);
+typedef struct {
+    const void *k;
+    const float *k_weight;
+    const void *v;
+    const void *q_in;
+    const float *q_weight;
+    void *q_out;
+    void *k_cache;
+    void *v_cache;
+    const int64_t *slots;
+    const int32_t *positions;
+    const float *cos, *sin;
+    pam_heads_t k_heads, v_heads, q_in_heads, q_out_heads;
+    pam_cache_t k_cache_layout, v_cache_layout;
+    pam_rotation_t rotation;
+    int64_t tokens;
+    int32_t d;
+    float eps;
+} pam_append_kv_t;
+
+pam_status_t pam_append_kv(const pam_append_kv_t *args, hipStream_t stream);
 
 /*
  * PAM attention of new tokens over a paged cache.  Sequence b (0 <= b <
@@ -148,35 +192,41 @@ pam_status_t pam_append_kv(int64_t tokens, int32_t d, const pam_heads_t *k, cons
  * instead of as zero.
  *
  * max_q: at least every sequence's count of new tokens (tokens past it get
- * no output); max_kv: at least every kv_lens[b] (keys past it are not seen),
- * at most table_width * page_size, the table's row length.  q and out: tokens
- * x heads x d, out float32; heads a multiple of the caches'; d a multiple of
- * 8, 8 .. 256.  scale finite.  workspace: pam_paged_attention_workspace_size
- * bytes for the same sizes (0 possible), 16-byte aligned, untouched by others
- * until the call's kernels are done.
+ * no output, nor do tokens of no sequence); max_kv: at least every kv_lens[b]
+ * (keys past it are not seen), at most table_width * page_size, the table's
+ * row length.  q and out: tokens x heads x d, out float32; heads a multiple
+ * of the caches'; d a multiple of 8, 8 .. 256.  window >= 0.  scale finite.
+ * workspace: pam_paged_attention_workspace_size bytes for the same sizes (0
+ * possible), 16-byte aligned, untouched by others until the call's kernels
+ * are done.
  */
 typedef struct {
+    const void *q;
+    const void *k_cache, *v_cache;
+    float *out;
     const int32_t *q_starts;   /* batch + 1, or NULL */
     const int32_t *kv_lens;    /* batch */
     const int32_t *table;      /* batch rows of table_width entries */
+    void *workspace;
+    pam_heads_t q_heads, out_heads;
+    pam_cache_t k_cache_layout, v_cache_layout;
     int64_t table_stride;
     int64_t tokens;            /* rows of q and out */
+    int32_t d;
     int32_t batch;
     int32_t table_width;
-    int32_t max_q;
-    int32_t max_kv;
     int32_t causal;
     int32_t window;
     float scale;
-} pam_sequences_t;
+    int32_t max_q;
+    int32_t max_kv;
+    int64_t workspace_bytes;
+} pam_paged_attention_t;
 
 pam_status_t pam_paged_attention_workspace_size(int32_t d, int32_t q_heads, int32_t kv_heads, pam_type_t kv_type,
                                                 int32_t batch, int32_t max_q, int32_t max_kv, size_t *bytes);
 
-pam_status_t pam_paged_attention(int32_t d, const pam_heads_t *q, const pam_cache_t *k_cache,
-                                 const pam_cache_t *v_cache, const pam_sequences_t *sequences,
-                                 const pam_heads_t *out, void *workspace, size_t workspace_bytes,
-                                 hipStream_t stream);
+pam_status_t pam_paged_attention(const pam_paged_attention_t *args, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -20,6 +20,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
 from . import _check, _launch, _require, _same_device, _torch, load
 
@@ -29,29 +30,10 @@ __all__ = ["norm_rope", "norm_rope_grad", "append_kv", "paged_attention"]
 EXPORTS = ("pam_norm_rope", "pam_norm_rope_grad_workspace_size", "pam_norm_rope_grad", "pam_append_kv",
            "pam_paged_attention_workspace_size", "pam_paged_attention")
 
-
-class _Heads(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("stride_token", ctypes.c_int64), ("stride_head", ctypes.c_int64),
-                ("heads", ctypes.c_int32), ("type", ctypes.c_int32)]
-
-
-class _Rotation(ctypes.Structure):
-    _fields_ = [("positions", ctypes.c_void_p), ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p),
-                ("rows", ctypes.c_int64), ("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
-
-
-class _Cache(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("stride_page", ctypes.c_int64), ("stride_slot", ctypes.c_int64),
-                ("stride_head", ctypes.c_int64), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
-                ("heads", ctypes.c_int32), ("type", ctypes.c_int32)]
-
-
-class _Sequences(ctypes.Structure):
-    _fields_ = [("q_starts", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p), ("table", ctypes.c_void_p),
-                ("table_stride", ctypes.c_int64), ("tokens", ctypes.c_int64), ("batch", ctypes.c_int32),
-                ("table_width", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_kv", ctypes.c_int32),
-                ("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("scale", ctypes.c_float)]
-
+# The argument structures of include/pam_attention.h: the pointers, then the
+# layouts and sizes (``_HEADS``, ``_ROTATION``, ``_CACHE``).
+_HEADS, _ROTATION, _CACHE = "qqii", "qii", "qqqqiiii"
+_NONE = (0, 0, 0, 0)
 
 _bound = None
 
@@ -60,15 +42,11 @@ def _library() -> ctypes.CDLL:
     global _bound
     if _bound is None:
         lib = load()
-        i32, i64, vp, f32, sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float, ctypes.c_size_t
-        heads, rotation, cache = (ctypes.POINTER(t) for t in (_Heads, _Rotation, _Cache))
-        lib.pam_norm_rope.argtypes = [i64, i32, heads, vp, heads, heads, vp, heads, f32, rotation, vp]
-        lib.pam_norm_rope_grad_workspace_size.argtypes = [i64, i32, i32, i32, ctypes.POINTER(sz)]
-        lib.pam_norm_rope_grad.argtypes = [i64, i32, heads, vp, heads, heads, vp, heads, vp, heads, heads, vp, f32,
-                                           rotation, vp, sz, vp]
-        lib.pam_append_kv.argtypes = [i64, i32, heads, vp, heads, heads, vp, heads, f32, rotation, cache, cache, vp, vp]
-        lib.pam_paged_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
-        lib.pam_paged_attention.argtypes = [i32, heads, cache, cache, ctypes.POINTER(_Sequences), heads, vp, sz, vp]
+        i32, i64, vp, psz = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.POINTER(ctypes.c_size_t)
+        for name in ("pam_norm_rope", "pam_norm_rope_grad", "pam_append_kv", "pam_paged_attention"):
+            getattr(lib, name).argtypes = [ctypes.c_char_p, vp]
+        lib.pam_norm_rope_grad_workspace_size.argtypes = [i64, i32, i32, i32, psz]
+        lib.pam_paged_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, i32, psz]
         for name in EXPORTS:
             getattr(lib, name).restype = i32
         _bound = lib
@@ -80,15 +58,15 @@ def _is_bf16(t) -> int:
 
 
 def _heads(t):
-    return None if t is None else _Heads(t.data_ptr(), t.stride(0), t.stride(1), t.shape[1], _is_bf16(t))
+    return _NONE if t is None else (t.stride(0), t.stride(1), t.shape[1], _is_bf16(t))
 
 
 def _cache(t):
-    return _Cache(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2), t.shape[0], t.shape[1], t.shape[2], _is_bf16(t))
+    return (t.stride(0), t.stride(1), t.stride(2), t.shape[0], t.shape[1], t.shape[2], _is_bf16(t), 0)
 
 
 def _ints(t, name: str, dtype, *shape):
-    """An index tensor of the given type and shape (None: any), contiguous."""
+    """An index tensor of the given type and shape (None: any), contiguous, on the GPU."""
     torch = _torch()
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
@@ -108,11 +86,11 @@ def _weight(w, name: str, d: int):
 
 
 def _rotation(positions, cos, sin, interleaved: bool, tokens: int, d: int):
-    """The rotation's arguments, or None where there is none."""
+    """The rotation's layout; rot = 0 where there is none."""
     torch = _torch()
     given = [x is not None for x in (positions, cos, sin)]
     if not any(given):
-        return None
+        return (0, 0, 0)
     if not all(given):
         raise ValueError("positions, cos and sin must be given together")
     _ints(positions, "positions", torch.int32, tokens)
@@ -124,16 +102,7 @@ def _rotation(positions, cos, sin, interleaved: bool, tokens: int, d: int):
         raise ValueError(f"cos and sin differ in shape: {tuple(cos.shape)} and {tuple(sin.shape)}")
     if 2 * cos.shape[1] > d:
         raise ValueError(f"the tables turn {2 * cos.shape[1]} values, the heads have {d}")
-    return _Rotation(positions.data_ptr(), cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1],
-                     int(bool(interleaved)))
-
-
-def _ref(struct):
-    return None if struct is None else ctypes.byref(struct)
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+    return (cos.shape[0], 2 * cos.shape[1], int(interleaved))
 
 
 def _head_tensors(*named):
@@ -158,17 +127,37 @@ def _head_tensors(*named):
     return first[1]
 
 
-def norm_rope(q, k, positions=None, cos=None, sin=None, q_weight=None, k_weight=None, eps: float = 1e-6,
-              interleaved: bool = False, out_dtype=None):
-    """Norm and position rotation of queries (tokens, heads, d) and keys (tokens,
-    key heads, d) in one pass; returns (q', k'), either input may be None.
+# Calls whose arguments' types, shapes, strides and devices have been checked
+# before: by all of these, the part of the argument structure that follows the
+# pointers, and what else the call needs.  (Checked anew, each call of
+# append_kv took 21 us of host time, of paged_attention 15.)
+_calls = {}
 
-    With a weight (d float32 values) a head's values x become x * weight /
-    sqrt(mean(x^2) + eps).  ``cos`` and ``sin`` are float32 (rows, rot / 2)
-    tables, ``positions`` int32 (tokens): the first ``rot`` values of each head
-    are turned in pairs (p, p + rot / 2), or (2p, 2p + 1) if ``interleaved``,
-    by the angles of the token's position.  float32 arithmetic, rounded once to
-    ``out_dtype`` (the inputs' type)."""
+
+def _sig(t):
+    return None if t is None else (t.dtype, t.shape, t.stride(), t.get_device())
+
+
+def _known(key, plan):
+    """The call's plan: plan() checks the arguments and makes it."""
+    try:
+        return _calls[key]
+    except KeyError:
+        made = plan()
+        if len(_calls) >= 4096:
+            _calls.clear()
+        _calls[key] = made
+        return made
+
+
+def _ptr(t):
+    return 0 if t is None else t.data_ptr()
+
+
+_norm_rope_ptrs = struct.Struct("9Q").pack
+
+
+def _norm_rope_plan(q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved, out_dtype):
     torch = _torch()
     ref = _head_tensors(("q", q), ("k", k))
     tokens, _, d = ref.shape
@@ -180,11 +169,70 @@ def norm_rope(q, k, positions=None, cos=None, sin=None, q_weight=None, k_weight=
     dtype = ref.dtype if out_dtype is None else out_dtype
     if dtype not in (torch.float32, torch.bfloat16):
         raise TypeError(f"out_dtype must be float32 or bfloat16, got {dtype}")
-    qo, ko = (None if t is None else torch.empty(t.shape, dtype=dtype, device=ref.device) for t in (q, k))
-    _launch(ref, _library().pam_norm_rope, tokens, d, _ref(_heads(q)), _ptr(q_weight if q is not None else None),
-            _ref(_heads(qo)), _ref(_heads(k)), _ptr(k_weight if k is not None else None), _ref(_heads(ko)), float(eps),
-            _ref(rot))
+    outs = [_NONE if t is None else (t.shape[1] * d, d, t.shape[1], int(dtype == torch.bfloat16)) for t in (q, k)]
+    tail = struct.pack("=" + _HEADS * 4 + _ROTATION + "qif", *_heads(q), *outs[0], *_heads(k), *outs[1], *rot, tokens, d,
+                       eps)
+    return tail, dtype
+
+
+def norm_rope(q, k, positions=None, cos=None, sin=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+              interleaved: bool = False, out_dtype=None):
+    """Norm and position rotation of queries (tokens, heads, d) and keys (tokens,
+    key heads, d) in one pass; returns (q', k'), either input may be None.
+
+    With a weight (d float32 values) a head's values x become x * weight /
+    sqrt(mean(x^2) + eps).  ``cos`` and ``sin`` are float32 (rows, rot / 2)
+    tables, ``positions`` int32 (tokens): the first ``rot`` values of each head
+    are turned in pairs (p, p + rot / 2), or (2p, 2p + 1) if ``interleaved``,
+    by the angles of the token's position.  float32 arithmetic, rounded once to
+    ``out_dtype`` (the inputs' type)."""
+    eps, interleaved = float(eps), bool(interleaved)
+    if q is None:
+        q_weight = None
+    if k is None:
+        k_weight = None
+    try:
+        key = (0, _sig(q), _sig(k), _sig(positions), _sig(cos), _sig(sin), _sig(q_weight), _sig(k_weight), eps,
+               interleaved, out_dtype)
+    except AttributeError:
+        key = None
+    args = (q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved, out_dtype)
+    tail, dtype = _norm_rope_plan(*args) if key is None else _known(key, lambda: _norm_rope_plan(*args))
+    empty = _torch().empty
+    ref = q if q is not None else k
+    qo, ko = (None if t is None else empty(t.shape, dtype=dtype, device=ref.device) for t in (q, k))
+    _launch(ref, (_bound or _library()).pam_norm_rope, _norm_rope_ptrs(
+        _ptr(q), _ptr(qo), _ptr(q_weight), _ptr(k), _ptr(ko), _ptr(k_weight), _ptr(positions), _ptr(cos), _ptr(sin))
+        + tail)
     return qo, ko
+
+
+_norm_rope_grad_ptrs = struct.Struct("14Q").pack
+
+
+def _norm_rope_grad_plan(dq, dk, q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved):
+    if (dq is None) != (q is None) or (dk is None) != (k is None):
+        raise ValueError("q and dq, k and dk must be given together")
+    ref = _head_tensors(("q", q), ("dq", dq), ("k", k), ("dk", dk))
+    for x, dx, name in ((q, dq, "dq"), (k, dk, "dk")):
+        if x is not None and x.shape != dx.shape:
+            raise ValueError(f"{name} must have shape {tuple(x.shape)}, got {tuple(dx.shape)}")
+    tokens, _, d = ref.shape
+    _weight(q_weight, "q_weight", d)
+    _weight(k_weight, "k_weight", d)
+    rot = _rotation(positions, cos, sin, interleaved, tokens, d)
+    _same_device(ref, ("q_weight", q_weight), ("k_weight", k_weight), ("positions", positions), ("cos", cos),
+                 ("sin", sin))
+    nbytes = 0
+    if q_weight is not None or k_weight is not None:
+        need = ctypes.c_size_t()
+        _check(_library().pam_norm_rope_grad_workspace_size(tokens, d, 0 if q is None else q.shape[1],
+                                                            0 if k is None else k.shape[1], ctypes.byref(need)))
+        nbytes = int(need.value)
+    outs = [_NONE if t is None else (t.shape[1] * d, d, t.shape[1], _is_bf16(t)) for t in (q, k)]
+    tail = struct.pack("=" + _HEADS * 6 + _ROTATION + "qqif", *_heads(q), *_heads(dq), *outs[0], *_heads(k), *_heads(dk),
+                       *outs[1], *rot, tokens, nbytes, d, eps)
+    return tail, nbytes
 
 
 def norm_rope_grad(dq, dk, q, k, positions=None, cos=None, sin=None, q_weight=None, k_weight=None,
@@ -193,36 +241,26 @@ def norm_rope_grad(dq, dk, q, k, positions=None, cos=None, sin=None, q_weight=No
     its inputs, (gradient of q, of k, of q_weight, of k_weight); None for what
     was not given.  Gradients have their input's type, the weights' float32."""
     torch = _torch()
-    if (dq is None) != (q is None) or (dk is None) != (k is None):
-        raise ValueError("q and dq, k and dk must be given together")
-    ref = _head_tensors(("q", q), ("dq", dq), ("k", k), ("dk", dk))
-    for x, dx, name in ((q, dq, "dq"), (k, dk, "dk")):
-        if x is not None and x.shape != dx.shape:
-            raise ValueError(f"{name} must have shape {tuple(x.shape)}, got {tuple(dx.shape)}")
-    tokens, _, d = ref.shape
+    eps, interleaved = float(eps), bool(interleaved)
     if q is None:
         q_weight = None
     if k is None:
         k_weight = None
-    _weight(q_weight, "q_weight", d)
-    _weight(k_weight, "k_weight", d)
-    rot = _rotation(positions, cos, sin, interleaved, tokens, d)
-    _same_device(ref, ("q_weight", q_weight), ("k_weight", k_weight), ("positions", positions), ("cos", cos),
-                 ("sin", sin))
-    gq, gk = (None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
-    gqw, gkw = (None if w is None else torch.empty_like(w) for w in (q_weight, k_weight))
-    lib = _library()
-    keep = None
-    nbytes = 0
-    if gqw is not None or gkw is not None:
-        need = ctypes.c_size_t()
-        _check(lib.pam_norm_rope_grad_workspace_size(tokens, d, 0 if q is None else q.shape[1],
-                                                     0 if k is None else k.shape[1], ctypes.byref(need)))
-        nbytes = int(need.value)
-        keep = torch.empty(nbytes, dtype=torch.uint8, device=ref.device) if nbytes else None
-    _launch(ref, lib.pam_norm_rope_grad, tokens, d, _ref(_heads(q)), _ptr(q_weight), _ref(_heads(dq)),
-            _ref(_heads(gq)), _ptr(gqw), _ref(_heads(k)), _ptr(k_weight), _ref(_heads(dk)), _ref(_heads(gk)), _ptr(gkw),
-            float(eps), _ref(rot), _ptr(keep), nbytes)
+    try:
+        key = (1, _sig(dq), _sig(dk), _sig(q), _sig(k), _sig(positions), _sig(cos), _sig(sin), _sig(q_weight),
+               _sig(k_weight), eps, interleaved)
+    except AttributeError:
+        key = None
+    args = (dq, dk, q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved)
+    tail, nbytes = _norm_rope_grad_plan(*args) if key is None else _known(key, lambda: _norm_rope_grad_plan(*args))
+    ref = q if q is not None else k
+    empty, device = torch.empty, ref.device
+    gq, gk = (None if t is None else empty(t.shape, dtype=t.dtype, device=device) for t in (q, k))
+    gqw, gkw = (None if w is None else empty(w.shape, dtype=w.dtype, device=device) for w in (q_weight, k_weight))
+    keep = empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    _launch(ref, (_bound or _library()).pam_norm_rope_grad, _norm_rope_grad_ptrs(
+        _ptr(q), _ptr(q_weight), _ptr(dq), _ptr(gq), _ptr(gqw), _ptr(k), _ptr(k_weight), _ptr(dk), _ptr(gk), _ptr(gkw),
+        _ptr(positions), _ptr(cos), _ptr(sin), _ptr(keep)) + tail)
     del keep
     return gq, gk, gqw, gkw
 
@@ -235,15 +273,10 @@ def _caches(k_cache, v_cache):
     _same_device(k_cache, ("v_cache", v_cache))
 
 
-def append_kv(k, v, k_cache, v_cache, slots, positions=None, cos=None, sin=None, k_weight=None, q=None, q_weight=None,
-              eps: float = 1e-6, interleaved: bool = False):
-    """Writes the keys and values (tokens, key heads, d) of new tokens into the
-    paged caches (pages, page_size, key heads, d): token t to slot ``slots[t]``
-    (int64, page * page_size + place; outside the cache, as -1: not stored).
-    Keys are normed (``k_weight``) and rotated as by ``norm_rope`` on the way;
-    both are rounded to the cache's type.  With ``q``, the same tokens' queries
-    are normed (``q_weight``) and rotated in the same launch and returned in
-    q's type, else None."""
+_append_ptrs = struct.Struct("12Q").pack
+
+
+def _append_plan(k, v, k_cache, v_cache, slots, positions, cos, sin, k_weight, q, q_weight, eps, interleaved):
     torch = _torch()
     ref = _head_tensors(("k", k), ("v", v), ("q", q))
     _caches(k_cache, v_cache)
@@ -256,10 +289,34 @@ def append_kv(k, v, k_cache, v_cache, slots, positions=None, cos=None, sin=None,
     rot = _rotation(positions, cos, sin, interleaved, tokens, d)
     _same_device(ref, ("k_cache", k_cache), ("slots", slots), ("q_weight", q_weight), ("k_weight", k_weight),
                  ("positions", positions), ("cos", cos), ("sin", sin))
-    qo = None if q is None else torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _launch(ref, _library().pam_append_kv, tokens, d, _ref(_heads(k)), _ptr(k_weight), _ref(_heads(v)),
-            _ref(_heads(q)), _ptr(q_weight if q is not None else None), _ref(_heads(qo)), float(eps), _ref(rot),
-            _ref(_cache(k_cache)), _ref(_cache(v_cache)), slots.data_ptr())
+    out = _NONE if q is None else (q.shape[1] * d, d, q.shape[1], _is_bf16(q))
+    return struct.pack("=" + _HEADS * 4 + _CACHE * 2 + _ROTATION + "qif", *_heads(k), *_heads(v), *_heads(q), *out,
+                       *_cache(k_cache), *_cache(v_cache), *rot, tokens, d, eps)
+
+
+def append_kv(k, v, k_cache, v_cache, slots, positions=None, cos=None, sin=None, k_weight=None, q=None, q_weight=None,
+              eps: float = 1e-6, interleaved: bool = False):
+    """Writes the keys and values (tokens, key heads, d) of new tokens into the
+    paged caches (pages, page_size, key heads, d): token t to slot ``slots[t]``
+    (int64, page * page_size + place; outside the cache, as -1: not stored).
+    Keys are normed (``k_weight``) and rotated as by ``norm_rope`` on the way;
+    both are rounded to the cache's type.  With ``q``, the same tokens' queries
+    are normed (``q_weight``) and rotated in the same launch and returned in
+    q's type, else None."""
+    eps, interleaved = float(eps), bool(interleaved)
+    if q is None:
+        q_weight = None
+    args = (k, v, k_cache, v_cache, slots, positions, cos, sin, k_weight, q, q_weight, eps, interleaved)
+    try:
+        key = (2, _sig(k), _sig(v), _sig(k_cache), _sig(v_cache), _sig(slots), _sig(positions), _sig(cos), _sig(sin),
+               _sig(k_weight), _sig(q), _sig(q_weight), eps, interleaved)
+    except AttributeError:
+        key = None
+    tail = _append_plan(*args) if key is None else _known(key, lambda: _append_plan(*args))
+    qo = None if q is None else _torch().empty(q.shape, dtype=q.dtype, device=q.device)
+    _launch(k, (_bound or _library()).pam_append_kv, _append_ptrs(
+        _ptr(k), _ptr(k_weight), _ptr(v), _ptr(q), _ptr(q_weight), _ptr(qo), _ptr(k_cache), _ptr(v_cache), _ptr(slots),
+        _ptr(positions), _ptr(cos), _ptr(sin)) + tail)
     return qo
 
 
@@ -279,6 +336,43 @@ def _attention_workspace(sizes: tuple) -> int:
     return nbytes
 
 
+_attention_ptrs, _attention_end = struct.Struct("8Q").pack, struct.Struct("=iiq").pack
+
+
+def _attention_plan(q, k_cache, v_cache, table, kv_lens, q_starts, scale, causal, window, out):
+    torch = _torch()
+    _require(q, "q", 3, bf16_ok=True)
+    _caches(k_cache, v_cache)
+    tokens, heads, d = q.shape
+    page_size, kv_heads, cache_d = k_cache.shape[1:]
+    if k_cache.dtype != v_cache.dtype:
+        raise TypeError(f"the caches differ in type: {k_cache.dtype} and {v_cache.dtype}")
+    if cache_d != d:
+        raise ValueError(f"q has heads of {d} values, the caches of {cache_d}")
+    if not isinstance(kv_lens, torch.Tensor) or kv_lens.dim() != 1:
+        raise ValueError("kv_lens must be a one-dimensional tensor")
+    batch = kv_lens.shape[0]
+    _ints(kv_lens, "kv_lens", torch.int32, batch)
+    _ints(table, "table", torch.int32, batch, None)
+    if q_starts is not None:
+        _ints(q_starts, "q_starts", torch.int32, batch + 1)
+    elif tokens != batch:
+        raise ValueError(f"without q_starts q must have one token a sequence: {tokens} tokens, {batch} sequences")
+    if window < 0:
+        raise ValueError("window must be >= 0")
+    outs = (heads * d, d, heads, 0)
+    if out is not None:
+        _require(out, "out", 3)
+        if out.shape != q.shape:
+            raise ValueError(f"out must have shape {tuple(q.shape)}, got {tuple(out.shape)}")
+        outs = _heads(out)
+    _same_device(q, ("k_cache", k_cache), ("table", table), ("kv_lens", kv_lens), ("q_starts", q_starts), ("out", out))
+    width = table.shape[1]
+    tail = struct.pack("=" + _HEADS * 2 + _CACHE * 2 + "qqiiiiif", *_heads(q), *outs, *_cache(k_cache), *_cache(v_cache),
+                       width, tokens, d, batch, width, int(causal), window, 1.0 / math.sqrt(d) if scale is None else scale)
+    return tail, (d, heads, kv_heads, _is_bf16(k_cache), batch), width * page_size
+
+
 def paged_attention(q, k_cache, v_cache, table, kv_lens, q_starts=None, max_q: int = 1, max_kv: int | None = None,
                     scale: float | None = None, causal: bool = True, window: int = 0, out=None):
     """softmax(scale Q .^ K^T) .^ V of new tokens over a paged cache, as float32
@@ -294,44 +388,23 @@ def paged_attention(q, k_cache, v_cache, table, kv_lens, q_starts=None, max_q: i
     its own position (all, without ``causal``), the last ``window`` of them
     where that is positive; a token without keys gets zeros.  ``scale`` is 1 /
     sqrt(d) if not given.  Tokens of no sequence are left unwritten."""
+    causal, window, scale = bool(causal), int(window), None if scale is None else float(scale)
+    args = (q, k_cache, v_cache, table, kv_lens, q_starts, scale, causal, window, out)
+    try:
+        key = (3, _sig(q), _sig(k_cache), _sig(v_cache), _sig(table), _sig(kv_lens), _sig(q_starts), scale, causal,
+               window, _sig(out))
+    except AttributeError:
+        key = None
+    tail, sizes, reach = _attention_plan(*args) if key is None else _known(key, lambda: _attention_plan(*args))
     torch = _torch()
-    _require(q, "q", 3, bf16_ok=True)
-    _caches(k_cache, v_cache)
-    tokens, heads, d = q.shape
-    pages, page_size, kv_heads, cache_d = k_cache.shape
-    if k_cache.dtype != v_cache.dtype:
-        raise TypeError(f"the caches differ in type: {k_cache.dtype} and {v_cache.dtype}")
-    if cache_d != d:
-        raise ValueError(f"q has heads of {d} values, the caches of {cache_d}")
-    if not isinstance(kv_lens, torch.Tensor) or kv_lens.dim() != 1:
-        raise ValueError("kv_lens must be a one-dimensional tensor")
-    batch = kv_lens.shape[0]
-    _ints(kv_lens, "kv_lens", torch.int32, batch)
-    _ints(table, "table", torch.int32, batch, None)
-    if q_starts is not None:
-        _ints(q_starts, "q_starts", torch.int32, batch + 1)
-    elif tokens != batch:
-        raise ValueError(f"without q_starts q must have one token a sequence: {tokens} tokens, {batch} sequences")
-    else:
-        max_q = 1
-    if max_kv is None:
-        max_kv = table.shape[1] * page_size
-    if window < 0:
-        raise ValueError("window must be >= 0")
+    max_q = 1 if q_starts is None else int(max_q)
+    max_kv = reach if max_kv is None else int(max_kv)
+    nbytes = _attention_workspace((*sizes, max_q, max_kv))
     if out is None:
-        out = torch.empty((tokens, heads, d), dtype=torch.float32, device=q.device)
-    else:
-        _require(out, "out", 3)
-        if out.shape != q.shape:
-            raise ValueError(f"out must have shape {tuple(q.shape)}, got {tuple(out.shape)}")
-    _same_device(q, ("k_cache", k_cache), ("table", table), ("kv_lens", kv_lens), ("q_starts", q_starts), ("out", out))
-    max_q, max_kv = int(max_q), int(max_kv)
-    seq = _Sequences(_ptr(q_starts), kv_lens.data_ptr(), table.data_ptr(), table.shape[1], tokens, batch,
-                     table.shape[1], max_q, max_kv, int(bool(causal)), int(window),
-                     1.0 / math.sqrt(d) if scale is None else float(scale))
-    nbytes = _attention_workspace((d, heads, kv_heads, _is_bf16(k_cache), batch, max_q, max_kv))
+        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
     keep = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
-    _launch(q, _library().pam_paged_attention, d, _ref(_heads(q)), _ref(_cache(k_cache)), _ref(_cache(v_cache)),
-            ctypes.byref(seq), _ref(_heads(out)), _ptr(keep), nbytes)
+    _launch(q, (_bound or _library()).pam_paged_attention, _attention_ptrs(
+        _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(q_starts), _ptr(kv_lens), _ptr(table), _ptr(keep))
+        + tail + _attention_end(max_q, max_kv, nbytes))
     del keep
     return out

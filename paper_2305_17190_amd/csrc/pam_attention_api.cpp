@@ -29,41 +29,41 @@ pam_status_t invalid(const char *name, const char *why) {
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 constexpr int64_t kMaxRows = 0x7FFFFFFF;         // rows of a head launch, slots of a cache
-constexpr int64_t kMaxStride = (int64_t)1 << 48; // sums of strided offsets stay inside int64
+constexpr int64_t kMaxStride = (int64_t)1 << 31; // times a count below 2^31: offsets stay inside int64
 constexpr int64_t kMaxLaunchGroups = 16777215;   // workgroups of 256 threads: below 2^32 threads
 
 bool is_bf16(pam_type_t t) { return t == PAM_TYPE_BF16; }
 
-pam_status_t check_heads(const pam_heads_t &h, const char *name, int64_t tokens, bool must_have_data = true) {
+pam_status_t check_heads(const void *data, const pam_heads_t &h, const char *name, int64_t tokens) {
     if (h.type != PAM_TYPE_F32 && h.type != PAM_TYPE_BF16)
         return invalid(name, ": type must be PAM_TYPE_F32 or PAM_TYPE_BF16");
     if (h.heads < 1)
         return invalid(name, ": heads must be at least 1");
     if (h.stride_token < 0 || h.stride_head < 0 || h.stride_token > kMaxStride || h.stride_head > kMaxStride)
-        return invalid(name, ": strides must be in [0, 2^48]");
-    if (must_have_data && tokens > 0 && h.data == nullptr)
+        return invalid(name, ": strides must be in [0, 2^31]");
+    if (tokens > 0 && data == nullptr)
         return invalid(name, ": data is NULL");
     return PAM_SUCCESS;
 }
 
 // A written operand: its rows may not share memory.
-pam_status_t check_written(const pam_heads_t &h, const char *name, int64_t tokens, int32_t d) {
+pam_status_t check_written(const void *data, const pam_heads_t &h, const char *name, int64_t tokens, int32_t d) {
     if ((tokens > 1 && h.stride_token < d) || (h.heads > 1 && h.stride_head < d))
         return invalid(name, ": rows of a written operand overlap");
-    return check_heads(h, name, tokens);
+    return check_heads(data, h, name, tokens);
 }
 
-pam_status_t check_cache(const pam_cache_t &c, const char *name, bool must_have_data) {
+pam_status_t check_cache(const void *data, const pam_cache_t &c, const char *name, bool must_have_data) {
     if (c.type != PAM_TYPE_F32 && c.type != PAM_TYPE_BF16)
         return invalid(name, ": type must be PAM_TYPE_F32 or PAM_TYPE_BF16");
     if (c.heads < 1 || c.page_size < 1 || c.pages < 0)
         return invalid(name, ": heads and page_size must be at least 1, pages at least 0");
     if (c.pages > kMaxRows / c.page_size)
         return invalid(name, ": pages * page_size must be below 2^31");
-    if (c.stride_page < 0 || c.stride_slot < 0 || c.stride_head < 0 || c.stride_page > kMaxStride / (c.pages + 1) ||
+    if (c.stride_page < 0 || c.stride_slot < 0 || c.stride_head < 0 || c.stride_page > kMaxStride ||
         c.stride_slot > kMaxStride || c.stride_head > kMaxStride)
         return invalid(name, ": stride out of range");
-    if (must_have_data && c.pages > 0 && c.data == nullptr)
+    if (must_have_data && c.pages > 0 && data == nullptr)
         return invalid(name, ": data is NULL");
     return PAM_SUCCESS;
 }
@@ -78,33 +78,28 @@ pam_status_t check_dim(int64_t tokens, int32_t d, float eps) {
     return PAM_SUCCESS;
 }
 
-pam_status_t check_rotation(const pam_rotation_t *r, int64_t tokens, int32_t d) {
-    if (r == nullptr)
-        return PAM_SUCCESS;
-    if (r->rot < 0 || r->rot > d || r->rot % 2 != 0)
+template <typename A> pam_status_t check_rotation(const A &a) {
+    const pam_rotation_t &r = a.rotation;
+    if (r.rot < 0 || r.rot > a.d || r.rot % 2 != 0)
         return invalid("rot must be even and in [0, d]");
-    if (r->rows < 0 || r->rows > kMaxRows)
+    if (r.rows < 0 || r.rows > kMaxRows)
         return invalid("the rotation's rows must be in [0, 2^31)");
-    if (tokens > 0 && (r->positions == nullptr || (r->rows > 0 && r->rot > 0 && (r->cos == nullptr || r->sin == nullptr))))
+    if (a.tokens > 0 && r.rot > 0 && (a.positions == nullptr || (r.rows > 0 && (a.cos == nullptr || a.sin == nullptr))))
         return invalid("positions, cos and sin must be non-NULL");
     return PAM_SUCCESS;
 }
 
-template <typename P> void set_rotation(P &p, const pam_rotation_t *r) {
-    if (r == nullptr || r->rot == 0) {
-        p.rot = 0;
-        p.interleaved = 0;
-        p.positions = nullptr;
-        p.cos = p.sin = nullptr;
-        p.rows = 0;
-        return;
-    }
-    p.rot = r->rot;
-    p.interleaved = r->interleaved != 0;
-    p.positions = r->positions;
-    p.cos = r->cos;
-    p.sin = r->sin;
-    p.rows = r->rows;
+template <typename P, typename A> void set_common(P &p, const A &a) {
+    const bool turns = a.rotation.rot > 0;
+    p.tokens = a.tokens;
+    p.d = a.d;
+    p.eps = a.eps;
+    p.rot = a.rotation.rot;
+    p.interleaved = turns && a.rotation.interleaved != 0;
+    p.positions = turns ? a.positions : nullptr;
+    p.cos = turns ? a.cos : nullptr;
+    p.sin = turns ? a.sin : nullptr;
+    p.rows = turns ? a.rotation.rows : 0;
 }
 
 pam_status_t check_rows(int64_t tokens, int64_t heads) {
@@ -113,10 +108,11 @@ pam_status_t check_rows(int64_t tokens, int64_t heads) {
     return PAM_SUCCESS;
 }
 
-void add_part(pamk::HeadRowsParams &p, const pam_heads_t &in, const float *weight, bool rotate) {
+pamk::HeadPart &add_part(pamk::HeadRowsParams &p, const void *data, const pam_heads_t &in, const float *weight,
+                         bool rotate) {
     pamk::HeadPart &part = p.part[p.parts++];
     part = pamk::HeadPart{};
-    part.in = in.data;
+    part.in = data;
     part.weight = weight;
     part.in_token = in.stride_token;
     part.in_head = in.stride_head;
@@ -124,17 +120,18 @@ void add_part(pamk::HeadRowsParams &p, const pam_heads_t &in, const float *weigh
     part.heads = in.heads;
     part.rotate = rotate;
     p.heads += in.heads;
+    return part;
 }
 
-void to_heads(pamk::HeadPart &part, const pam_heads_t &out) {
-    part.out = out.data;
+void to_heads(pamk::HeadPart &part, void *data, const pam_heads_t &out) {
+    part.out = data;
     part.out_token = out.stride_token;
     part.out_head = out.stride_head;
     part.out_bf16 = is_bf16(out.type);
 }
 
-void to_cache(pamk::HeadPart &part, const pam_cache_t &c) {
-    part.out = c.data;
+void to_cache(pamk::HeadPart &part, void *data, const pam_cache_t &c) {
+    part.out = data;
     part.out_token = c.stride_page;
     part.out_slot = c.stride_slot;
     part.out_head = c.stride_head;
@@ -238,41 +235,40 @@ pam_status_t check_attention_sizes(int32_t d, int32_t q_heads, int32_t kv_heads,
 
 extern "C" {
 
-pam_status_t pam_norm_rope(int64_t tokens, int32_t d, const pam_heads_t *q_in, const float *q_weight,
-                           const pam_heads_t *q_out, const pam_heads_t *k_in, const float *k_weight,
-                           const pam_heads_t *k_out, float eps, const pam_rotation_t *rotation, hipStream_t stream) {
-    PAM_TRY(check_dim(tokens, d, eps));
-    if ((q_in == nullptr) != (q_out == nullptr) || (k_in == nullptr) != (k_out == nullptr))
+pam_status_t pam_norm_rope(const pam_norm_rope_t *args, hipStream_t stream) {
+    if (args == nullptr)
+        return invalid("args is NULL");
+    const pam_norm_rope_t &a = *args;
+    PAM_TRY(check_dim(a.tokens, a.d, a.eps));
+    const bool has_q = a.q_in_heads.heads != 0, has_k = a.k_in_heads.heads != 0;
+    if (has_q != (a.q_out_heads.heads != 0) || has_k != (a.k_out_heads.heads != 0))
         return invalid("in and out must be given together");
-    if (q_in == nullptr && k_in == nullptr)
+    if (!has_q && !has_k)
         return invalid("neither queries nor keys given");
-    if (q_in != nullptr && k_in != nullptr && q_in->type != k_in->type)
+    if (has_q && has_k && a.q_in_heads.type != a.k_in_heads.type)
         return invalid("q_in and k_in must have one type");
     pamk::HeadRowsParams p{};
-    const pam_heads_t *in[] = {q_in, k_in}, *out[] = {q_out, k_out};
-    const float *weight[] = {q_weight, k_weight};
-    const char *in_name[] = {"q_in", "k_in"}, *out_name[] = {"q_out", "k_out"};
-    for (int i = 0; i < 2; ++i) {
-        if (in[i] == nullptr)
-            continue;
-        PAM_TRY(check_heads(*in[i], in_name[i], tokens));
-        PAM_TRY(check_written(*out[i], out_name[i], tokens, d));
-        if (in[i]->heads != out[i]->heads)
-            return invalid(out_name[i], ": another count of heads than the input");
-        add_part(p, *in[i], weight[i], rotation != nullptr);
-        to_heads(p.part[p.parts - 1], *out[i]);
+    if (has_q) {
+        PAM_TRY(check_heads(a.q_in, a.q_in_heads, "q_in", a.tokens));
+        PAM_TRY(check_written(a.q_out, a.q_out_heads, "q_out", a.tokens, a.d));
+        if (a.q_in_heads.heads != a.q_out_heads.heads)
+            return invalid("q_out: another count of heads than the input");
+        to_heads(add_part(p, a.q_in, a.q_in_heads, a.q_weight, true), a.q_out, a.q_out_heads);
     }
-    PAM_TRY(check_rotation(rotation, tokens, d));
-    PAM_TRY(check_rows(tokens, p.heads));
-    if (tokens == 0)
+    if (has_k) {
+        PAM_TRY(check_heads(a.k_in, a.k_in_heads, "k_in", a.tokens));
+        PAM_TRY(check_written(a.k_out, a.k_out_heads, "k_out", a.tokens, a.d));
+        if (a.k_in_heads.heads != a.k_out_heads.heads)
+            return invalid("k_out: another count of heads than the input");
+        to_heads(add_part(p, a.k_in, a.k_in_heads, a.k_weight, true), a.k_out, a.k_out_heads);
+    }
+    PAM_TRY(check_rotation(a));
+    PAM_TRY(check_rows(a.tokens, p.heads));
+    if (a.tokens == 0)
         return PAM_SUCCESS;
     PAM_TRY(api_check_device());
-    p.tokens = tokens;
-    p.d = d;
-    p.eps = eps;
-    set_rotation(p, rotation);
-    const bool bf16 = is_bf16(q_in != nullptr ? q_in->type : k_in->type);
-    const hipError_t e = pamk::launch_head_rows(bf16, p, stream);
+    set_common(p, a);
+    const hipError_t e = pamk::launch_head_rows(is_bf16(has_q ? a.q_in_heads.type : a.k_in_heads.type), p, stream);
     return e == hipSuccess ? PAM_SUCCESS : api_fail_hip(e, "pam_norm_rope kernel launch");
 }
 
@@ -291,131 +287,128 @@ pam_status_t pam_norm_rope_grad_workspace_size(int64_t tokens, int32_t d, int32_
     return PAM_SUCCESS;
 }
 
-pam_status_t pam_norm_rope_grad(int64_t tokens, int32_t d, const pam_heads_t *q_in, const float *q_weight,
-                                const pam_heads_t *dq_out, const pam_heads_t *dq_in, float *dq_weight,
-                                const pam_heads_t *k_in, const float *k_weight, const pam_heads_t *dk_out,
-                                const pam_heads_t *dk_in, float *dk_weight, float eps,
-                                const pam_rotation_t *rotation, void *workspace, size_t workspace_bytes,
-                                hipStream_t stream) {
-    PAM_TRY(check_dim(tokens, d, eps));
-    if (q_in == nullptr && k_in == nullptr)
+pam_status_t pam_norm_rope_grad(const pam_norm_rope_grad_t *args, hipStream_t stream) {
+    if (args == nullptr)
+        return invalid("args is NULL");
+    const pam_norm_rope_grad_t &a = *args;
+    PAM_TRY(check_dim(a.tokens, a.d, a.eps));
+    struct Side {
+        const void *x, *dz;
+        void *dx;
+        const pam_heads_t &x_heads, &dz_heads, &dx_heads;
+        const float *weight;
+        float *dweight;
+        const char *names[3];
+    };
+    const Side sides[] = {{a.q_in, a.dq_out, a.dq_in, a.q_in_heads, a.dq_out_heads, a.dq_in_heads, a.q_weight,
+                           a.dq_weight, {"q_in", "dq_out", "dq_in"}},
+                          {a.k_in, a.dk_out, a.dk_in, a.k_in_heads, a.dk_out_heads, a.dk_in_heads, a.k_weight,
+                           a.dk_weight, {"k_in", "dk_out", "dk_in"}}};
+    if (a.q_in_heads.heads == 0 && a.k_in_heads.heads == 0)
         return invalid("neither queries nor keys given");
-    const pam_heads_t *x[] = {q_in, k_in}, *dz[] = {dq_out, dk_out}, *dx[] = {dq_in, dk_in};
-    const float *weight[] = {q_weight, k_weight};
-    float *dweight[] = {dq_weight, dk_weight};
-    const char *names[][3] = {{"q_in", "dq_out", "dq_in"}, {"k_in", "dk_out", "dk_in"}};
     pamk::HeadGradParams p{};
-    pam_type_t type = q_in != nullptr ? q_in->type : k_in->type;
+    const pam_type_t type = a.q_in_heads.heads != 0 ? a.q_in_heads.type : a.k_in_heads.type;
     bool weights = false;
     int64_t rows[2] = {0, 0};
     for (int i = 0; i < 2; ++i) {
-        if ((x[i] == nullptr) != (dz[i] == nullptr) || (x[i] == nullptr) != (dx[i] == nullptr))
+        const Side &s = sides[i];
+        const bool given = s.x_heads.heads != 0;
+        if (given != (s.dz_heads.heads != 0) || given != (s.dx_heads.heads != 0))
             return invalid("an input and its two gradients must be given together");
-        if ((weight[i] == nullptr) != (dweight[i] == nullptr))
+        if ((s.weight == nullptr) != (s.dweight == nullptr))
             return invalid("a weight and its gradient must be given together");
-        if (x[i] == nullptr) {
-            if (weight[i] != nullptr)
+        if (!given) {
+            if (s.weight != nullptr)
                 return invalid("a weight without its input");
             continue;
         }
-        PAM_TRY(check_heads(*x[i], names[i][0], tokens));
-        PAM_TRY(check_heads(*dz[i], names[i][1], tokens));
-        PAM_TRY(check_written(*dx[i], names[i][2], tokens, d));
-        if (x[i]->heads != dz[i]->heads || x[i]->heads != dx[i]->heads)
-            return invalid(names[i][0], ": another count of heads than its gradients");
-        if (x[i]->type != type || dz[i]->type != type || dx[i]->type != type)
+        PAM_TRY(check_heads(s.x, s.x_heads, s.names[0], a.tokens));
+        PAM_TRY(check_heads(s.dz, s.dz_heads, s.names[1], a.tokens));
+        PAM_TRY(check_written(s.dx, s.dx_heads, s.names[2], a.tokens, a.d));
+        if (s.x_heads.heads != s.dz_heads.heads || s.x_heads.heads != s.dx_heads.heads)
+            return invalid(s.names[0], ": another count of heads than its gradients");
+        if (s.x_heads.type != type || s.dz_heads.type != type || s.dx_heads.type != type)
             return invalid("inputs and gradients must have one type");
         pamk::HeadGradPart &part = p.part[i];
-        part.x = x[i]->data;
-        part.dz = dz[i]->data;
-        part.dx = dx[i]->data;
-        part.weight = weight[i];
-        part.dweight = dweight[i];
-        part.x_token = x[i]->stride_token;
-        part.x_head = x[i]->stride_head;
-        part.dz_token = dz[i]->stride_token;
-        part.dz_head = dz[i]->stride_head;
-        part.dx_token = dx[i]->stride_token;
-        part.dx_head = dx[i]->stride_head;
-        part.heads = x[i]->heads;
-        rows[i] = tokens * x[i]->heads;
-        weights = weights || weight[i] != nullptr;
+        part.x = s.x;
+        part.dz = s.dz;
+        part.dx = s.dx;
+        part.weight = s.weight;
+        part.dweight = s.dweight;
+        part.x_token = s.x_heads.stride_token;
+        part.x_head = s.x_heads.stride_head;
+        part.dz_token = s.dz_heads.stride_token;
+        part.dz_head = s.dz_heads.stride_head;
+        part.dx_token = s.dx_heads.stride_token;
+        part.dx_head = s.dx_heads.stride_head;
+        part.heads = s.x_heads.heads;
+        rows[i] = a.tokens * s.x_heads.heads;
+        weights = weights || s.weight != nullptr;
     }
-    PAM_TRY(check_rotation(rotation, tokens, d));
-    PAM_TRY(check_rows(tokens, (int64_t)p.part[0].heads + p.part[1].heads));
-    if (tokens == 0 && !weights)
+    PAM_TRY(check_rotation(a));
+    PAM_TRY(check_rows(a.tokens, (int64_t)p.part[0].heads + p.part[1].heads));
+    if (a.tokens == 0 && !weights)
         return PAM_SUCCESS;
-    p.tokens = tokens;
-    p.d = d;
-    p.eps = eps;
-    set_rotation(p, rotation);
-    const bool bf16 = is_bf16(type);
+    set_common(p, a);
     int most[2];
     grad_budget(rows[0], rows[1], most);
     for (int i = 0; i < 2; ++i)
-        p.part[i].groups = pamk::head_grad_groups(bf16, rows[i], d, p.rot, most[i]);
-    if (weights && tokens > 0) {
-        const size_t need = (size_t)((int64_t)(p.part[0].groups + p.part[1].groups) * d) * sizeof(float);
-        if (workspace == nullptr || workspace_bytes < need)
+        p.part[i].groups = pamk::head_grad_groups(is_bf16(type), rows[i], a.d, p.rot, most[i]);
+    if (weights && a.tokens > 0) {
+        const int64_t need = (int64_t)(p.part[0].groups + p.part[1].groups) * a.d * (int64_t)sizeof(float);
+        if (a.workspace == nullptr || a.workspace_bytes < need)
             return invalid("workspace is NULL or smaller than pam_norm_rope_grad_workspace_size says");
-        if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0)
+        if ((reinterpret_cast<uintptr_t>(a.workspace) & 15u) != 0)
             return invalid("workspace must be 16-byte aligned");
-        p.part[0].partial = static_cast<float *>(workspace);
-        p.part[1].partial = p.part[0].partial + (int64_t)p.part[0].groups * d;
+        p.part[0].partial = static_cast<float *>(a.workspace);
+        p.part[1].partial = p.part[0].partial + (int64_t)p.part[0].groups * a.d;
     }
     PAM_TRY(api_check_device());
-    const hipError_t e = pamk::launch_head_grad(bf16, p, stream);
+    const hipError_t e = pamk::launch_head_grad(is_bf16(type), p, stream);
     return e == hipSuccess ? PAM_SUCCESS : api_fail_hip(e, "pam_norm_rope_grad kernel launch");
 }
 
-pam_status_t pam_append_kv(int64_t tokens, int32_t d, const pam_heads_t *k, const float *k_weight,
-                           const pam_heads_t *v, const pam_heads_t *q_in, const float *q_weight,
-                           const pam_heads_t *q_out, float eps, const pam_rotation_t *rotation,
-                           const pam_cache_t *k_cache, const pam_cache_t *v_cache, const int64_t *slots,
-                           hipStream_t stream) {
-    PAM_TRY(check_dim(tokens, d, eps));
-    if (k == nullptr || v == nullptr || k_cache == nullptr || v_cache == nullptr)
-        return invalid("k, v, k_cache and v_cache must be non-NULL");
-    if ((q_in == nullptr) != (q_out == nullptr))
+pam_status_t pam_append_kv(const pam_append_kv_t *args, hipStream_t stream) {
+    if (args == nullptr)
+        return invalid("args is NULL");
+    const pam_append_kv_t &a = *args;
+    PAM_TRY(check_dim(a.tokens, a.d, a.eps));
+    const bool has_q = a.q_in_heads.heads != 0;
+    if (has_q != (a.q_out_heads.heads != 0))
         return invalid("q_in and q_out must be given together");
-    PAM_TRY(check_heads(*k, "k", tokens));
-    PAM_TRY(check_heads(*v, "v", tokens));
-    PAM_TRY(check_cache(*k_cache, "k_cache", tokens > 0));
-    PAM_TRY(check_cache(*v_cache, "v_cache", tokens > 0));
-    if (k->type != v->type || (q_in != nullptr && q_in->type != k->type))
+    const pam_cache_t &kc = a.k_cache_layout, &vc = a.v_cache_layout;
+    PAM_TRY(check_heads(a.k, a.k_heads, "k", a.tokens));
+    PAM_TRY(check_heads(a.v, a.v_heads, "v", a.tokens));
+    PAM_TRY(check_cache(a.k_cache, kc, "k_cache", a.tokens > 0));
+    PAM_TRY(check_cache(a.v_cache, vc, "v_cache", a.tokens > 0));
+    if (a.k_heads.type != a.v_heads.type || (has_q && a.q_in_heads.type != a.k_heads.type))
         return invalid("k, v and q_in must have one type");
-    if (k->heads != k_cache->heads || v->heads != v_cache->heads || k->heads != v->heads)
+    if (a.k_heads.heads != kc.heads || a.v_heads.heads != vc.heads || a.k_heads.heads != a.v_heads.heads)
         return invalid("k, v and the caches must have one count of heads");
-    if (k_cache->pages != v_cache->pages || k_cache->page_size != v_cache->page_size)
+    if (kc.pages != vc.pages || kc.page_size != vc.page_size)
         return invalid("the caches must have one count and size of pages");
-    PAM_TRY(check_rotation(rotation, tokens, d));
+    PAM_TRY(check_rotation(a));
     pamk::HeadRowsParams p{};
-    add_part(p, *k, k_weight, rotation != nullptr);
-    to_cache(p.part[0], *k_cache);
-    add_part(p, *v, nullptr, false);
-    to_cache(p.part[1], *v_cache);
-    if (q_in != nullptr) {
-        PAM_TRY(check_heads(*q_in, "q_in", tokens));
-        PAM_TRY(check_written(*q_out, "q_out", tokens, d));
-        if (q_in->heads != q_out->heads)
+    to_cache(add_part(p, a.k, a.k_heads, a.k_weight, true), a.k_cache, kc);
+    to_cache(add_part(p, a.v, a.v_heads, nullptr, false), a.v_cache, vc);
+    if (has_q) {
+        PAM_TRY(check_heads(a.q_in, a.q_in_heads, "q_in", a.tokens));
+        PAM_TRY(check_written(a.q_out, a.q_out_heads, "q_out", a.tokens, a.d));
+        if (a.q_in_heads.heads != a.q_out_heads.heads)
             return invalid("q_out: another count of heads than the input");
-        add_part(p, *q_in, q_weight, rotation != nullptr);
-        to_heads(p.part[2], *q_out);
+        to_heads(add_part(p, a.q_in, a.q_in_heads, a.q_weight, true), a.q_out, a.q_out_heads);
     }
-    PAM_TRY(check_rows(tokens, p.heads));
-    if (tokens > 0 && slots == nullptr)
+    PAM_TRY(check_rows(a.tokens, p.heads));
+    if (a.tokens > 0 && a.slots == nullptr)
         return invalid("slots is NULL");
-    if (tokens == 0)
+    if (a.tokens == 0)
         return PAM_SUCCESS;
     PAM_TRY(api_check_device());
-    p.tokens = tokens;
-    p.d = d;
-    p.eps = eps;
-    set_rotation(p, rotation);
-    p.slots = slots;
-    p.page_size = k_cache->page_size;
-    p.cache_slots = k_cache->pages * k_cache->page_size;
-    const hipError_t e = pamk::launch_head_rows(is_bf16(k->type), p, stream);
+    set_common(p, a);
+    p.slots = a.slots;
+    p.page_size = kc.page_size;
+    p.cache_slots = kc.pages * kc.page_size;
+    const hipError_t e = pamk::launch_head_rows(is_bf16(a.k_heads.type), p, stream);
     return e == hipSuccess ? PAM_SUCCESS : api_fail_hip(e, "pam_append_kv kernel launch");
 }
 
@@ -430,63 +423,62 @@ pam_status_t pam_paged_attention_workspace_size(int32_t d, int32_t q_heads, int3
     return PAM_SUCCESS;
 }
 
-pam_status_t pam_paged_attention(int32_t d, const pam_heads_t *q, const pam_cache_t *k_cache,
-                                 const pam_cache_t *v_cache, const pam_sequences_t *sequences,
-                                 const pam_heads_t *out, void *workspace, size_t workspace_bytes,
-                                 hipStream_t stream) {
-    if (q == nullptr || k_cache == nullptr || v_cache == nullptr || sequences == nullptr || out == nullptr)
-        return invalid("q, k_cache, v_cache, sequences and out must be non-NULL");
-    const pam_sequences_t &s = *sequences;
+pam_status_t pam_paged_attention(const pam_paged_attention_t *args, hipStream_t stream) {
+    if (args == nullptr)
+        return invalid("args is NULL");
+    const pam_paged_attention_t &s = *args;
+    const pam_cache_t &kc = s.k_cache_layout, &vc = s.v_cache_layout;
     if (s.tokens < 0)
         return invalid("tokens must be >= 0");
-    PAM_TRY(check_attention_sizes(d, q->heads, k_cache->heads, s.batch, s.max_q, s.max_kv));
-    PAM_TRY(check_heads(*q, "q", s.tokens));
-    PAM_TRY(check_written(*out, "out", s.tokens, d));
-    if (out->type != PAM_TYPE_F32)
+    PAM_TRY(check_attention_sizes(s.d, s.q_heads.heads, kc.heads, s.batch, s.max_q, s.max_kv));
+    PAM_TRY(check_heads(s.q, s.q_heads, "q", s.tokens));
+    PAM_TRY(check_written(s.out, s.out_heads, "out", s.tokens, s.d));
+    if (s.out_heads.type != PAM_TYPE_F32)
         return invalid("out: must be PAM_TYPE_F32");
-    if (out->heads != q->heads)
+    if (s.out_heads.heads != s.q_heads.heads)
         return invalid("out: another count of heads than q");
-    PAM_TRY(check_cache(*k_cache, "k_cache", true));
-    PAM_TRY(check_cache(*v_cache, "v_cache", true));
-    if (k_cache->type != v_cache->type || k_cache->heads != v_cache->heads || k_cache->pages != v_cache->pages ||
-        k_cache->page_size != v_cache->page_size)
+    PAM_TRY(check_cache(s.k_cache, kc, "k_cache", true));
+    PAM_TRY(check_cache(s.v_cache, vc, "v_cache", true));
+    if (kc.type != vc.type || kc.heads != vc.heads || kc.pages != vc.pages || kc.page_size != vc.page_size)
         return invalid("the caches must agree in type, heads, pages and page_size");
     if (s.table_width < 0 || s.table_stride < s.table_width || s.table_stride > kMaxStride)
         return invalid("table_stride must be at least table_width, which must be >= 0");
-    if (s.max_kv > (int64_t)s.table_width * k_cache->page_size)
+    if (s.max_kv > (int64_t)s.table_width * kc.page_size)
         return invalid("max_kv must be at most table_width * page_size");
     if (s.q_starts == nullptr && s.tokens < s.batch)
         return invalid("without q_starts there must be one token a sequence");
+    if (s.window < 0)
+        return invalid("window must be >= 0");
     if (!std::isfinite(s.scale))
         return invalid("scale must be finite");
     if (s.batch == 0 || s.tokens == 0 || s.max_q == 0)
         return PAM_SUCCESS;
     if (s.kv_lens == nullptr || (s.max_kv > 0 && s.table == nullptr))
         return invalid("kv_lens and table must be non-NULL");
-    const bool bf16 = is_bf16(k_cache->type);
-    const AttentionPlan plan = attention_plan(d, q->heads, k_cache->heads, bf16, s.batch, s.max_q, s.max_kv);
+    const bool bf16 = is_bf16(kc.type);
+    const AttentionPlan plan = attention_plan(s.d, s.q_heads.heads, kc.heads, bf16, s.batch, s.max_q, s.max_kv);
     const int64_t most_groups = plan.form == Form::tiles ? plan.slab * plan.splits * std::max(plan.split_keys / 128, 2)
                                                          : plan.units * plan.splits;
     if (plan.units > kMaxLaunchGroups || most_groups > kMaxLaunchGroups)
         return invalid("too many workgroups (batch * heads * rows * keys too large)");
     if (plan.bytes() > 0) {
-        if (workspace == nullptr || workspace_bytes < plan.bytes())
+        if (s.workspace == nullptr || s.workspace_bytes < 0 || (size_t)s.workspace_bytes < plan.bytes())
             return invalid("workspace is NULL or smaller than pam_paged_attention_workspace_size says");
-        if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0)
+        if ((reinterpret_cast<uintptr_t>(s.workspace) & 15u) != 0)
             return invalid("workspace must be 16-byte aligned");
     }
     PAM_TRY(api_check_device());
 
     pamk::AttentionParams p{};
-    p.q = q->data;
-    p.q_token = q->stride_token;
-    p.q_head = q->stride_head;
-    p.q_bf16 = is_bf16(q->type);
-    p.k = {k_cache->data, k_cache->stride_page, k_cache->stride_slot, k_cache->stride_head, k_cache->pages};
-    p.v = {v_cache->data, v_cache->stride_page, v_cache->stride_slot, v_cache->stride_head, v_cache->pages};
+    p.q = s.q;
+    p.q_token = s.q_heads.stride_token;
+    p.q_head = s.q_heads.stride_head;
+    p.q_bf16 = is_bf16(s.q_heads.type);
+    p.k = {s.k_cache, kc.stride_page, kc.stride_slot, kc.stride_head, kc.pages};
+    p.v = {s.v_cache, vc.stride_page, vc.stride_slot, vc.stride_head, vc.pages};
     // key / page_size for key < 2^31 by a multiplication: with 2^l >= size,
     // mul = 2^32 (2^l - size) / size + 1, (mulhi(key, mul) + key) >> l.
-    p.page_size = (uint32_t)k_cache->page_size;
+    p.page_size = (uint32_t)kc.page_size;
     while (((uint64_t)1 << p.page_shift) < p.page_size)
         ++p.page_shift;
     p.page_mul = (uint32_t)(((((uint64_t)1 << p.page_shift) - p.page_size) << 32) / p.page_size + 1);
@@ -494,14 +486,14 @@ pam_status_t pam_paged_attention(int32_t d, const pam_heads_t *q, const pam_cach
     p.kv_lens = s.kv_lens;
     p.table = s.table;
     p.table_stride = s.table_stride;
-    p.out = static_cast<float *>(out->data);
-    p.out_token = out->stride_token;
-    p.out_head = out->stride_head;
+    p.out = s.out;
+    p.out_token = s.out_heads.stride_token;
+    p.out_head = s.out_heads.stride_head;
     p.tokens = s.tokens;
     p.batch = s.batch;
-    p.kv_heads = k_cache->heads;
-    p.group = q->heads / k_cache->heads;
-    p.d = d;
+    p.kv_heads = kc.heads;
+    p.group = s.q_heads.heads / kc.heads;
+    p.d = s.d;
     p.max_q = s.q_starts == nullptr ? 1 : s.max_q;
     p.max_kv = s.max_kv;
     p.causal = s.causal;
@@ -511,9 +503,9 @@ pam_status_t pam_paged_attention(int32_t d, const pam_heads_t *q, const pam_cach
     p.row_blocks = plan.row_blocks;
     p.splits = plan.splits;
     p.split_keys = plan.split_keys;
-    p.scores = static_cast<float *>(workspace);
-    p.stats = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.scores);
-    p.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.scores + plan.stats);
+    p.scores = static_cast<float *>(s.workspace);
+    p.stats = reinterpret_cast<float *>(static_cast<char *>(s.workspace) + plan.scores);
+    p.partial = reinterpret_cast<float *>(static_cast<char *>(s.workspace) + plan.scores + plan.stats);
 
     if (plan.partial == 0)
         p.partial = nullptr;

@@ -21,20 +21,45 @@ def lib():
     return att._library()
 
 
-def heads(data=P, token=512, head=64, count=8, kind=0):
-    return att._Heads(data, token, head, count, kind)
+class Heads(ctypes.Structure):
+    _fields_ = [("stride_token", ctypes.c_int64), ("stride_head", ctypes.c_int64), ("heads", ctypes.c_int32),
+                ("type", ctypes.c_int32)]
 
 
-def cache(data=P, page=8192, slot=512, head=64, pages=10, size=16, count=8, kind=0):
-    return att._Cache(data, page, slot, head, pages, size, count, kind)
+class Rotation(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("rot", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
 
-def rotation(positions=P, cos=P, sin=P, rows=100, rot=64, interleaved=0):
-    return att._Rotation(positions, cos, sin, rows, rot, interleaved)
+class Cache(ctypes.Structure):
+    _fields_ = [("stride_page", ctypes.c_int64), ("stride_slot", ctypes.c_int64), ("stride_head", ctypes.c_int64),
+                ("pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
-def ref(x):
-    return None if x is None else ctypes.byref(x)
+def heads(token=512, head=64, count=8, kind=0):
+    return Heads(token, head, count, kind)
+
+
+def cache(page=8192, slot=512, head=64, pages=10, size=16, count=8, kind=0):
+    return Cache(page, slot, head, pages, size, count, kind, 0)
+
+
+def rotation(rows=100, rot=64, interleaved=0):
+    return Rotation(rows, rot, interleaved)
+
+
+NONE = heads(0, 0, 0, 0)
+
+
+def call(lib, name, pointers, layouts, **changes):
+    """The entry point `name` on a structure of `pointers` (names, all valid)
+    and then `layouts` (name, C type, value), with some of them changed."""
+    fields = [(n, ctypes.c_void_p) for n in pointers] + [(n, t) for n, t, _ in layouts]
+    values = dict({n: P for n in pointers}, **{n: v for n, _, v in layouts})
+    assert set(changes) <= set(values), set(changes) - set(values)
+    values.update(changes)
+    args = type(name, (ctypes.Structure,), {"_fields_": fields})(*(values[n] for n, _ in fields))
+    return getattr(lib, name)(bytes(args), None)
 
 
 def test_every_declared_symbol_is_exported(lib):
@@ -46,53 +71,62 @@ def test_every_declared_symbol_is_exported(lib):
         assert hasattr(lib, name)
 
 
+I32, I64, F32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+
+
 def norm_rope(lib, **kw):
-    a = dict(tokens=4, d=64, q_in=heads(), qw=P, q_out=heads(), k_in=heads(), kw=P, k_out=heads(), eps=1e-6,
-             rot=rotation())
-    a.update(kw)
-    return lib.pam_norm_rope(a["tokens"], a["d"], ref(a["q_in"]), a["qw"], ref(a["q_out"]), ref(a["k_in"]), a["kw"],
-                             ref(a["k_out"]), a["eps"], ref(a["rot"]), None)
+    return call(lib, "pam_norm_rope", ["q_in", "q_out", "q_weight", "k_in", "k_out", "k_weight", "positions", "cos", "sin"],
+                [(n, Heads, heads()) for n in ("q_in_heads", "q_out_heads", "k_in_heads", "k_out_heads")]
+                + [("rotation", Rotation, rotation()), ("tokens", I64, 4), ("d", I32, 64), ("eps", F32, 1e-6)], **kw)
 
 
-BAD_HEADS = [heads(data=None), heads(count=0), heads(token=-1), heads(head=-5), heads(kind=2), heads(token=1 << 60)]
-BAD_ROTATIONS = [rotation(positions=None), rotation(cos=None), rotation(sin=None), rotation(rot=63), rotation(rot=66),
-                 rotation(rot=-2), rotation(rows=-1), rotation(rows=1 << 31)]
+BAD_HEADS = [heads(count=-1), heads(token=-1), heads(head=-5), heads(kind=2), heads(token=1 << 60)]
+BAD_ROTATIONS = [dict(positions=None), dict(cos=None), dict(sin=None)] + [
+    dict(rotation=r) for r in (rotation(rot=63), rotation(rot=66), rotation(rot=-2), rotation(rows=-1),
+                               rotation(rows=1 << 31))]
 
 
 @pytest.mark.parametrize("kw", [
     dict(tokens=-1), dict(d=63), dict(d=0), dict(d=258), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")),
-    dict(q_out=None), dict(k_in=None), dict(q_in=None, q_out=None, k_in=None, k_out=None),
-    dict(k_in=heads(kind=1)), dict(q_out=heads(count=4)), dict(q_out=heads(token=32)), dict(k_out=heads(head=63)),
-    dict(tokens=1 << 30)] + [dict(q_in=h) for h in BAD_HEADS] + [dict(k_out=h) for h in BAD_HEADS]
-    + [dict(rot=r) for r in BAD_ROTATIONS])
+    dict(q_out_heads=NONE), dict(k_in_heads=NONE), dict(q_in=None), dict(k_out=None),
+    dict(q_in_heads=NONE, q_out_heads=NONE, k_in_heads=NONE, k_out_heads=NONE), dict(k_in_heads=heads(kind=1)),
+    dict(q_out_heads=heads(count=4)), dict(q_out_heads=heads(token=32)), dict(k_out_heads=heads(head=63)),
+    dict(tokens=1 << 30)] + [dict(q_in_heads=h) for h in BAD_HEADS] + [dict(k_out_heads=h) for h in BAD_HEADS]
+    + BAD_ROTATIONS)
 def test_norm_rope_refuses(lib, kw):
     assert norm_rope(lib, **kw) == INVALID and lib.pam_last_error() != b""
 
 
+def test_no_arguments_are_refused(lib):
+    for name in ("pam_norm_rope", "pam_norm_rope_grad", "pam_append_kv", "pam_paged_attention"):
+        assert getattr(lib, name)(None, None) == INVALID
+
+
 def test_nothing_to_do_launches_nothing(lib):
-    none = heads(data=None)
-    assert norm_rope(lib, tokens=0, q_in=none, q_out=none, k_in=none, k_out=none, rot=rotation(None, None, None)) == 0
-    assert append(lib, tokens=0, k=none, v=none, k_cache=cache(data=None), v_cache=cache(data=None), slots=None,
-                  q_in=None, q_out=None, rot=None) == 0
+    assert norm_rope(lib, tokens=0, q_in=None, q_out=None, k_in=None, k_out=None, positions=None, cos=None, sin=None) == 0
+    assert append(lib, tokens=0, k=None, v=None, k_cache=None, v_cache=None, slots=None, q_in_heads=NONE,
+                  q_out_heads=NONE, rotation=rotation(rot=0)) == 0
     assert attention(lib, batch=0) == 0
-    assert attention(lib, tokens=0, q=none, out=none) == 0
-    assert grad(lib, tokens=0, qw=None, dqw=None, kw=None, dkw=None, workspace=None) == 0
+    assert attention(lib, tokens=0, q=None, out=None) == 0
+    assert grad(lib, tokens=0, q_weight=None, dq_weight=None, k_weight=None, dk_weight=None, workspace=None) == 0
 
 
 def grad(lib, **kw):
-    a = dict(tokens=4, d=64, q=heads(), qw=P, dq=heads(), gq=heads(), dqw=P, k=heads(), kw=P, dk=heads(), gk=heads(),
-             dkw=P, eps=1e-6, rot=rotation(), workspace=P, bytes=1 << 30)
-    a.update(kw)
-    return lib.pam_norm_rope_grad(a["tokens"], a["d"], ref(a["q"]), a["qw"], ref(a["dq"]), ref(a["gq"]), a["dqw"],
-                                  ref(a["k"]), a["kw"], ref(a["dk"]), ref(a["gk"]), a["dkw"], a["eps"], ref(a["rot"]),
-                                  a["workspace"], a["bytes"], None)
+    return call(lib, "pam_norm_rope_grad",
+                ["q_in", "q_weight", "dq_out", "dq_in", "dq_weight", "k_in", "k_weight", "dk_out", "dk_in", "dk_weight",
+                 "positions", "cos", "sin", "workspace"],
+                [(n + "_heads", Heads, heads()) for n in ("q_in", "dq_out", "dq_in", "k_in", "dk_out", "dk_in")]
+                + [("rotation", Rotation, rotation()), ("tokens", I64, 4), ("workspace_bytes", I64, 1 << 30),
+                   ("d", I32, 64), ("eps", F32, 1e-6)], **kw)
 
 
 @pytest.mark.parametrize("kw", [
-    dict(tokens=-1), dict(d=65), dict(eps=-1.0), dict(dq=None), dict(gk=None), dict(q=None), dict(qw=None), dict(dkw=None),
-    dict(q=None, dq=None, gq=None), dict(dq=heads(count=3)), dict(gq=heads(kind=1)), dict(dk=heads(kind=1)),
-    dict(gq=heads(token=8)), dict(workspace=None), dict(bytes=8), dict(workspace=P + 4)]
-    + [dict(dq=h) for h in BAD_HEADS] + [dict(rot=r) for r in BAD_ROTATIONS])
+    dict(tokens=-1), dict(d=65), dict(eps=-1.0), dict(dq_out_heads=NONE), dict(dk_in_heads=NONE), dict(q_in_heads=NONE),
+    dict(dq_out=None), dict(dk_in=None), dict(q_weight=None), dict(dk_weight=None),
+    dict(q_in_heads=NONE, dq_out_heads=NONE, dq_in_heads=NONE), dict(dq_out_heads=heads(count=3)),
+    dict(dq_in_heads=heads(kind=1)), dict(dk_out_heads=heads(kind=1)), dict(dq_in_heads=heads(token=8)),
+    dict(workspace=None), dict(workspace_bytes=8), dict(workspace_bytes=-1), dict(workspace=P + 4)]
+    + [dict(dq_out_heads=h) for h in BAD_HEADS] + BAD_ROTATIONS)
 def test_grad_refuses(lib, kw):
     assert grad(lib, **kw) == INVALID and lib.pam_last_error() != b""
 
@@ -112,48 +146,49 @@ def test_grad_workspace_sizes(lib):
 
 
 def append(lib, **kw):
-    a = dict(tokens=4, d=64, k=heads(), kw=P, v=heads(), q_in=heads(), qw=P, q_out=heads(), eps=1e-6, rot=rotation(),
-             k_cache=cache(), v_cache=cache(), slots=P)
-    a.update(kw)
-    return lib.pam_append_kv(a["tokens"], a["d"], ref(a["k"]), a["kw"], ref(a["v"]), ref(a["q_in"]), a["qw"],
-                             ref(a["q_out"]), a["eps"], ref(a["rot"]), ref(a["k_cache"]), ref(a["v_cache"]), a["slots"],
-                             None)
+    return call(lib, "pam_append_kv",
+                ["k", "k_weight", "v", "q_in", "q_weight", "q_out", "k_cache", "v_cache", "slots", "positions", "cos",
+                 "sin"],
+                [(n, Heads, heads()) for n in ("k_heads", "v_heads", "q_in_heads", "q_out_heads")]
+                + [("k_cache_layout", Cache, cache()), ("v_cache_layout", Cache, cache()),
+                   ("rotation", Rotation, rotation()), ("tokens", I64, 4), ("d", I32, 64), ("eps", F32, 1e-6)], **kw)
 
 
-BAD_CACHES = [cache(data=None), cache(page=-1), cache(slot=-1), cache(head=-1), cache(pages=-1), cache(size=0),
-              cache(count=0), cache(kind=7), cache(pages=1 << 27), cache(page=1 << 60)]
+BAD_CACHES = [cache(page=-1), cache(slot=-1), cache(head=-1), cache(pages=-1), cache(size=0), cache(count=0),
+              cache(kind=7), cache(pages=1 << 27), cache(page=1 << 60)]
 
 
 @pytest.mark.parametrize("kw", [
-    dict(tokens=-1), dict(d=7), dict(k=None), dict(v=None), dict(k_cache=None), dict(slots=None), dict(q_out=None),
-    dict(v=heads(kind=1)), dict(q_in=heads(kind=1)), dict(k=heads(count=4)), dict(v=heads(count=4)),
-    dict(v_cache=cache(pages=9)), dict(v_cache=cache(size=8)), dict(q_out=heads(count=2)), dict(q_out=heads(head=8))]
-    + [dict(k=h) for h in BAD_HEADS] + [dict(v_cache=c) for c in BAD_CACHES] + [dict(rot=r) for r in BAD_ROTATIONS])
+    dict(tokens=-1), dict(d=7), dict(k=None), dict(v=None), dict(k_cache=None), dict(v_cache=None), dict(slots=None),
+    dict(q_out_heads=NONE), dict(q_out=None), dict(v_heads=heads(kind=1)), dict(q_in_heads=heads(kind=1)),
+    dict(k_heads=heads(count=4)), dict(v_heads=heads(count=4)), dict(k_heads=NONE), dict(v_cache_layout=cache(pages=9)),
+    dict(v_cache_layout=cache(size=8)), dict(q_out_heads=heads(count=2)), dict(q_out_heads=heads(head=8))]
+    + [dict(k_heads=h) for h in BAD_HEADS] + [dict(v_cache_layout=c) for c in BAD_CACHES] + BAD_ROTATIONS)
 def test_append_refuses(lib, kw):
     assert append(lib, **kw) == INVALID and lib.pam_last_error() != b""
 
 
-def attention(lib, q=None, k_cache=None, v_cache=None, out=None, d=64, workspace=P, bytes=1 << 40, **kw):
-    s = dict(q_starts=P, kv_lens=P, table=P, table_stride=20, tokens=40, batch=4, table_width=20, max_q=10, max_kv=300,
-             causal=1, window=0, scale=0.125)
-    s.update(kw)
-    seq = att._Sequences(*(s[name] for name, _ in att._Sequences._fields_))
-    return lib.pam_paged_attention(d, ref(q or heads()), ref(k_cache or cache()), ref(v_cache or cache()), ref(seq),
-                                   ref(out or heads()), workspace, bytes, None)
+def attention(lib, **kw):
+    return call(lib, "pam_paged_attention",
+                ["q", "k_cache", "v_cache", "out", "q_starts", "kv_lens", "table", "workspace"],
+                [("q_heads", Heads, heads()), ("out_heads", Heads, heads()), ("k_cache_layout", Cache, cache()),
+                 ("v_cache_layout", Cache, cache()), ("table_stride", I64, 1250), ("tokens", I64, 40), ("d", I32, 64),
+                 ("batch", I32, 4), ("table_width", I32, 1250), ("causal", I32, 1), ("window", I32, 0),
+                 ("scale", F32, 0.125), ("max_q", I32, 10), ("max_kv", I32, 20000), ("workspace_bytes", I64, 1 << 40)],
+                **kw)
 
 
 @pytest.mark.parametrize("kw", [
     dict(d=12), dict(d=0), dict(d=264), dict(tokens=-1), dict(batch=-1), dict(max_q=-1), dict(max_kv=-1),
-    dict(max_kv=321), dict(table_width=-1), dict(table_stride=19), dict(kv_lens=None), dict(table=None),
-    dict(q_starts=None, tokens=3), dict(scale=float("inf")), dict(scale=float("nan")), dict(q=heads(count=12)),
-    dict(out=heads(kind=1)), dict(out=heads(count=4)), dict(out=heads(head=32)), dict(v_cache=cache(kind=1)),
-    dict(v_cache=cache(pages=4)), dict(v_cache=cache(size=8)), dict(v_cache=cache(count=4)), dict(workspace=None),
-    dict(bytes=0), dict(workspace=P + 8), dict(batch=1 << 30, max_q=1 << 20)]
-    + [dict(q=h) for h in BAD_HEADS] + [dict(k_cache=c) for c in BAD_CACHES])
+    dict(max_kv=20001), dict(table_width=-1), dict(table_stride=1249), dict(kv_lens=None), dict(table=None),
+    dict(q_starts=None, tokens=3), dict(scale=float("inf")), dict(scale=float("nan")), dict(window=-1), dict(q=None),
+    dict(out=None), dict(k_cache=None), dict(v_cache=None), dict(q_heads=heads(count=12)), dict(q_heads=NONE),
+    dict(out_heads=heads(kind=1)), dict(out_heads=heads(count=4)), dict(out_heads=heads(head=32)),
+    dict(v_cache_layout=cache(kind=1)), dict(v_cache_layout=cache(pages=4)), dict(v_cache_layout=cache(size=8)),
+    dict(v_cache_layout=cache(count=4)), dict(workspace=None), dict(workspace_bytes=0), dict(workspace_bytes=-1),
+    dict(workspace=P + 8), dict(batch=1 << 30, max_q=1 << 20)]
+    + [dict(q_heads=h) for h in BAD_HEADS] + [dict(k_cache_layout=c) for c in BAD_CACHES])
 def test_attention_refuses(lib, kw):
-    # Long enough that the call has a workspace.
-    if "max_kv" not in kw and "table_width" not in kw and "table_stride" not in kw:
-        kw = dict(max_kv=20000, table_width=1250, table_stride=1250, **kw)
     assert attention(lib, **kw) == INVALID and lib.pam_last_error() != b""
 
 
