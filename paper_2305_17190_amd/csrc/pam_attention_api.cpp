@@ -28,7 +28,8 @@ pam_status_t invalid(const char *name, const char *why) {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-constexpr int64_t kMaxRows = 0x7FFFFFFF;         // rows of a head launch, slots of a cache
+constexpr int64_t kMaxRows = 0x7FFFFFFF;         // slots of a cache, positions of a table
+constexpr int64_t kMaxHeadRows = (int64_t)1 << 25;  // a launch of them, 4 a workgroup, stays below 2^32 threads
 constexpr int64_t kMaxStride = (int64_t)1 << 31; // times a count below 2^31: offsets stay inside int64
 constexpr int64_t kMaxLaunchGroups = 16777215;   // workgroups of 256 threads: below 2^32 threads
 
@@ -103,8 +104,8 @@ template <typename P, typename A> void set_common(P &p, const A &a) {
 }
 
 pam_status_t check_rows(int64_t tokens, int64_t heads) {
-    if (tokens > kMaxRows / heads)
-        return invalid("tokens times heads must be below 2^31");
+    if (tokens > kMaxHeadRows / heads)
+        return invalid("tokens times heads must be at most 2^25");
     return PAM_SUCCESS;
 }
 
@@ -114,27 +115,26 @@ pamk::HeadPart &add_part(pamk::HeadRowsParams &p, const void *data, const pam_he
     part = pamk::HeadPart{};
     part.in = data;
     part.weight = weight;
-    part.in_token = in.stride_token;
-    part.in_head = in.stride_head;
-    part.first = p.heads;
-    part.heads = in.heads;
+    part.in_token = (uint32_t)in.stride_token;
+    part.in_head = (uint32_t)in.stride_head;
+    part.heads = (uint32_t)in.heads;
+    pamk::fast_divisor(part.heads, part.heads_mul, part.heads_shift);
     part.rotate = rotate;
-    p.heads += in.heads;
     return part;
 }
 
 void to_heads(pamk::HeadPart &part, void *data, const pam_heads_t &out) {
     part.out = data;
-    part.out_token = out.stride_token;
-    part.out_head = out.stride_head;
+    part.out_token = (uint32_t)out.stride_token;
+    part.out_head = (uint32_t)out.stride_head;
     part.out_bf16 = is_bf16(out.type);
 }
 
 void to_cache(pamk::HeadPart &part, void *data, const pam_cache_t &c) {
     part.out = data;
-    part.out_token = c.stride_page;
-    part.out_slot = c.stride_slot;
-    part.out_head = c.stride_head;
+    part.out_token = (uint32_t)c.stride_page;
+    part.out_slot = (uint32_t)c.stride_slot;
+    part.out_head = (uint32_t)c.stride_head;
     part.out_bf16 = is_bf16(c.type);
     part.paged = 1;
 }
@@ -263,7 +263,7 @@ pam_status_t pam_norm_rope(const pam_norm_rope_t *args, hipStream_t stream) {
         to_heads(add_part(p, a.k_in, a.k_in_heads, a.k_weight, true), a.k_out, a.k_out_heads);
     }
     PAM_TRY(check_rotation(a));
-    PAM_TRY(check_rows(a.tokens, p.heads));
+    PAM_TRY(check_rows(a.tokens, (int64_t)a.q_in_heads.heads + a.k_in_heads.heads));
     if (a.tokens == 0)
         return PAM_SUCCESS;
     PAM_TRY(api_check_device());
@@ -335,18 +335,19 @@ pam_status_t pam_norm_rope_grad(const pam_norm_rope_grad_t *args, hipStream_t st
         part.dx = s.dx;
         part.weight = s.weight;
         part.dweight = s.dweight;
-        part.x_token = s.x_heads.stride_token;
-        part.x_head = s.x_heads.stride_head;
-        part.dz_token = s.dz_heads.stride_token;
-        part.dz_head = s.dz_heads.stride_head;
-        part.dx_token = s.dx_heads.stride_token;
-        part.dx_head = s.dx_heads.stride_head;
-        part.heads = s.x_heads.heads;
+        part.x_token = (uint32_t)s.x_heads.stride_token;
+        part.x_head = (uint32_t)s.x_heads.stride_head;
+        part.dz_token = (uint32_t)s.dz_heads.stride_token;
+        part.dz_head = (uint32_t)s.dz_heads.stride_head;
+        part.dx_token = (uint32_t)s.dx_heads.stride_token;
+        part.dx_head = (uint32_t)s.dx_heads.stride_head;
+        part.heads = (uint32_t)s.x_heads.heads;
+        pamk::fast_divisor(part.heads, part.heads_mul, part.heads_shift);
         rows[i] = a.tokens * s.x_heads.heads;
         weights = weights || s.weight != nullptr;
     }
     PAM_TRY(check_rotation(a));
-    PAM_TRY(check_rows(a.tokens, (int64_t)p.part[0].heads + p.part[1].heads));
+    PAM_TRY(check_rows(a.tokens, (int64_t)a.q_in_heads.heads + a.k_in_heads.heads));
     if (a.tokens == 0 && !weights)
         return PAM_SUCCESS;
     set_common(p, a);
@@ -398,7 +399,7 @@ pam_status_t pam_append_kv(const pam_append_kv_t *args, hipStream_t stream) {
             return invalid("q_out: another count of heads than the input");
         to_heads(add_part(p, a.q_in, a.q_in_heads, a.q_weight, true), a.q_out, a.q_out_heads);
     }
-    PAM_TRY(check_rows(a.tokens, p.heads));
+    PAM_TRY(check_rows(a.tokens, (int64_t)a.k_heads.heads + a.v_heads.heads + a.q_in_heads.heads));
     if (a.tokens > 0 && a.slots == nullptr)
         return invalid("slots is NULL");
     if (a.tokens == 0)
@@ -406,7 +407,8 @@ pam_status_t pam_append_kv(const pam_append_kv_t *args, hipStream_t stream) {
     PAM_TRY(api_check_device());
     set_common(p, a);
     p.slots = a.slots;
-    p.page_size = kc.page_size;
+    p.page_size = (uint32_t)kc.page_size;
+    pamk::fast_divisor(p.page_size, p.page_mul, p.page_shift);
     p.cache_slots = kc.pages * kc.page_size;
     const hipError_t e = pamk::launch_head_rows(is_bf16(a.k_heads.type), p, stream);
     return e == hipSuccess ? PAM_SUCCESS : api_fail_hip(e, "pam_append_kv kernel launch");
@@ -476,12 +478,8 @@ pam_status_t pam_paged_attention(const pam_paged_attention_t *args, hipStream_t 
     p.q_bf16 = is_bf16(s.q_heads.type);
     p.k = {s.k_cache, kc.stride_page, kc.stride_slot, kc.stride_head, kc.pages};
     p.v = {s.v_cache, vc.stride_page, vc.stride_slot, vc.stride_head, vc.pages};
-    // key / page_size for key < 2^31 by a multiplication: with 2^l >= size,
-    // mul = 2^32 (2^l - size) / size + 1, (mulhi(key, mul) + key) >> l.
     p.page_size = (uint32_t)kc.page_size;
-    while (((uint64_t)1 << p.page_shift) < p.page_size)
-        ++p.page_shift;
-    p.page_mul = (uint32_t)(((((uint64_t)1 << p.page_shift) - p.page_size) << 32) / p.page_size + 1);
+    pamk::fast_divisor(p.page_size, p.page_mul, p.page_shift);
     p.q_starts = s.q_starts;
     p.kv_lens = s.kv_lens;
     p.table = s.table;

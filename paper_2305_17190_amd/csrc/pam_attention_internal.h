@@ -14,10 +14,11 @@ struct HeadPart {
     const void *in;
     void *out;
     const float *weight;            // norm's weight, or nullptr: no norm
-    int64_t in_token, in_head;      // strides, elements
-    int64_t out_token, out_head;    // out_token: stride of a page where paged
-    int64_t out_slot;               // paged: stride of a slot
-    int32_t first, heads;           // heads first .. first + heads - 1 of a token's rows
+    uint32_t in_token, in_head;     // strides, elements
+    uint32_t out_token, out_head;   // out_token: stride of a page where paged
+    uint32_t out_slot;              // paged: stride of a slot
+    uint32_t heads, heads_mul, heads_shift;   // fast_divisor(heads)
+    uint32_t first;                 // first workgroup of the part
     int32_t out_bf16;
     int32_t paged;
     int32_t rotate;
@@ -26,7 +27,6 @@ struct HeadPart {
 struct HeadRowsParams {
     HeadPart part[3];
     int32_t parts;
-    int32_t heads;                  // of all parts
     int64_t tokens;
     int32_t d, rot, interleaved;
     float eps;
@@ -35,8 +35,17 @@ struct HeadRowsParams {
     int64_t rows;                   // positions in the tables
     const int64_t *slots;
     int64_t cache_slots;            // pages * page_size
-    int32_t page_size;
+    uint32_t page_size, page_mul, page_shift;   // fast_divisor(page_size)
 };
+
+// n / divisor for n < 2^31 by a multiplication: (mulhi(n, mul) + n) >> shift, with
+// 2^shift >= divisor and mul = 2^32 (2^shift - divisor) / divisor + 1.
+inline void fast_divisor(uint32_t divisor, uint32_t &mul, uint32_t &shift) {
+    shift = 0;
+    while (((uint64_t)1 << shift) < divisor)
+        ++shift;
+    mul = (uint32_t)(((((uint64_t)1 << shift) - divisor) << 32) / divisor + 1);
+}
 
 // Norm and rotation of every part's rows, into tensors or cache slots.
 // bf16: the inputs are bfloat16.
@@ -48,8 +57,8 @@ struct HeadGradPart {
     const float *weight;
     float *dweight;
     float *partial;                 // [groups][d]
-    int64_t x_token, x_head, dz_token, dz_head, dx_token, dx_head;
-    int32_t heads;
+    uint32_t x_token, x_head, dz_token, dz_head, dx_token, dx_head;
+    uint32_t heads, heads_mul, heads_shift;
     int32_t groups;                 // workgroups of this part
 };
 
@@ -84,7 +93,7 @@ struct AttentionParams {
     int64_t q_token, q_head;
     int32_t q_bf16;
     CacheView k, v;
-    uint32_t page_size, page_mul, page_shift;   // key / page_size = (mulhi(key, mul) + key) >> shift
+    uint32_t page_size, page_mul, page_shift;   // fast_divisor(page_size)
     const int32_t *q_starts, *kv_lens, *table;
     int64_t table_stride;
     float *out;

@@ -24,8 +24,6 @@ namespace pamk {
 namespace {
 
 constexpr int kThreads = 256;
-// Workgroups per launch at most (the grid, in threads, stays below 2^32).
-constexpr int64_t kMaxGroups = 16777215;
 
 // V values of one type as registers; memory at any alignment of the element.
 template <typename T, int V> struct Vec;
@@ -40,13 +38,9 @@ __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 
 // Nearest even; NaN stays NaN.
-__device__ __forceinline__ uint16_t to_bf16(float x) {
-    const uint32_t u = __float_as_uint(x);
-    const uint32_t r = (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
-    return (uint16_t)((u & 0x7FFFFFFFu) > 0x7F800000u ? 0x7FC0u : r);
-}
+__device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
-template <typename T, int V> __device__ __forceinline__ void load(const void *base, int64_t at, float (&x)[V]) {
+template <typename T, int V> __device__ __forceinline__ void load(const void *base, uint64_t at, float (&x)[V]) {
     if constexpr (V == 1) {
         x[0] = widen(static_cast<const T *>(base)[at]);
     } else {
@@ -57,7 +51,7 @@ template <typename T, int V> __device__ __forceinline__ void load(const void *ba
     }
 }
 
-template <int V> __device__ __forceinline__ void store(void *base, int64_t at, const float (&x)[V], bool bf16) {
+template <int V> __device__ __forceinline__ void store(void *base, uint64_t at, const float (&x)[V], bool bf16) {
     if (bf16) {
         if constexpr (V == 1) {
             static_cast<uint16_t *>(base)[at] = to_bf16(x[0]);
@@ -86,11 +80,36 @@ template <int V> __device__ __forceinline__ void store(void *base, int64_t at, c
     }
 }
 
-// Sum over `lanes` (a power of two) neighbouring lanes.
+// Sum over `lanes` (a power of two) neighbouring lanes, in all of them.
+template <int CTRL> __device__ __forceinline__ float plus_dpp(float x) {
+    return x + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), CTRL, 0xF, 0xF, false));
+}
 __device__ __forceinline__ float lane_sum(float x, int lanes) {
-    for (int s = 1; s < lanes; s *= 2)
-        x += __shfl_xor(x, s);
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    if (lanes > 1)
+        x = plus_dpp<0xB1>(x);        // lane ^ 1
+    if (lanes > 2)
+        x = plus_dpp<0x4E>(x);        // lane ^ 2
+    if (lanes > 4)
+        x = plus_dpp<0x141>(x);       // 7 - lane: the other four
+    if (lanes > 8)
+        x = plus_dpp<0x140>(x);       // 15 - lane: the other eight
+    if (lanes > 16) {
+        const u32x2 s = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+        x = __uint_as_float(s.x) + __uint_as_float(s.y);
+    }
+    if (lanes > 32) {
+        const u32x2 s = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+        x = __uint_as_float(s.x) + __uint_as_float(s.y);
+    }
     return x;
+}
+
+// 1 / sqrt(sum / d + eps), the instruction's to 1 ulp; an infinite mean gives 0.
+__device__ __forceinline__ float inverse_root(float sum, int d, float eps) {
+    return __builtin_amdgcn_rsqf(sum * __builtin_amdgcn_rcpf((float)d) + eps);
 }
 
 // Where a unit's two groups of V values lie in the row, and its first pair.
@@ -139,85 +158,94 @@ __device__ __forceinline__ void turn(float (&lo)[V], float (&hi)[V], const float
 template <int V>
 __device__ __forceinline__ void angles(const float *cos, const float *sin, int position, int64_t rows, int rot,
                                        int pair, float (&c)[V], float (&s)[V]) {
-    if (position >= 0 && position < rows) {
-        const int64_t at = (int64_t)position * (rot / 2) + pair;
+    const bool known = position >= 0 && position < rows;
+    const uint64_t at = (uint64_t)(known ? position : 0) * (uint32_t)(rot / 2) + (uint32_t)pair;
+    if (rows > 0) {
         load<float, V>(cos, at, c);
         load<float, V>(sin, at, s);
-    } else {
+    }
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            c[i] = s[i] = __uint_as_float(0x7FC00000u);
+    for (int i = 0; i < V; ++i) {
+        c[i] = known ? c[i] : __uint_as_float(0x7FC00000u);
+        s[i] = known ? s[i] : __uint_as_float(0x7FC00000u);
     }
 }
 
-// N units a lane, `lanes` lanes a row (a power of two, at most a wave); rows,
-// tokens times heads, below 2^31.
+// N units a lane, `lanes` lanes a row (a power of two, at most a wave); a
+// workgroup's rows are of one part, tokens times heads of it below 2^31.
 template <typename T, int V, int N>
 __global__ void __launch_bounds__(kThreads) head_rows_kernel(const HeadRowsParams p, int lanes) {
+    const int which = p.parts > 2 && blockIdx.x >= p.part[2].first ? 2 : p.parts > 1 && blockIdx.x >= p.part[1].first ? 1 : 0;
+    const HeadPart &part = p.part[which];
     const int lane = threadIdx.x & (lanes - 1);
-    const int64_t rows = p.tokens * p.heads;
-    for (int64_t row = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / lanes; row < rows;
-         row += (int64_t)gridDim.x * (kThreads / lanes)) {
-        const int64_t token = (uint32_t)row / (uint32_t)p.heads;
-        int head = (int)(row - token * p.heads);
-        int which = 0;
-        while (which + 1 < p.parts && head >= p.part[which + 1].first)
-            ++which;
-        const HeadPart &part = p.part[which];
-        head -= part.first;
+    const uint32_t rows = (uint32_t)p.tokens * part.heads;
+    const uint32_t row = (blockIdx.x - part.first) * (uint32_t)(kThreads / lanes) + threadIdx.x / (uint32_t)lanes;
+    if (row >= rows)
+        return;
+    const uint32_t token = (__umulhi(row, part.heads_mul) + row) >> part.heads_shift;
+    const uint32_t head = row - token * part.heads;
+    const bool turns = p.rot > 0 && part.rotate, normed = part.weight != nullptr;
+    const int position = turns ? p.positions[token] : 0;
+    const int64_t slot = part.paged ? p.slots[token] : 0;
+    const uint64_t in_row = (uint64_t)token * part.in_token + (uint64_t)head * part.in_head;
 
-        int64_t out_row;
-        if (part.paged) {
-            const int64_t slot = p.slots[token];
-            if (slot < 0 || slot >= p.cache_slots)
-                continue;
-            const uint32_t page = (uint32_t)slot / (uint32_t)p.page_size;
-            out_row = (int64_t)page * part.out_token + (int64_t)((uint32_t)slot - page * p.page_size) * part.out_slot +
-                      (int64_t)head * part.out_head;
+    float lo[N][V], hi[N][V];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const Unit<V> u(lane + n * lanes, p.d, p.rot, p.interleaved);
+        if (u.live) {
+            load<T, V>(part.in, in_row + u.lo, lo[n]);
+            load<T, V>(part.in, in_row + u.hi, hi[n]);
         } else {
-            out_row = token * part.out_token + (int64_t)head * part.out_head;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                lo[n][i] = hi[n][i] = 0.0f;
         }
-        const int64_t in_row = token * part.in_token + (int64_t)head * part.in_head;
-
-        float lo[N][V], hi[N][V];
+    }
+    float wl[N][V], wh[N][V], c[N][V], s[N][V];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const Unit<V> u(lane + n * lanes, p.d, p.rot, p.interleaved);
+        if (u.live && normed) {
+            load<float, V>(part.weight, u.lo, wl[n]);
+            load<float, V>(part.weight, u.hi, wh[n]);
+        }
+        if (u.rotated && turns)
+            angles<V>(p.cos, p.sin, position, p.rows, p.rot, u.pair, c[n], s[n]);
+    }
+    uint64_t out_row = (uint64_t)token * part.out_token + (uint64_t)head * part.out_head;
+    if (part.paged) {
+        if (slot < 0 || slot >= p.cache_slots)
+            return;
+        const uint32_t page = (__umulhi((uint32_t)slot, p.page_mul) + (uint32_t)slot) >> p.page_shift;
+        out_row = (uint64_t)page * part.out_token + (uint64_t)((uint32_t)slot - page * p.page_size) * part.out_slot +
+                  (uint64_t)head * part.out_head;
+    }
+    if (normed) {
         float sum = 0.0f;
-    #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const Unit<V> u(lane + n * lanes, p.d, p.rot, p.interleaved);
-            if (u.live) {
-                load<T, V>(part.in, in_row + u.lo, lo[n]);
-                load<T, V>(part.in, in_row + u.hi, hi[n]);
-    #pragma unroll
-                for (int i = 0; i < V; ++i)
-                    sum += lo[n][i] * lo[n][i] + hi[n][i] * hi[n][i];
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                sum += lo[n][i] * lo[n][i] + hi[n][i] * hi[n][i];
+        const float r = inverse_root(lane_sum(sum, lanes), p.d, p.eps);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                lo[n][i] *= r * wl[n][i];
+                hi[n][i] *= r * wh[n][i];
             }
-        }
-        float r = 1.0f;
-        if (part.weight != nullptr)
-            r = 1.0f / sqrtf(lane_sum(sum, lanes) / (float)p.d + p.eps);
-    #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const Unit<V> u(lane + n * lanes, p.d, p.rot, p.interleaved);
-            if (!u.live)
-                continue;
-            if (part.weight != nullptr) {
-                float wl[V], wh[V];
-                load<float, V>(part.weight, u.lo, wl);
-                load<float, V>(part.weight, u.hi, wh);
-    #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    lo[n][i] = lo[n][i] * r * wl[i];
-                    hi[n][i] = hi[n][i] * r * wh[i];
-                }
-            }
-            if (part.rotate && u.rotated) {
-                float c[V], s[V];
-                angles<V>(p.cos, p.sin, p.positions[token], p.rows, p.rot, u.pair, c, s);
-                turn<V>(lo[n], hi[n], c, s, p.interleaved);
-            }
-            store<V>(part.out, out_row + u.lo, lo[n], part.out_bf16);
-            store<V>(part.out, out_row + u.hi, hi[n], part.out_bf16);
-        }
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const Unit<V> u(lane + n * lanes, p.d, p.rot, p.interleaved);
+        if (!u.live)
+            continue;
+        if (u.rotated && turns)
+            turn<V>(lo[n], hi[n], c[n], s[n], p.interleaved);
+        store<V>(part.out, out_row + u.lo, lo[n], part.out_bf16);
+        store<V>(part.out, out_row + u.hi, hi[n], part.out_bf16);
     }
 }
 
@@ -233,7 +261,7 @@ __global__ void __launch_bounds__(kThreads) head_grad_kernel(const HeadGradParam
     const int group = blockIdx.x - (second ? p.part[0].groups : 0);
     const int lane = threadIdx.x & (lanes - 1);
     const int per = kThreads / lanes;
-    const int64_t rows = p.tokens * part.heads;
+    const uint32_t rows = (uint32_t)p.tokens * part.heads;
     const bool normed = part.weight != nullptr;
 
     float wl[N][V], wh[N][V], dl[N][V], dh[N][V];
@@ -248,12 +276,12 @@ __global__ void __launch_bounds__(kThreads) head_grad_kernel(const HeadGradParam
             load<float, V>(part.weight, u.hi, wh[n]);
         }
     }
-    for (int64_t row = (int64_t)group * per + threadIdx.x / lanes; row < rows; row += (int64_t)part.groups * per) {
-        const int64_t token = (uint32_t)row / (uint32_t)part.heads;
-        const int64_t head = row - token * part.heads;
-        const int64_t x_row = token * part.x_token + head * part.x_head;
-        const int64_t z_row = token * part.dz_token + head * part.dz_head;
-        const int64_t d_row = token * part.dx_token + head * part.dx_head;
+    for (uint32_t row = group * per + threadIdx.x / lanes; row < rows; row += part.groups * per) {
+        const uint32_t token = (__umulhi(row, part.heads_mul) + row) >> part.heads_shift;
+        const uint32_t head = row - token * part.heads;
+        const uint64_t x_row = (uint64_t)token * part.x_token + (uint64_t)head * part.x_head;
+        const uint64_t z_row = (uint64_t)token * part.dz_token + (uint64_t)head * part.dz_head;
+        const uint64_t d_row = (uint64_t)token * part.dx_token + (uint64_t)head * part.dx_head;
         float gl[N][V], gh[N][V], xl[N][V], xh[N][V];
         float square = 0.0f, dot = 0.0f;
 #pragma unroll
@@ -285,8 +313,8 @@ __global__ void __launch_bounds__(kThreads) head_grad_kernel(const HeadGradParam
         }
         float r = 1.0f, back = 0.0f;
         if (normed) {
-            r = 1.0f / sqrtf(lane_sum(square, lanes) / (float)p.d + p.eps);
-            back = r * r * (lane_sum(dot, lanes) / (float)p.d);
+            r = inverse_root(lane_sum(square, lanes), p.d, p.eps);
+            back = r * r * (lane_sum(dot, lanes) * __builtin_amdgcn_rcpf((float)p.d));
         }
 #pragma unroll
         for (int n = 0; n < N; ++n) {
@@ -331,27 +359,28 @@ __global__ void __launch_bounds__(kThreads) head_grad_kernel(const HeadGradParam
     }
 }
 
-// dweight[i] = sum over the part's groups of partial[group][i]: 16 columns and
-// 16 runs of groups a workgroup, each run in order, then the runs in order.
-__global__ void __launch_bounds__(256) head_weight_kernel(const HeadGradParams p, int columns) {
-    __shared__ float sums[16][17];
-    const HeadGradPart &part = p.part[blockIdx.x / columns];
-    const int c = threadIdx.x % 16, run = threadIdx.x / 16;
-    const int i = (int)(blockIdx.x % columns) * 16 + c;
+// dweight[i] = sum over the part's groups of partial[group][i]: a workgroup takes
+// two columns (d is even), a lane every 256th group in order, then the lanes' sums
+// are added in halves.
+__global__ void __launch_bounds__(kThreads) head_weight_kernel(const HeadGradParams p) {
+    typedef float f32x2 __attribute__((ext_vector_type(2), aligned(4)));
+    __shared__ f32x2 sums[kThreads];
+    const HeadGradPart &part = p.part[blockIdx.x / (p.d / 2)];
+    const int i = (int)(blockIdx.x % (p.d / 2)) * 2;
     if (part.weight == nullptr)
         return;
-    float total = 0.0f;
-    if (i < p.d)
-        for (int g = run; g < part.groups; g += 16)
-            total += part.partial[(int64_t)g * p.d + i];
-    sums[run][c] = total;
-    __syncthreads();
-    if (run == 0 && i < p.d) {
-        total = 0.0f;
-        for (int r = 0; r < 16; ++r)
-            total += sums[r][c];
-        part.dweight[i] = total;
+    f32x2 total = {0.0f, 0.0f};
+#pragma unroll 4
+    for (int g = threadIdx.x; g < part.groups; g += kThreads)
+        total += *reinterpret_cast<const f32x2 *>(part.partial + (int64_t)g * p.d + i);
+    sums[threadIdx.x] = total;
+    for (int half = kThreads / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (threadIdx.x < half)
+            sums[threadIdx.x] += sums[threadIdx.x + half];
     }
+    if (threadIdx.x == 0)
+        *reinterpret_cast<f32x2 *>(part.dweight + i) = sums[0];
 }
 
 // V of a row of d values, `rot` of them rotated.
@@ -362,17 +391,25 @@ int unit_width(bool bf16, int d, int rot) {
     return 1;
 }
 
-// Lanes a row: its units on up to a wave's lanes.
-int row_lanes(int units) {
+// 16 values a lane where the row has them, so that what a row costs once is
+// spread over many; at most 64 lanes (V == 1, d == 256).
+int units_a_lane(int v) { return v == 8 ? 1 : 2; }
+
+// Lanes a row with n units a lane.
+int row_lanes(int units, int n) {
     int lanes = 1;
-    while (lanes < units && lanes < 64)
+    while (lanes * n < units)
         lanes *= 2;
     return lanes;
 }
 
-template <typename T, int V, int N> hipError_t rows_launch(const HeadRowsParams &p, int lanes, hipStream_t stream) {
+template <typename T, int V, int N> hipError_t rows_launch(HeadRowsParams p, int lanes, hipStream_t stream) {
     const int64_t per = kThreads / lanes;
-    const int64_t groups = std::min((p.tokens * p.heads + per - 1) / per, kMaxGroups);
+    int64_t groups = 0;
+    for (int i = 0; i < p.parts; ++i) {
+        p.part[i].first = (uint32_t)groups;
+        groups += (p.tokens * p.part[i].heads + per - 1) / per;
+    }
     hipLaunchKernelGGL((head_rows_kernel<T, V, N>), dim3((unsigned)groups), dim3(kThreads), 0, stream, p, lanes);
     return hipGetLastError();
 }
@@ -386,8 +423,7 @@ template <typename T, int V, int N> hipError_t grad_launch(const HeadGradParams 
     }
     if (p.part[0].weight == nullptr && p.part[1].weight == nullptr)
         return hipSuccess;
-    const int columns = (p.d + 15) / 16;
-    hipLaunchKernelGGL(head_weight_kernel, dim3((unsigned)(2 * columns)), dim3(256), 0, stream, p, columns);
+    hipLaunchKernelGGL(head_weight_kernel, dim3((unsigned)p.d), dim3(kThreads), 0, stream, p);
     return hipGetLastError();
 }
 
@@ -395,34 +431,29 @@ template <typename T, int V, int N> hipError_t grad_launch(const HeadGradParams 
 
 hipError_t launch_head_rows(bool bf16, const HeadRowsParams &p, hipStream_t stream) {
     const int v = unit_width(bf16, p.d, p.rot);
-    const int units = p.d / (2 * v);
-    const int lanes = row_lanes(units);
-    if (units > 64)   // V == 1 and d > 128
-        return bf16 ? rows_launch<uint16_t, 1, 2>(p, lanes, stream) : rows_launch<float, 1, 2>(p, lanes, stream);
+    const int lanes = row_lanes(p.d / (2 * v), units_a_lane(v));
     switch (v) {
     case 8: return rows_launch<uint16_t, 8, 1>(p, lanes, stream);
-    case 4: return bf16 ? rows_launch<uint16_t, 4, 1>(p, lanes, stream) : rows_launch<float, 4, 1>(p, lanes, stream);
-    case 2: return bf16 ? rows_launch<uint16_t, 2, 1>(p, lanes, stream) : rows_launch<float, 2, 1>(p, lanes, stream);
-    default: return bf16 ? rows_launch<uint16_t, 1, 1>(p, lanes, stream) : rows_launch<float, 1, 1>(p, lanes, stream);
+    case 4: return bf16 ? rows_launch<uint16_t, 4, 2>(p, lanes, stream) : rows_launch<float, 4, 2>(p, lanes, stream);
+    case 2: return bf16 ? rows_launch<uint16_t, 2, 2>(p, lanes, stream) : rows_launch<float, 2, 2>(p, lanes, stream);
+    default: return bf16 ? rows_launch<uint16_t, 1, 2>(p, lanes, stream) : rows_launch<float, 1, 2>(p, lanes, stream);
     }
 }
 
 int head_grad_groups(bool bf16, int64_t rows, int d, int rot, int most) {
-    const int per = kThreads / row_lanes(d / (2 * unit_width(bf16, d, rot)));
+    const int v = unit_width(bf16, d, rot);
+    const int per = kThreads / row_lanes(d / (2 * v), units_a_lane(v));
     return (int)std::min<int64_t>((rows + per - 1) / per, most);
 }
 
 hipError_t launch_head_grad(bool bf16, const HeadGradParams &p, hipStream_t stream) {
     const int v = unit_width(bf16, p.d, p.rot);
-    const int units = p.d / (2 * v);
-    const int lanes = row_lanes(units);
-    if (units > 64)
-        return bf16 ? grad_launch<uint16_t, 1, 2>(p, lanes, stream) : grad_launch<float, 1, 2>(p, lanes, stream);
+    const int lanes = row_lanes(p.d / (2 * v), units_a_lane(v));
     switch (v) {
     case 8: return grad_launch<uint16_t, 8, 1>(p, lanes, stream);
-    case 4: return bf16 ? grad_launch<uint16_t, 4, 1>(p, lanes, stream) : grad_launch<float, 4, 1>(p, lanes, stream);
-    case 2: return bf16 ? grad_launch<uint16_t, 2, 1>(p, lanes, stream) : grad_launch<float, 2, 1>(p, lanes, stream);
-    default: return bf16 ? grad_launch<uint16_t, 1, 1>(p, lanes, stream) : grad_launch<float, 1, 1>(p, lanes, stream);
+    case 4: return bf16 ? grad_launch<uint16_t, 4, 2>(p, lanes, stream) : grad_launch<float, 4, 2>(p, lanes, stream);
+    case 2: return bf16 ? grad_launch<uint16_t, 2, 2>(p, lanes, stream) : grad_launch<float, 2, 2>(p, lanes, stream);
+    default: return bf16 ? grad_launch<uint16_t, 1, 2>(p, lanes, stream) : grad_launch<float, 1, 2>(p, lanes, stream);
     }
 }
 
