@@ -51,6 +51,24 @@ template <typename T, int V> __device__ __forceinline__ void load(const void *ba
     }
 }
 
+// V values as they lie in memory, to be widened when they are used.
+template <typename T, int V> struct Raw {
+    typename Vec<T, V>::type v;
+    __device__ __forceinline__ void load(const void *base, uint64_t at) {
+        v = *reinterpret_cast<const typename Vec<T, V>::type *>(static_cast<const T *>(base) + at);
+    }
+    __device__ __forceinline__ void get(float (&x)[V]) const {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            x[i] = widen(v[i]);
+    }
+};
+template <typename T> struct Raw<T, 1> {
+    T v;
+    __device__ __forceinline__ void load(const void *base, uint64_t at) { v = static_cast<const T *>(base)[at]; }
+    __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = widen(v); }
+};
+
 template <int V> __device__ __forceinline__ void store(void *base, uint64_t at, const float (&x)[V], bool bf16) {
     if (bf16) {
         if constexpr (V == 1) {
@@ -276,11 +294,48 @@ __global__ void __launch_bounds__(kThreads) head_grad_kernel(const HeadGradParam
             load<float, V>(part.weight, u.hi, wh[n]);
         }
     }
-    for (uint32_t row = group * per + threadIdx.x / lanes; row < rows; row += part.groups * per) {
-        const uint32_t token = (__umulhi(row, part.heads_mul) + row) >> part.heads_shift;
-        const uint32_t head = row - token * part.heads;
+    // A row's loads are on their way while the row before it is worked on; its
+    // position, which they wait for, a row earlier still.
+    const uint32_t step = (uint32_t)part.groups * per;
+    auto token_of = [&](uint32_t row) { return (__umulhi(row, part.heads_mul) + row) >> part.heads_shift; };
+    auto position_of = [&](uint32_t row) { return p.positions != nullptr && row < rows ? p.positions[token_of(row)] : 0; };
+    struct Item {
+        Raw<T, V> zl[N], zh[N], xl[N], xh[N];
+        float c[N][V], s[N][V];
+    };
+    auto fetch = [&](uint32_t row, int position) {
+        Item item;
+        const uint32_t token = token_of(row), head = row - token * part.heads;
         const uint64_t x_row = (uint64_t)token * part.x_token + (uint64_t)head * part.x_head;
         const uint64_t z_row = (uint64_t)token * part.dz_token + (uint64_t)head * part.dz_head;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const Unit<V> u(lane + n * lanes, p.d, p.rot, p.interleaved);
+            if (!u.live)
+                continue;
+            item.zl[n].load(part.dz, z_row + u.lo);
+            item.zh[n].load(part.dz, z_row + u.hi);
+            if (normed) {
+                item.xl[n].load(part.x, x_row + u.lo);
+                item.xh[n].load(part.x, x_row + u.hi);
+            }
+            if (u.rotated && p.positions != nullptr)
+                angles<V>(p.cos, p.sin, position, p.rows, p.rot, u.pair, item.c[n], item.s[n]);
+        }
+        return item;
+    };
+    uint32_t row = group * per + threadIdx.x / lanes;
+    Item next;
+    int position = position_of(row);
+    if (row < rows)
+        next = fetch(row, position);
+    position = position_of(row + step);
+    for (; row < rows; row += step) {
+        const Item item = next;
+        if (row + step < rows)
+            next = fetch(row + step, position);
+        position = position_of(row + 2 * step);
+        const uint32_t token = token_of(row), head = row - token * part.heads;
         const uint64_t d_row = (uint64_t)token * part.dx_token + (uint64_t)head * part.dx_head;
         float gl[N][V], gh[N][V], xl[N][V], xh[N][V];
         float square = 0.0f, dot = 0.0f;
@@ -289,21 +344,18 @@ __global__ void __launch_bounds__(kThreads) head_grad_kernel(const HeadGradParam
             const Unit<V> u(lane + n * lanes, p.d, p.rot, p.interleaved);
             if (!u.live)
                 continue;
-            load<T, V>(part.dz, z_row + u.lo, gl[n]);
-            load<T, V>(part.dz, z_row + u.hi, gh[n]);
-            if (normed) {
-                load<T, V>(part.x, x_row + u.lo, xl[n]);
-                load<T, V>(part.x, x_row + u.hi, xh[n]);
-            }
+            item.zl[n].get(gl[n]);
+            item.zh[n].get(gh[n]);
             if (u.rotated && p.positions != nullptr) {
-                float c[V], s[V];
-                angles<V>(p.cos, p.sin, p.positions[token], p.rows, p.rot, u.pair, c, s);
+                float back[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i)
-                    s[i] = -s[i];
-                turn<V>(gl[n], gh[n], c, s, p.interleaved);
+                    back[i] = -item.s[n][i];
+                turn<V>(gl[n], gh[n], item.c[n], back, p.interleaved);
             }
             if (normed) {
+                item.xl[n].get(xl[n]);
+                item.xh[n].get(xh[n]);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     square += xl[n][i] * xl[n][i] + xh[n][i] * xh[n][i];
@@ -394,6 +446,8 @@ int unit_width(bool bf16, int d, int rot) {
 // 16 values a lane where the row has them, so that what a row costs once is
 // spread over many; at most 64 lanes (V == 1, d == 256).
 int units_a_lane(int v) { return v == 8 ? 1 : 2; }
+// The gradient's lanes hold more of each value.
+int grad_units(int v) { return v >= 4 ? 1 : 2; }
 
 // Lanes a row with n units a lane.
 int row_lanes(int units, int n) {
@@ -442,16 +496,17 @@ hipError_t launch_head_rows(bool bf16, const HeadRowsParams &p, hipStream_t stre
 
 int head_grad_groups(bool bf16, int64_t rows, int d, int rot, int most) {
     const int v = unit_width(bf16, d, rot);
-    const int per = kThreads / row_lanes(d / (2 * v), units_a_lane(v));
-    return (int)std::min<int64_t>((rows + per - 1) / per, most);
+    const int per = kThreads / row_lanes(d / (2 * v), grad_units(v));
+    // One round of workgroups: four a compute unit, three with 8 values a load.
+    return (int)std::min<int64_t>((rows + per - 1) / per, v == 8 ? std::max(most * 3 / 4, 1) : most);
 }
 
 hipError_t launch_head_grad(bool bf16, const HeadGradParams &p, hipStream_t stream) {
     const int v = unit_width(bf16, p.d, p.rot);
-    const int lanes = row_lanes(p.d / (2 * v), units_a_lane(v));
+    const int lanes = row_lanes(p.d / (2 * v), grad_units(v));
     switch (v) {
     case 8: return grad_launch<uint16_t, 8, 1>(p, lanes, stream);
-    case 4: return bf16 ? grad_launch<uint16_t, 4, 2>(p, lanes, stream) : grad_launch<float, 4, 2>(p, lanes, stream);
+    case 4: return bf16 ? grad_launch<uint16_t, 4, 1>(p, lanes, stream) : grad_launch<float, 4, 1>(p, lanes, stream);
     case 2: return bf16 ? grad_launch<uint16_t, 2, 2>(p, lanes, stream) : grad_launch<float, 2, 2>(p, lanes, stream);
     default: return bf16 ? grad_launch<uint16_t, 1, 2>(p, lanes, stream) : grad_launch<float, 1, 2>(p, lanes, stream);
     }
