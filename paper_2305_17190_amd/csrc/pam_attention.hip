@@ -34,7 +34,7 @@ namespace pamk {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostWaves = 8;
+constexpr int kMostWaves = 16;
 constexpr int kGroup = 64;            // keys a wave takes at a time
 constexpr int kLoads = 4;             // loads of a batch at most; a wave has one to two batches in flight
 
@@ -94,9 +94,10 @@ template <int R> struct Area {
 // the wave.  next(first) starts to fetch what the group from `first` on needs,
 // keep(buffer) puts it where load(buffer, n) finds load n's offset; use(buffer,
 // n, words) takes load n, done(buffer, first) closes a group.
-template <typename T, int L, typename Next, typename Keep, typename From, typename Use, typename Done>
+// begin() runs once the first loads are out.
+template <typename T, int L, typename Next, typename Keep, typename From, typename Begin, typename Use, typename Done>
 __device__ __forceinline__ void stream_keys(const void *data, int first, int end, int step, Next next, Keep keep,
-                                            From from, Use use, Done done) {
+                                            From from, Begin begin, Use use, Done done) {
     constexpr int B = L / 2 < kLoads ? L / 2 : kLoads;
     constexpr int N = L / B;
     if (first >= end)
@@ -107,6 +108,7 @@ __device__ __forceinline__ void stream_keys(const void *data, int first, int end
 #pragma unroll
     for (int u = 0; u < B; ++u)
         w[0][u] = load16<T>(data, from(0, u));
+    begin();
     for (int buffer = 0; first < end; first += step, buffer ^= 1) {
         next(first + step);
 #pragma unroll
@@ -194,7 +196,6 @@ __device__ __forceinline__ void score_keys(const AttentionParams &p, const Unit 
     const int at = (lane % L) * E, reads = at < p.d ? at : 0;
     const Rows<R> rows(p, unit);
     uint32_t q[R][E];
-    load_queries<E, R>(p, unit, at, q);
     int64_t place = -1;
     uint64_t there[2] = {0, 0};
     float v[S + 1][R];
@@ -209,6 +210,7 @@ __device__ __forceinline__ void score_keys(const AttentionParams &p, const Unit 
             wave_sync();
         },
         [&](int buffer, int n) { return area.from[buffer][n * K + lane / L] + reads; },
+        [&]() { load_queries<E, R>(p, unit, at, q); },
         [&](int, int n, const u32x4 &w) {
             float sum[R];
 #pragma unroll
@@ -387,7 +389,7 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
             put<R>(reinterpret_cast<float *>(area.pr[buffer]) + lane * R, t);
             wave_sync();
         },
-        [&](int buffer, int n) { return area.from[buffer][n * K + lane / L] + reads; },
+        [&](int buffer, int n) { return area.from[buffer][n * K + lane / L] + reads; }, []() {},
         [&](int buffer, int n, const u32x4 &w) {
             float b[R];
             get<R>(reinterpret_cast<const float *>(area.pr[buffer]) + (n * K + lane / L) * R, b);
@@ -414,6 +416,7 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
             if constexpr (L <= 32)
                 acc[r][i] = merge<5>(acc[r][i], acc[r][i], lane);
         }
+    __syncthreads();                   // scratch may be where the areas are
     if (lane < L) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -455,17 +458,18 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
     }
 }
 
-// A unit in one workgroup: its scores stay in LDS.
+// A unit in one workgroup: its scores stay in LDS, followed by what the waves
+// keep of their keys and, in the same place, their outputs.
 template <typename T, int L, int R>
-__global__ void __launch_bounds__(kMostWaves * 64) attention_whole_kernel(const AttentionParams p) {
-    extern __shared__ float s[];
-    __shared__ Area<R> areas[kMostWaves];
+__global__ void __launch_bounds__(whole_most_waves(R) * 64) attention_whole_kernel(const AttentionParams p) {
+    extern __shared__ float4 lds[];
     __shared__ float top[kMostWaves][R], sum[kMostWaves][R];
     const Unit unit(p, blockIdx.x);
     if (unit.rows == 0)
         return;
     const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    float *scratch = s + (int64_t)p.max_kv * R;
+    float *s = reinterpret_cast<float *>(lds), *after = reinterpret_cast<float *>(lds + (p.max_kv * R + 3) / 4);
+    Area<R> *areas = reinterpret_cast<Area<R> *>(after);
     Running<R> row;
     score_keys<T, L, R>(p, unit, unit.lo + wave * kGroup, unit.hi, waves * kGroup, areas[wave],
                         [&](int key, const float (&t)[R]) {
@@ -473,7 +477,7 @@ __global__ void __launch_bounds__(kMostWaves * 64) attention_whole_kernel(const 
                             put<R>(s + (key - unit.lo) * R, t);
                         });
     row.over_group(top, sum);
-    value_keys<T, L, R>(p, unit, unit.lo, unit.hi, s, row, areas, scratch, nullptr);
+    value_keys<T, L, R>(p, unit, unit.lo, unit.hi, s, row, areas, after, nullptr);
 }
 
 // Consecutive workgroups, which go to the chip's eight dies in turn, take one
@@ -576,8 +580,8 @@ hipError_t launch(Which which, const AttentionParams &p, hipStream_t stream) {
     const void *kernel = which == kWhole    ? (const void *)attention_whole_kernel<T, L, R>
                          : which == kScores ? (const void *)attention_scores_kernel<T, L, R>
                                             : (const void *)attention_values_kernel<T, L, R>;
-    const int threads = which == kWhole ? whole_waves(p.max_kv) * 64 : kThreads;
-    const size_t lds = which == kWhole ? ((size_t)p.max_kv + threads / 64 * L * kPer<T>) * R * sizeof(float) : 0;
+    const int threads = which == kWhole ? whole_waves(p.max_kv, R) * 64 : kThreads;
+    const size_t lds = which == kWhole ? (size_t)whole_lds(p.max_kv, R, L, sizeof(T) == 2) : 0;
     const unsigned grid = which == kWhole ? units : units * (unsigned)p.splits;
     void *args[] = {const_cast<AttentionParams *>(&p)};
     return hipLaunchKernel(kernel, dim3(grid), dim3((unsigned)threads), args, lds, stream);

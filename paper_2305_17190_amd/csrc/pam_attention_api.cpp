@@ -166,7 +166,6 @@ struct AttentionPlan {
     size_t bytes() const { return scores + stats + partial; }
 };
 
-constexpr int64_t kTileRows = 33;         // fewest rows of a key head that run as tiles
 constexpr int64_t kSlabBytes = (int64_t)512 << 20;   // scores of one round of launches, about
 
 AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool bf16, int32_t batch, int32_t max_q,
@@ -176,22 +175,37 @@ AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool 
     a.lanes = 4;
     while (a.lanes * per < d)
         a.lanes *= 2;
-    const int64_t rows = (int64_t)max_q * (q_heads / kv_heads);
-    if (rows >= kTileRows) {
+    const int64_t rows = std::max<int64_t>((int64_t)max_q * (q_heads / kv_heads), 1);
+    const int64_t heads = (int64_t)batch * kv_heads;
+
+    // Few rows a unit, or tiles: by the time of each, in microseconds for MACs in
+    // millions, fitted to 70 calls.  A tile's waves are few and each long (chunk of
+    // 42 tokens over 291 keys of 256: 149 us as tiles, 48 with few rows), but
+    // two to three times as fast where they fill the chip (512 x 4 heads over 4096
+    // keys of 128: 675 us, 1384 with few rows).
+    const int64_t blocks = ceil_div(rows, 8), each = ceil_div(rows, blocks);
+    const int few_rows = (int)(each <= 4 ? each : each <= 6 ? 6 : 8);
+    const double macs = 2e-6 * (double)d * (double)heads * (double)max_kv;
+    const double few_us = 15.0 + macs * (double)(blocks * few_rows) / 12.0;
+    const double tile_us = 50.0 + 0.3 * d + macs * (double)(ceil_div(rows, 64) * 64) / 22.0;
+    const bool tiled = tile_us < few_us;
+    if (tiled) {
         // 128 rows a unit where that leaves two rounds of score tiles, four
         // workgroups a compute unit; else 64, which waste less.
-        const int64_t tiles = (int64_t)batch * kv_heads * ceil_div(rows, 128) * ceil_div(max_kv, 128);
+        const int64_t tiles = heads * ceil_div(rows, 128) * ceil_div(max_kv, 128);
         a.rows = rows > 64 && tiles >= 2048 ? 128 : 64;
     } else {
-        const int64_t blocks = ceil_div(std::max<int64_t>(rows, 1), 8), each = ceil_div(std::max<int64_t>(rows, 1), blocks);
-        a.rows = (int)(each <= 4 ? each : each <= 6 ? 6 : 8);
+        a.rows = few_rows;
     }
-    a.row_blocks = (int)ceil_div(std::max<int64_t>(rows, 1), a.rows);
-    a.units = a.slab = (int64_t)batch * kv_heads * a.row_blocks;
+    a.row_blocks = (int)ceil_div(rows, a.rows);
+    a.units = a.slab = heads * a.row_blocks;
     a.splits = 1;
-    a.form = rows >= kTileRows ? Form::tiles
-             : pamk::whole_lds(max_kv, a.rows, a.lanes, bf16) <= pamk::kWholeLds && (a.units >= 256 || max_kv <= 256) ? Form::whole
-                                                                                            : Form::split;
+    // One launch where a workgroup's four waves take the keys in one go (one of
+    // 1000 keys, 16 waves: 35 us, split 21), or where the units fill the chip and
+    // their scores fit in LDS.
+    const int64_t lds = pamk::whole_lds(max_kv, a.rows, a.lanes, bf16);
+    const bool whole = (max_kv <= 256 && lds <= pamk::kWholeLds) || (a.units >= 256 && lds <= pamk::kWholeLds / 2);
+    a.form = tiled ? Form::tiles : whole ? Form::whole : Form::split;
     if (a.form == Form::whole || a.units == 0)
         return a;
     if (a.form == Form::tiles) {
@@ -499,6 +513,9 @@ pam_status_t pam_paged_attention(const pam_paged_attention_t *args, hipStream_t 
     p.scale = (float)((double)s.scale * 1.4426950408889634);
     p.rows = plan.rows;
     p.row_blocks = plan.row_blocks;
+    pamk::fast_divisor((uint32_t)p.row_blocks, p.blocks_mul, p.blocks_shift);
+    pamk::fast_divisor((uint32_t)p.kv_heads, p.heads_mul, p.heads_shift);
+    pamk::fast_divisor((uint32_t)p.group, p.group_mul, p.group_shift);
     p.splits = plan.splits;
     p.split_keys = plan.split_keys;
     p.scores = static_cast<float *>(s.workspace);

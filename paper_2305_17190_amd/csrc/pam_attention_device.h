@@ -56,6 +56,11 @@ __device__ __forceinline__ float pam_fma(float a1, float m, uint32_t b, float ac
 
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & kExpMask) != kExpMask; }
 
+// n / divisor, the host's fast_divisor.
+__device__ __forceinline__ uint32_t divided(uint32_t n, uint32_t mul, uint32_t shift) {
+    return (__umulhi(n, mul) + n) >> shift;
+}
+
 // The unit a workgroup works on, and which keys its rows see.
 struct Unit {
     int b, head, first_row, rows;   // rows of it that exist
@@ -66,9 +71,9 @@ struct Unit {
     const int32_t *table;
 
     __device__ __forceinline__ Unit(const AttentionParams &p, int unit) {
-        const int block = unit % p.row_blocks;
-        const int bh = unit / p.row_blocks;
-        b = bh / p.kv_heads;
+        const int bh = (int)divided((uint32_t)unit, p.blocks_mul, p.blocks_shift);
+        const int block = unit - bh * p.row_blocks;
+        b = (int)divided((uint32_t)bh, p.heads_mul, p.heads_shift);
         head = bh - b * p.kv_heads;
         first_token = p.q_starts ? p.q_starts[b] : b;
         const int64_t count = p.q_starts ? (int64_t)p.q_starts[b + 1] - first_token : 1;
@@ -90,7 +95,9 @@ struct Unit {
             hi = row_hi(p, rows - 1);
         }
     }
-    __device__ __forceinline__ int token(const AttentionParams &p, int row) const { return (first_row + row) / p.group; }
+    __device__ __forceinline__ int token(const AttentionParams &p, int row) const {
+        return (int)divided((uint32_t)(first_row + row), p.group_mul, p.group_shift);
+    }
     // Keys lo <= j < hi are those the row sees (page permitting).
     __device__ __forceinline__ int row_lo(const AttentionParams &p, int row) const {
         if (p.window <= 0)
@@ -113,7 +120,7 @@ struct Unit {
     }
     // Element offset of a key's row in a cache, or -1 where its page is not one.
     __device__ __forceinline__ int64_t key_at(const AttentionParams &p, const CacheView &c, int key) const {
-        const uint32_t page = (__umulhi((uint32_t)key, p.page_mul) + (uint32_t)key) >> p.page_shift;
+        const uint32_t page = divided((uint32_t)key, p.page_mul, p.page_shift);
         const int id = table[page];
         if (id < 0 || id >= c.pages)
             return -1;

@@ -103,6 +103,8 @@ struct AttentionParams {
     int32_t max_q, max_kv, causal, window;
     float scale;                    // times log2(e)
     int32_t rows, row_blocks;
+    uint32_t blocks_mul, blocks_shift, heads_mul, heads_shift, group_mul, group_shift;   // fast_divisor of
+                                    // row_blocks, kv_heads and group
     int32_t first_unit;             // of this launch; workspaces count units from it
     int32_t splits, split_keys;     // keys of a unit: splits of split_keys (a multiple of 64)
     float *scores;                  // [unit][splits * split_keys][rows], in units of log2
@@ -111,16 +113,21 @@ struct AttentionParams {
 };
 
 // Few rows a unit (pam_attention.hip), `lanes` lanes a key: one launch with
-// the scores in LDS (max_kv * rows floats, and its waves' outputs), or two with
-// the keys split.
-inline int whole_waves(int max_kv) { return max_kv <= 256 ? 4 : 8; }
-// LDS bytes of one launch's workgroup: scores, and per wave its outputs and the
-// 64 keys it works on.
-inline int64_t whole_lds(int64_t max_kv, int64_t rows, int lanes, bool bf16) {
-    const int64_t waves = 8;
-    return 4 * rows * (max_kv + waves * lanes * (bf16 ? 8 : 4)) + waves * 128 * (8 + 4 * rows) + 512;
+// the scores in LDS, or two with the keys split.
+// The one launch's waves: of 64 keys each, 16 at most with up to 4 rows (128
+// registers a lane), else 8.
+constexpr int whole_most_waves(int rows) { return rows <= 4 ? 16 : 8; }
+inline int whole_waves(int64_t max_kv, int rows) {
+    const int64_t waves = (max_kv + 63) / 64;
+    return waves < 4 ? 4 : waves < whole_most_waves(rows) ? (int)waves : whole_most_waves(rows);
 }
-constexpr int64_t kWholeLds = 65536;   // at most
+// Its LDS bytes: the scores, and the keys that the waves work on or, afterwards,
+// their outputs.
+inline int64_t whole_lds(int64_t max_kv, int rows, int lanes, bool bf16) {
+    const int64_t waves = whole_waves(max_kv, rows), keys = 128 * (8 + 4 * rows), out = 4 * rows * lanes * (bf16 ? 8 : 4);
+    return (4 * rows * max_kv + 15) / 16 * 16 + waves * (keys > out ? keys : out);
+}
+constexpr int64_t kWholeLds = 131072;   // at most
 hipError_t launch_attention_whole(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream);
 hipError_t launch_attention_scores(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream);
 hipError_t launch_attention_values(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream);
