@@ -35,7 +35,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMostWaves = 16;
-constexpr int kGroup = 64;            // keys a wave takes at a time
+// Keys a wave takes at a time: 64, or 16 in small problems, where more and
+// shorter waves end sooner (F, for fine).
+constexpr int kGroup = 64, kFineGroup = 16;
+template <bool F> constexpr int group_keys() { return F ? kFineGroup : kGroup; }
 constexpr int kLoads = 4;             // loads of a batch at most; a wave has one to two batches in flight
 
 __device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x); }
@@ -94,11 +97,13 @@ template <int R> struct Area {
 // the wave.  next(first) starts to fetch what the group from `first` on needs,
 // keep(buffer) puts it where load(buffer, n) finds load n's offset; use(buffer,
 // n, words) takes load n, done(buffer, first) closes a group.
-// begin() runs once the first loads are out.
-template <typename T, int L, typename Next, typename Keep, typename From, typename Begin, typename Use, typename Done>
+// begin() runs once the first loads are out.  Fine groups: all loads of a group
+// at once, one group after the other.
+template <typename T, int L, bool F, typename Next, typename Keep, typename From, typename Begin, typename Use,
+          typename Done>
 __device__ __forceinline__ void stream_keys(const void *data, int first, int end, int step, Next next, Keep keep,
                                             From from, Begin begin, Use use, Done done) {
-    constexpr int B = L / 2 < kLoads ? L / 2 : kLoads;
+    constexpr int B = F ? L / 4 : L / 2 < kLoads ? L / 2 : kLoads;
     constexpr int N = L / B;
     if (first >= end)
         return;
@@ -109,6 +114,22 @@ __device__ __forceinline__ void stream_keys(const void *data, int first, int end
     for (int u = 0; u < B; ++u)
         w[0][u] = load16<T>(data, from(0, u));
     begin();
+    if constexpr (F) {
+        for (;;) {
+#pragma unroll
+            for (int u = 0; u < B; ++u)
+                use(0, u, w[0][u]);
+            done(0, first);
+            first += step;
+            if (first >= end)
+                return;
+            next(first);
+            keep(0);
+#pragma unroll
+            for (int u = 0; u < B; ++u)
+                w[0][u] = load16<T>(data, from(0, u));
+        }
+    }
     for (int buffer = 0; first < end; first += step, buffer ^= 1) {
         next(first + step);
 #pragma unroll
@@ -183,25 +204,26 @@ __device__ __forceinline__ void load_queries(const AttentionParams &p, const Uni
     }
 }
 
-// Scores, in units of log2, of the wave's keys first, first + step, ... below end, 64 at a time:
+// Scores, in units of log2, of the wave's keys first, first + step, ... below end, a group at a time:
 // take(key, t) gets a key's scores, -inf
 // where a row does not see it.
-template <typename T, int L, int R, typename Take>
+template <typename T, int L, int R, bool F, typename Take>
 __device__ __forceinline__ void score_keys(const AttentionParams &p, const Unit &unit, int first, int end, int step,
                                            Area<R> &area, Take take) {
     constexpr int E = kPer<T>;
     constexpr int K = 64 / L;
-    constexpr int S = log2_of(L);
+    constexpr int S = log2_of(L), M = F ? S - 2 : S;   // steps, and those that merge; the others add to both sides
+    constexpr int G = group_keys<F>();
     const int lane = threadIdx.x & 63;
     const int at = (lane % L) * E, reads = at < p.d ? at : 0;
     const Rows<R> rows(p, unit);
     uint32_t q[R][E];
     int64_t place = -1;
     uint64_t there[2] = {0, 0};
-    float v[S + 1][R];
-    stream_keys<T, L>(
+    float v[M + 1][R];
+    stream_keys<T, L, F>(
         p.k.data, first, end, step,
-        [&](int from) { place = from + lane < end ? unit.key_at(p, p.k, from + lane) : -1; },
+        [&](int from) { place = lane < G && from + lane < end ? unit.key_at(p, p.k, from + lane) : -1; },
         [&](int buffer) {
             wave_sync();
             there[0] = there[1];
@@ -228,26 +250,27 @@ __device__ __forceinline__ void score_keys(const AttentionParams &p, const Unit 
             // number goes with bit S - 1 - j of the lane's.
             int level = 0;
 #pragma unroll
-            for (int j = 0; j < S; ++j)
+            for (int j = 0; j < M; ++j)
                 level += (n & ((2 << j) - 1)) == (2 << j) - 1;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float x = sum[r];
-                if (level > 0)
-                    x = merge<S - 1>(v[0][r], x, lane);
-                if constexpr (S > 1)
+                if constexpr (M > 0)
+                    if (level > 0)
+                        x = merge<S - 1>(v[0][r], x, lane);
+                if constexpr (M > 1)
                     if (level > 1)
                         x = merge<S - 2>(v[1][r], x, lane);
-                if constexpr (S > 2)
+                if constexpr (M > 2)
                     if (level > 2)
                         x = merge<S - 3>(v[2][r], x, lane);
-                if constexpr (S > 3)
+                if constexpr (M > 3)
                     if (level > 3)
                         x = merge<S - 4>(v[3][r], x, lane);
-                if constexpr (S > 4)
+                if constexpr (M > 4)
                     if (level > 4)
                         x = merge<S - 5>(v[4][r], x, lane);
-                if constexpr (S > 5)
+                if constexpr (M > 5)
                     if (level > 5)
                         x = merge<0>(v[5][r], x, lane);
                 v[level][r] = x;
@@ -255,13 +278,18 @@ __device__ __forceinline__ void score_keys(const AttentionParams &p, const Unit 
         },
         [&](int buffer, int from) {
             // The lane's own key: its number's bits from the loads' are the
-            // lane's in reverse.
-            const int own = (int)(__brev((uint32_t)(lane % L)) >> (32 - S)) * K + lane / L, key = from + own;
-            const bool exists = there[0] >> own & 1;
+            // lane's in reverse (four lanes with a key in fine groups).
+            const int own = ((int)(__brev((uint32_t)(lane % L)) >> (32 - S)) & (G / K - 1)) * K + lane / L;
+            const int key = from + own;
+            const bool exists = there[F ? 1 : 0] >> own & 1;   // a group ahead where streamed
             float t[R];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                float sum = v[S][r];
+                float sum = v[M][r];
+                if constexpr (F) {
+                    sum += dpp<kXor2>(sum);
+                    sum += dpp<kXor1>(sum);
+                }
                 const bool sees = exists && key >= rows.lo[r] && key < rows.hi[r];
                 if (sees && !finite(sum)) {
                     sum = 0.0f;
@@ -271,7 +299,7 @@ __device__ __forceinline__ void score_keys(const AttentionParams &p, const Unit 
                 }
                 t[r] = sees ? sum * p.scale : kNegInf;
             }
-            if (key < end)
+            if (key < end && (!F || lane % 4 == 0))
                 take(key, t);
         });
 }
@@ -353,7 +381,7 @@ template <int R> struct Running {
 // out[row][i] = sum over keys begin <= j < end of P .^ v, the scores at
 // scores[(j - origin) * R + row]; to out's rows (partial == nullptr) or
 // partial[row * d + i].
-template <typename T, int L, int R>
+template <typename T, int L, int R, bool F>
 __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit &unit, int begin, int end,
                                            const float *scores, const Running<R> &row, Area<R> *areas, float *scratch,
                                            float *partial) {
@@ -373,16 +401,17 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
     }
     int64_t place = -1;
     float t[R];
-    stream_keys<T, L>(
-        p.v.data, begin + wave * kGroup, end, waves * kGroup,
+    constexpr int G = group_keys<F>();
+    stream_keys<T, L, F>(
+        p.v.data, begin + wave * G, end, waves * G,
         [&](int from) {
-            const int mine = from + lane;
+            const int mine = from + lane % G;
             place = mine < end ? unit.key_at(p, p.v, mine) : -1;
             get<R>(scores + (int64_t)(min(mine, end - 1) - begin) * R, t);
         },
         [&](int buffer) {
             wave_sync();
-            area.from[buffer][lane] = place >= 0 ? place : 0;
+            area.from[buffer][lane] = place >= 0 ? place : 0;   // fine groups: four times over
 #pragma unroll
             for (int r = 0; r < R; ++r)
                 t[r] = real(probability(place >= 0 ? exp2_from(t[r], row.m[r]) : 0.0f, inverse[r]));
@@ -460,7 +489,7 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
 
 // A unit in one workgroup: its scores stay in LDS, followed by what the waves
 // keep of their keys and, in the same place, their outputs.
-template <typename T, int L, int R>
+template <typename T, int L, int R, bool F>
 __global__ void __launch_bounds__(whole_most_waves(R) * 64) attention_whole_kernel(const AttentionParams p) {
     extern __shared__ float4 lds[];
     __shared__ float top[kMostWaves][R], sum[kMostWaves][R];
@@ -471,13 +500,14 @@ __global__ void __launch_bounds__(whole_most_waves(R) * 64) attention_whole_kern
     float *s = reinterpret_cast<float *>(lds), *after = reinterpret_cast<float *>(lds + (p.max_kv * R + 3) / 4);
     Area<R> *areas = reinterpret_cast<Area<R> *>(after);
     Running<R> row;
-    score_keys<T, L, R>(p, unit, unit.lo + wave * kGroup, unit.hi, waves * kGroup, areas[wave],
+    constexpr int G = group_keys<F>();
+    score_keys<T, L, R, F>(p, unit, unit.lo + wave * G, unit.hi, waves * G, areas[wave],
                         [&](int key, const float (&t)[R]) {
                             row.score(t);
                             put<R>(s + (key - unit.lo) * R, t);
                         });
     row.over_group(top, sum);
-    value_keys<T, L, R>(p, unit, unit.lo, unit.hi, s, row, areas, after, nullptr);
+    value_keys<T, L, R, F>(p, unit, unit.lo, unit.hi, s, row, areas, after, nullptr);
 }
 
 // Consecutive workgroups, which go to the chip's eight dies in turn, take one
@@ -486,7 +516,7 @@ __global__ void __launch_bounds__(whole_most_waves(R) * 64) attention_whole_kern
 //
 // Long contexts, first launch: scores of one split of a unit's keys, with the
 // split's maximum and sum for each row.
-template <typename T, int L, int R>
+template <typename T, int L, int R, bool F>
 __global__ void __launch_bounds__(kThreads) attention_scores_kernel(const AttentionParams p) {
     __shared__ Area<R> areas[kThreads / 64];
     __shared__ float top[kMostWaves][R], sum[kMostWaves][R];
@@ -498,7 +528,8 @@ __global__ void __launch_bounds__(kThreads) attention_scores_kernel(const Attent
     const int wave = threadIdx.x >> 6;
     Running<R> row;
     float *scores = p.scores + (int64_t)index * p.splits * p.split_keys * R;
-    score_keys<T, L, R>(p, unit, begin + wave * kGroup, end, kThreads, areas[wave],
+    constexpr int G = group_keys<F>();
+    score_keys<T, L, R, F>(p, unit, begin + wave * G, end, kThreads / 64 * G, areas[wave],
                         [&](int key, const float (&t)[R]) {
                             row.score(t);
                             put<R>(scores + (int64_t)key * R, t);
@@ -513,7 +544,7 @@ __global__ void __launch_bounds__(kThreads) attention_scores_kernel(const Attent
 
 // Second launch: the unit's maxima and sums from all its splits', then one
 // split's part of P V.
-template <typename T, int L, int R>
+template <typename T, int L, int R, bool F>
 __global__ void __launch_bounds__(kThreads) attention_values_kernel(const AttentionParams p) {
     __shared__ Area<R> areas[kThreads / 64];
     __shared__ float scratch[kThreads / 64 * R * L * kPer<T>];
@@ -534,7 +565,7 @@ __global__ void __launch_bounds__(kThreads) attention_values_kernel(const Attent
             row.take(r, m[r], l[r]);
     }
     row.over_wave();
-    value_keys<T, L, R>(p, unit, begin, end, p.scores + ((int64_t)index * p.splits * p.split_keys + begin) * R, row,
+    value_keys<T, L, R, F>(p, unit, begin, end, p.scores + ((int64_t)index * p.splits * p.split_keys + begin) * R, row,
                         areas, scratch, p.partial + ((int64_t)index * p.splits + split) * R * p.d);
 }
 
@@ -574,37 +605,41 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(const Attentio
 
 enum Which { kWhole, kScores, kValues };
 
-template <typename T, int L, int R>
+template <typename T, int L, int R, bool F>
 hipError_t launch(Which which, const AttentionParams &p, hipStream_t stream) {
     const unsigned units = (unsigned)(p.batch * p.kv_heads * p.row_blocks);
-    const void *kernel = which == kWhole    ? (const void *)attention_whole_kernel<T, L, R>
-                         : which == kScores ? (const void *)attention_scores_kernel<T, L, R>
-                                            : (const void *)attention_values_kernel<T, L, R>;
-    const int threads = which == kWhole ? whole_waves(p.max_kv, R) * 64 : kThreads;
-    const size_t lds = which == kWhole ? (size_t)whole_lds(p.max_kv, R, L, sizeof(T) == 2) : 0;
+    const void *kernel = which == kWhole    ? (const void *)attention_whole_kernel<T, L, R, F>
+                         : which == kScores ? (const void *)attention_scores_kernel<T, L, R, F>
+                                            : (const void *)attention_values_kernel<T, L, R, F>;
+    const int threads = which == kWhole ? whole_waves(p.max_kv, R, F) * 64 : kThreads;
+    const size_t lds = which == kWhole ? (size_t)whole_lds(p.max_kv, R, L, sizeof(T) == 2, F) : 0;
     const unsigned grid = which == kWhole ? units : units * (unsigned)p.splits;
     void *args[] = {const_cast<AttentionParams *>(&p)};
     return hipLaunchKernel(kernel, dim3(grid), dim3((unsigned)threads), args, lds, stream);
 }
 
-template <typename T, int L> hipError_t for_rows(Which which, const AttentionParams &p, hipStream_t stream) {
+template <typename T, int L, bool F> hipError_t for_rows(Which which, const AttentionParams &p, hipStream_t stream) {
     switch (p.rows) {
-    case 1: return launch<T, L, 1>(which, p, stream);
-    case 2: return launch<T, L, 2>(which, p, stream);
-    case 3: return launch<T, L, 3>(which, p, stream);
-    case 4: return launch<T, L, 4>(which, p, stream);
-    case 6: return launch<T, L, 6>(which, p, stream);
-    default: return launch<T, L, 8>(which, p, stream);
+    case 1: return launch<T, L, 1, F>(which, p, stream);
+    case 2: return launch<T, L, 2, F>(which, p, stream);
+    case 3: return launch<T, L, 3, F>(which, p, stream);
+    case 4: return launch<T, L, 4, F>(which, p, stream);
+    case 6: return launch<T, L, 6, F>(which, p, stream);
+    default: return launch<T, L, 8, F>(which, p, stream);
     }
+}
+
+template <typename T, int L> hipError_t for_group(Which which, const AttentionParams &p, hipStream_t stream) {
+    return p.fine ? for_rows<T, L, true>(which, p, stream) : for_rows<T, L, false>(which, p, stream);
 }
 
 hipError_t for_type(Which which, bool bf16, int lanes, const AttentionParams &p, hipStream_t stream) {
     switch (lanes) {
-    case 4: return bf16 ? for_rows<uint16_t, 4>(which, p, stream) : for_rows<float, 4>(which, p, stream);
-    case 8: return bf16 ? for_rows<uint16_t, 8>(which, p, stream) : for_rows<float, 8>(which, p, stream);
-    case 16: return bf16 ? for_rows<uint16_t, 16>(which, p, stream) : for_rows<float, 16>(which, p, stream);
-    case 32: return bf16 ? for_rows<uint16_t, 32>(which, p, stream) : for_rows<float, 32>(which, p, stream);
-    default: return for_rows<float, 64>(which, p, stream);
+    case 4: return bf16 ? for_group<uint16_t, 4>(which, p, stream) : for_group<float, 4>(which, p, stream);
+    case 8: return bf16 ? for_group<uint16_t, 8>(which, p, stream) : for_group<float, 8>(which, p, stream);
+    case 16: return bf16 ? for_group<uint16_t, 16>(which, p, stream) : for_group<float, 16>(which, p, stream);
+    case 32: return bf16 ? for_group<uint16_t, 32>(which, p, stream) : for_group<float, 32>(which, p, stream);
+    default: return for_group<float, 64>(which, p, stream);
     }
 }
 

@@ -159,6 +159,7 @@ struct AttentionPlan {
     Form form;
     int lanes;        // lanes a key in the kernels for few rows
     int rows, row_blocks;
+    bool fine;        // few rows: waves of 16 keys
     int splits, split_keys;
     int64_t units;
     int64_t slab;     // units of one round of launches
@@ -200,10 +201,13 @@ AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool 
     a.row_blocks = (int)ceil_div(rows, a.rows);
     a.units = a.slab = heads * a.row_blocks;
     a.splits = 1;
-    // One launch where a workgroup's four waves take the keys in one go (one of
-    // 1000 keys, 16 waves: 35 us, split 21), or where the units fill the chip and
-    // their scores fit in LDS.
-    const int64_t lds = pamk::whole_lds(max_kv, a.rows, a.lanes, bf16);
+    // Waves of 16 keys where waves of 64 would leave half of the 1024 SIMDs without
+    // one (1000 keys x 8 heads of 128: 20.5 -> 16.4 us; 15006 keys x 4 units of 6 rows
+    // of 256, 940 waves of 64: 39 us, in waves of 16 52).
+    a.fine = a.units * ceil_div(max_kv, 64) <= 512;
+    // One launch for short contexts (one of 1000 keys in 16 waves: 35 us, split 21),
+    // and where the units fill the chip and their scores fit in LDS.
+    const int64_t lds = pamk::whole_lds(max_kv, a.rows, a.lanes, bf16, a.fine);
     const bool whole = (max_kv <= 256 && lds <= pamk::kWholeLds) || (a.units >= 256 && lds <= pamk::kWholeLds / 2);
     a.form = tiled ? Form::tiles : whole ? Form::whole : Form::split;
     if (a.form == Form::whole || a.units == 0)
@@ -218,9 +222,11 @@ AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool 
         const int64_t per = ceil_div(keys * a.slab * columns * waves, 4096);
         a.split_keys = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(per, 128) * 128, 128), 512);
     } else {
-        // About 1024 workgroups, of 256 to 1024 keys.
+        // About 1024 workgroups, of 256 to 1024 keys; of 64 in waves of 16.
         const int64_t keys = ceil_div((int64_t)max_kv * a.units, 1024);
         a.split_keys = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(keys, 256) * 256, 256), 1024);
+        if (a.fine)
+            a.split_keys = 64;
     }
     a.splits = (int)ceil_div(std::max(max_kv, 1), a.split_keys);
     const int64_t parts = a.slab * a.splits;
@@ -512,6 +518,7 @@ pam_status_t pam_paged_attention(const pam_paged_attention_t *args, hipStream_t 
     p.window = s.window;
     p.scale = (float)((double)s.scale * 1.4426950408889634);
     p.rows = plan.rows;
+    p.fine = plan.fine;
     p.row_blocks = plan.row_blocks;
     pamk::fast_divisor((uint32_t)p.row_blocks, p.blocks_mul, p.blocks_shift);
     pamk::fast_divisor((uint32_t)p.kv_heads, p.heads_mul, p.heads_shift);

@@ -105,6 +105,7 @@ struct AttentionParams {
     int32_t rows, row_blocks;
     uint32_t blocks_mul, blocks_shift, heads_mul, heads_shift, group_mul, group_shift;   // fast_divisor of
                                     // row_blocks, kv_heads and group
+    int32_t fine;                   // few rows: waves take 16 keys at a time, not 64
     int32_t first_unit;             // of this launch; workspaces count units from it
     int32_t splits, split_keys;     // keys of a unit: splits of split_keys (a multiple of 64)
     float *scores;                  // [unit][splits * split_keys][rows], in units of log2
@@ -114,17 +115,18 @@ struct AttentionParams {
 
 // Few rows a unit (pam_attention.hip), `lanes` lanes a key: one launch with
 // the scores in LDS, or two with the keys split.
-// The one launch's waves: of 64 keys each, 16 at most with up to 4 rows (128
-// registers a lane), else 8.
+// The one launch's waves: of 16 keys each (fine) or of 64; 16 at most with up to
+// 4 rows (128 registers a lane), else 8.
 constexpr int whole_most_waves(int rows) { return rows <= 4 ? 16 : 8; }
-inline int whole_waves(int64_t max_kv, int rows) {
-    const int64_t waves = (max_kv + 63) / 64;
+inline int whole_waves(int64_t max_kv, int rows, bool fine) {
+    const int64_t waves = (max_kv + 63) / (fine ? 16 : 64);
     return waves < 4 ? 4 : waves < whole_most_waves(rows) ? (int)waves : whole_most_waves(rows);
 }
 // Its LDS bytes: the scores, and the keys that the waves work on or, afterwards,
 // their outputs.
-inline int64_t whole_lds(int64_t max_kv, int rows, int lanes, bool bf16) {
-    const int64_t waves = whole_waves(max_kv, rows), keys = 128 * (8 + 4 * rows), out = 4 * rows * lanes * (bf16 ? 8 : 4);
+inline int64_t whole_lds(int64_t max_kv, int rows, int lanes, bool bf16, bool fine) {
+    const int64_t waves = whole_waves(max_kv, rows, fine);
+    const int64_t keys = 128 * (8 + 4 * rows), out = 4 * rows * lanes * (bf16 ? 8 : 4);
     return (4 * rows * max_kv + 15) / 16 * 16 + waves * (keys > out ? keys : out);
 }
 constexpr int64_t kWholeLds = 131072;   // at most
