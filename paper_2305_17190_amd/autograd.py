@@ -18,6 +18,9 @@ and dW likewise, through ``pam.exact_grad``.  With
 two operands to that many mantissa bits (App. "PAM with Narrower
 Mantissas"); the tensors themselves are not modified.  Inputs must be float32
 HIP tensors; there is no CPU path.
+
+``pam_norm_rope`` is the attention's norm of queries and keys with the position
+rotation (``pam.norm_rope``), ordinary arithmetic, float32 or bfloat16.
 """
 from __future__ import annotations
 
@@ -28,8 +31,10 @@ import torch
 from . import bmm as _bmm
 from . import exact_grad as _exact_grad
 from . import gemm as _gemm
+from . import norm_rope as _norm_rope
+from . import norm_rope_grad as _norm_rope_grad
 
-__all__ = ["pam_linear", "pam_matmul", "PAMLinear"]
+__all__ = ["pam_linear", "pam_matmul", "pam_norm_rope", "PAMLinear"]
 
 
 def _float32(**named) -> None:
@@ -128,6 +133,35 @@ def pam_matmul(a: torch.Tensor, b: torch.Tensor, mantissa_bits: int = 23) -> tor
     if a.dim() == 3 and b.dim() == 3:
         return _PAMBmmFn.apply(a, b, int(mantissa_bits))
     raise ValueError("pam_matmul takes two 2-D or two 3-D tensors")
+
+
+def _dense_heads(t: torch.Tensor) -> torch.Tensor:
+    return t if t is None or t.stride(-1) == 1 or t.numel() == 0 else t.contiguous()
+
+
+class _NormRopeFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved):
+        q, k = _dense_heads(q), _dense_heads(k)
+        ctx.save_for_backward(q, k, positions, cos, sin, q_weight, k_weight)
+        ctx.rest = eps, interleaved
+        return _norm_rope(q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        q, k, *rest = ctx.saved_tensors
+        gq, gk, gqw, gkw = _norm_rope_grad(_dense_heads(dq), _dense_heads(dk), q, k, *rest, *ctx.rest)
+        return gq, gk, None, None, None, gqw, gkw, None, None
+
+
+def pam_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor = None, cos: torch.Tensor = None,
+                  sin: torch.Tensor = None, q_weight: torch.Tensor = None, k_weight: torch.Tensor = None,
+                  eps: float = 1e-6, interleaved: bool = False):
+    """``pam.norm_rope`` of queries and keys (tokens, heads, d) with gradients for
+    q, k and the weights; the tables of angles are constants."""
+    if q is None or k is None:
+        raise ValueError("pam_norm_rope takes queries and keys; norm_rope takes one of them")
+    return _NormRopeFn.apply(q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved)
 
 
 class PAMLinear(torch.nn.Module):

@@ -30,25 +30,26 @@ constexpr int kPad = 4;               // words after each k step's row in LDS
 // A lane's 8 rows or columns of a 64-wide block: two groups of four.
 __device__ __forceinline__ int place(int group, int i) { return (i / 4) * 32 + group * 4 + i % 4; }
 
-// One row of a k step, eight columns; the eight integer additions stand
-// together, then the eight float ones, so that neighbours are independent and
-// pair up with another wave's.  Plain: both encodings' exponent fields lie in
-// [64, 190], so a + b' is the encoding of their PAM itself.
-__device__ __forceinline__ void plain_row(float (&c)[8], uint32_t b, const uint32_t (&a)[8]) {
-    uint32_t t0, t1, t2, t3, t4, t5, t6, t7;
+// One row of two k steps, four columns; equal instructions stand together, so
+// that neighbours are independent and pair up with another wave's.  Plain: all
+// encodings' exponent fields lie in [64, 190], so a + b' is the encoding of their
+// PAM itself.  The two steps' terms are added to each other first: no instruction
+// more, and half as many roundings of the long sum.
+__device__ __forceinline__ void plain_pair(float &c0, float &c1, float &c2, float &c3, uint32_t b, uint32_t d,
+                                           const uint32_t (&a)[4], const uint32_t (&e)[4]) {
+    uint32_t t0, t1, t2, t3, u0, u1, u2, u3;
     asm("v_add_u32 %[t0], %[a0], %[b]\n\tv_add_u32 %[t1], %[a1], %[b]\n\t"
         "v_add_u32 %[t2], %[a2], %[b]\n\tv_add_u32 %[t3], %[a3], %[b]\n\t"
-        "v_add_u32 %[t4], %[a4], %[b]\n\tv_add_u32 %[t5], %[a5], %[b]\n\t"
-        "v_add_u32 %[t6], %[a6], %[b]\n\tv_add_u32 %[t7], %[a7], %[b]\n\t"
+        "v_add_u32 %[u0], %[e0], %[d]\n\tv_add_u32 %[u1], %[e1], %[d]\n\t"
+        "v_add_u32 %[u2], %[e2], %[d]\n\tv_add_u32 %[u3], %[e3], %[d]\n\t"
+        "v_add_f32 %[t0], %[t0], %[u0]\n\tv_add_f32 %[t1], %[t1], %[u1]\n\t"
+        "v_add_f32 %[t2], %[t2], %[u2]\n\tv_add_f32 %[t3], %[t3], %[u3]\n\t"
         "v_add_f32 %[c0], %[c0], %[t0]\n\tv_add_f32 %[c1], %[c1], %[t1]\n\t"
-        "v_add_f32 %[c2], %[c2], %[t2]\n\tv_add_f32 %[c3], %[c3], %[t3]\n\t"
-        "v_add_f32 %[c4], %[c4], %[t4]\n\tv_add_f32 %[c5], %[c5], %[t5]\n\t"
-        "v_add_f32 %[c6], %[c6], %[t6]\n\tv_add_f32 %[c7], %[c7], %[t7]"
-        : [c0] "+v"(c[0]), [c1] "+v"(c[1]), [c2] "+v"(c[2]), [c3] "+v"(c[3]), [c4] "+v"(c[4]), [c5] "+v"(c[5]),
-          [c6] "+v"(c[6]), [c7] "+v"(c[7]), [t0] "=&v"(t0), [t1] "=&v"(t1), [t2] "=&v"(t2), [t3] "=&v"(t3),
-          [t4] "=&v"(t4), [t5] "=&v"(t5), [t6] "=&v"(t6), [t7] "=&v"(t7)
-        : [b] "v"(b), [a0] "v"(a[0]), [a1] "v"(a[1]), [a2] "v"(a[2]), [a3] "v"(a[3]), [a4] "v"(a[4]), [a5] "v"(a[5]),
-          [a6] "v"(a[6]), [a7] "v"(a[7]));
+        "v_add_f32 %[c2], %[c2], %[t2]\n\tv_add_f32 %[c3], %[c3], %[t3]"
+        : [c0] "+v"(c0), [c1] "+v"(c1), [c2] "+v"(c2), [c3] "+v"(c3), [t0] "=&v"(t0), [t1] "=&v"(t1), [t2] "=&v"(t2),
+          [t3] "=&v"(t3), [u0] "=&v"(u0), [u1] "=&v"(u1), [u2] "=&v"(u2), [u3] "=&v"(u3)
+        : [b] "v"(b), [d] "v"(d), [a0] "v"(a[0]), [a1] "v"(a[1]), [a2] "v"(a[2]), [a3] "v"(a[3]), [e0] "v"(e[0]),
+          [e1] "v"(e[1]), [e2] "v"(e[2]), [e3] "v"(e[3]));
 }
 
 // acc[r][c] += b[k][row r] .^ a[k][column c] over one chunk in LDS: `plain` or,
@@ -67,14 +68,18 @@ __device__ __forceinline__ void chunk_product(const uint32_t *a, const uint32_t 
     int first = __builtin_amdgcn_readfirstlane(plain ? kStep : 0);
     asm("" : "+s"(first));
     for (int k = 0; k < first; k += 2) {
+        uint32_t z[2][8];
+        read(b + k * (BM + kPad) + row, z[0]);
+        read(b + (k + 1) * (BM + kPad) + row, z[1]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            uint32_t x[8], z[8];
-            read(a + (k + h) * (BN + kPad) + col, x);
-            read(b + (k + h) * (BM + kPad) + row, z);
+            uint32_t x[2][4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                *reinterpret_cast<uint4 *>(x[i]) = *reinterpret_cast<const uint4 *>(a + (k + i) * (BN + kPad) + col + 32 * h);
 #pragma unroll
             for (int r = 0; r < 8; ++r)
-                plain_row(acc[r], z[r], x);
+                plain_pair(acc[r][4 * h], acc[r][4 * h + 1], acc[r][4 * h + 2], acc[r][4 * h + 3], z[0][r], z[1][r], x[0], x[1]);
         }
     }
 #pragma unroll 1
@@ -413,7 +418,7 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
     constexpr int VK = NT / (BN / E);              // and between its value items
     constexpr bool VB = sizeof(T) == 2;
     __shared__ Buffers<BM, BN, 2> buf;
-    __shared__ float row_max[BM], row_sum[BM];
+    __shared__ float row_max[BM], row_sum[BM], row_inverse[BM];
     extern __shared__ int64_t from[];              // the split's keys, -1: none
 
     const int dtiles = (p.d + BN - 1) / BN;
@@ -433,14 +438,32 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
     const int tiles = p.splits * (p.split_keys / kTile);
     const float *stats = p.stats + (int64_t)index * tiles * 2 * BM;
     const int first = unit.lo / kTile, last = unit.hi > unit.lo ? (unit.hi - 1) / kTile : first - 1;
-    for (int r = tid; r < BM; r += NT) {
+    {
+        // WN lanes a row, each every WN-th tile, joined through LDS.
+        const int r = tid % BM, part = tid / BM;
         float m = kNegInf, l = 0.0f;
-        for (int t = first; t <= last; ++t)
-            m = fmaxf(m, stats[(int64_t)t * 2 * BM + r]);
-        for (int t = first; t <= last; ++t)
-            l += stats[(int64_t)t * 2 * BM + BM + r] * exp2_from(stats[(int64_t)t * 2 * BM + r], m);
-        row_max[r] = m == kNegInf ? 0.0f : m;
-        row_sum[r] = l;
+#pragma unroll 4
+        for (int t = first + part; t <= last; t += WN) {
+            const float top = stats[(int64_t)t * 2 * BM + r], sum = stats[(int64_t)t * 2 * BM + BM + r];
+            const float to = fmaxf(m, top);
+            l = l * exp2_from(m, to) + sum * exp2_from(top, to);
+            m = to;
+        }
+        if (part > 0) {
+            row_max[r] = m;
+            row_sum[r] = l;
+        }
+        __syncthreads();
+        if (part == 0) {
+            if constexpr (WN == 2) {
+                const float to = fmaxf(m, row_max[r]);
+                l = l * exp2_from(m, to) + row_sum[r] * exp2_from(row_max[r], to);
+                m = to;
+            }
+            row_max[r] = m == kNegInf ? 0.0f : m;
+            row_sum[r] = l;
+            row_inverse[r] = r >= unit.rows ? 1.0f : l > 0.0f ? 1.0f / l : 0.0f;
+        }
     }
     const int start = begin / kStep * kStep;
     for (int j = tid; j < p.split_keys; j += NT) {
@@ -451,14 +474,6 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
         buf.odd[tid] = 0;
     __syncthreads();
     const int my_row = tid % (BM / 4) * 4;
-    float m4[4], inverse4[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        m4[i] = row_max[my_row + i];
-        const float l = row_sum[my_row + i];
-        inverse4[i] = my_row + i >= unit.rows ? 1.0f : l > 0.0f ? 1.0f / l : 0.0f;
-    }
-
     const float *scores = p.scores + (int64_t)index * tiles * kTile * BM;
     const int col = tid % (BN / E) * E, column = col_tile * BN + col;
     // Columns that do not exist hold ones, as rows do.
@@ -484,6 +499,9 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
         uint32_t *a = buf.a[chunk % buf.kCount], *b = buf.b[chunk % buf.kCount];
         Odd odd;
         float least = 1.0f;
+        const float4 m4 = *reinterpret_cast<const float4 *>(row_max + my_row);
+        const float4 inverse4 = *reinterpret_cast<const float4 *>(row_inverse + my_row);
+        const float top[4] = {m4.x, m4.y, m4.z, m4.w}, inverse[4] = {inverse4.x, inverse4.y, inverse4.z, inverse4.w};
 #pragma unroll
         for (int i = 0; i < SI; ++i) {
             const int k = tid / (BM / 4) + i * SK;
@@ -491,7 +509,7 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
             uint32_t x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float pr = __builtin_amdgcn_exp2f(t[e] - m4[e]) * inverse4[e];
+                const float pr = __builtin_amdgcn_exp2f(t[e] - top[e]) * inverse[e];
                 least = fminf(least, pr);
                 x[e] = __float_as_uint(pr) - kBias;
             }
