@@ -409,7 +409,7 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
 }
 
 template <typename T, int WM, int WN>
-__global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(4, 4))) tile_values_kernel(const AttentionParams p) {
+__global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(WM * WN == 1 ? 2 : 4, WM * WN == 1 ? 2 : 4))) tile_values_kernel(const AttentionParams p) {
     constexpr int BM = 64 * WM, BN = 64 * WN, NT = 64 * WM * WN;
     constexpr int E = kPer<T>;
     constexpr int SI = kStep * BM / 4 / NT;        // score items of 4 rows a lane and chunk
