@@ -85,13 +85,13 @@ typedef struct {
  */
 typedef struct {
     const void *q_in;
-    void *q_out;
     const float *q_weight;
     const void *k_in;
-    void *k_out;
     const float *k_weight;
     const int32_t *positions;
     const float *cos, *sin;
+    void *q_out;
+    void *k_out;
     pam_heads_t q_in_heads, q_out_heads, k_in_heads, k_out_heads;
     pam_rotation_t rotation;
     int64_t tokens;
@@ -117,15 +117,15 @@ typedef struct {
     const void *q_in;
     const float *q_weight;
     const void *dq_out;
-    void *dq_in;
-    float *dq_weight;
     const void *k_in;
     const float *k_weight;
     const void *dk_out;
-    void *dk_in;
-    float *dk_weight;
     const int32_t *positions;
     const float *cos, *sin;
+    void *dq_in;
+    float *dq_weight;
+    void *dk_in;
+    float *dk_weight;
     void *workspace;
     pam_heads_t q_in_heads, dq_out_heads, dq_in_heads, k_in_heads, dk_out_heads, dk_in_heads;
     pam_rotation_t rotation;
@@ -156,12 +156,12 @@ typedef struct {
     const void *v;
     const void *q_in;
     const float *q_weight;
-    void *q_out;
-    void *k_cache;
-    void *v_cache;
     const int64_t *slots;
     const int32_t *positions;
     const float *cos, *sin;
+    void *k_cache;             /* written */
+    void *v_cache;
+    void *q_out;
     pam_heads_t k_heads, v_heads, q_in_heads, q_out_heads;
     pam_cache_t k_cache_layout, v_cache_layout;
     pam_rotation_t rotation;
@@ -203,10 +203,10 @@ pam_status_t pam_append_kv(const pam_append_kv_t *args, hipStream_t stream);
 typedef struct {
     const void *q;
     const void *k_cache, *v_cache;
-    float *out;
     const int32_t *q_starts;   /* batch + 1, or NULL */
     const int32_t *kv_lens;    /* batch */
     const int32_t *table;      /* batch rows of table_width entries */
+    float *out;
     void *workspace;
     pam_heads_t q_heads, out_heads;
     pam_cache_t k_cache_layout, v_cache_layout;

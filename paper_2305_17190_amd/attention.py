@@ -22,7 +22,7 @@ import ctypes
 import math
 import struct
 
-from . import _check, _launch, _require, _same_device, _torch, load
+from . import PamError, _check, _launch, _require, _same_device, _torch, load
 
 __all__ = ["norm_rope", "norm_rope_grad", "append_kv", "paged_attention"]
 
@@ -132,29 +132,38 @@ def _head_tensors(*named):
 # pointers, and what else the call needs.  (Checked anew, each call of
 # append_kv took 21 us of host time, of paged_attention 15.)
 _calls = {}
+_pack_tensors = None
 
 
-def _sig(t):
-    return None if t is None else (t.dtype, t.shape, t.stride(), t.get_device())
+def _pack(*tensors):
+    """(key, addresses) of the tensors (``csrc/python/pack.cpp``); None where one is none."""
+    global _pack_tensors
+    if _pack_tensors is None:
+        _torch()                                     # whose libraries _pack.so links
+        try:
+            from . import _pack as module
+        except ImportError as e:
+            raise PamError(f"_pack.so is missing: build it with `python -m paper_2305_17190_amd.build` ({e})") from e
+        _pack_tensors = module.pack
+    return _pack_tensors(*tensors)
 
 
-def _known(key, plan):
-    """The call's plan: plan() checks the arguments and makes it."""
-    try:
-        return _calls[key]
-    except KeyError:
-        made = plan()
+def _known(key, plan, *args):
+    """The call's plan: plan(*args) checks the arguments and makes it."""
+    made = _calls.get(key)
+    if made is None:
+        made = plan(*args)
         if len(_calls) >= 4096:
             _calls.clear()
         _calls[key] = made
-        return made
+    return made
 
 
 def _ptr(t):
     return 0 if t is None else t.data_ptr()
 
 
-_norm_rope_ptrs = struct.Struct("9Q").pack
+_norm_rope_outs = struct.Struct("2Q").pack
 
 
 def _norm_rope_plan(q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved, out_dtype):
@@ -191,23 +200,21 @@ def norm_rope(q, k, positions=None, cos=None, sin=None, q_weight=None, k_weight=
         q_weight = None
     if k is None:
         k_weight = None
-    try:
-        key = (0, _sig(q), _sig(k), _sig(positions), _sig(cos), _sig(sin), _sig(q_weight), _sig(k_weight), eps,
-               interleaved, out_dtype)
-    except AttributeError:
-        key = None
+    packed = (_pack_tensors or _pack)(q, q_weight, k, k_weight, positions, cos, sin)
     args = (q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved, out_dtype)
-    tail, dtype = _norm_rope_plan(*args) if key is None else _known(key, lambda: _norm_rope_plan(*args))
+    if packed is None:
+        _norm_rope_plan(*args)                       # says which argument is none
+        raise TypeError("norm_rope takes dense tensors")
+    tail, dtype = _known((0, packed[0], eps, interleaved, out_dtype), _norm_rope_plan, *args)
     empty = _torch().empty
     ref = q if q is not None else k
-    qo, ko = (None if t is None else empty(t.shape, dtype=dtype, device=ref.device) for t in (q, k))
-    _launch(ref, (_bound or _library()).pam_norm_rope, _norm_rope_ptrs(
-        _ptr(q), _ptr(qo), _ptr(q_weight), _ptr(k), _ptr(ko), _ptr(k_weight), _ptr(positions), _ptr(cos), _ptr(sin))
-        + tail)
+    device = ref.device
+    qo, ko = (None if t is None else empty(t.shape, dtype=dtype, device=device) for t in (q, k))
+    _launch(ref, (_bound or _library()).pam_norm_rope, packed[1] + _norm_rope_outs(_ptr(qo), _ptr(ko)) + tail)
     return qo, ko
 
 
-_norm_rope_grad_ptrs = struct.Struct("14Q").pack
+_norm_rope_grad_outs = struct.Struct("5Q").pack
 
 
 def _norm_rope_grad_plan(dq, dk, q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved):
@@ -246,21 +253,19 @@ def norm_rope_grad(dq, dk, q, k, positions=None, cos=None, sin=None, q_weight=No
         q_weight = None
     if k is None:
         k_weight = None
-    try:
-        key = (1, _sig(dq), _sig(dk), _sig(q), _sig(k), _sig(positions), _sig(cos), _sig(sin), _sig(q_weight),
-               _sig(k_weight), eps, interleaved)
-    except AttributeError:
-        key = None
+    packed = (_pack_tensors or _pack)(q, q_weight, dq, k, k_weight, dk, positions, cos, sin)
     args = (dq, dk, q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved)
-    tail, nbytes = _norm_rope_grad_plan(*args) if key is None else _known(key, lambda: _norm_rope_grad_plan(*args))
+    if packed is None:
+        _norm_rope_grad_plan(*args)
+        raise TypeError("norm_rope_grad takes dense tensors")
+    tail, nbytes = _known((1, packed[0], eps, interleaved), _norm_rope_grad_plan, *args)
     ref = q if q is not None else k
     empty, device = torch.empty, ref.device
     gq, gk = (None if t is None else empty(t.shape, dtype=t.dtype, device=device) for t in (q, k))
     gqw, gkw = (None if w is None else empty(w.shape, dtype=w.dtype, device=device) for w in (q_weight, k_weight))
     keep = empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-    _launch(ref, (_bound or _library()).pam_norm_rope_grad, _norm_rope_grad_ptrs(
-        _ptr(q), _ptr(q_weight), _ptr(dq), _ptr(gq), _ptr(gqw), _ptr(k), _ptr(k_weight), _ptr(dk), _ptr(gk), _ptr(gkw),
-        _ptr(positions), _ptr(cos), _ptr(sin), _ptr(keep)) + tail)
+    _launch(ref, (_bound or _library()).pam_norm_rope_grad,
+            packed[1] + _norm_rope_grad_outs(_ptr(gq), _ptr(gqw), _ptr(gk), _ptr(gkw), _ptr(keep)) + tail)
     del keep
     return gq, gk, gqw, gkw
 
@@ -273,7 +278,7 @@ def _caches(k_cache, v_cache):
     _same_device(k_cache, ("v_cache", v_cache))
 
 
-_append_ptrs = struct.Struct("12Q").pack
+_append_outs = struct.Struct("Q").pack
 
 
 def _append_plan(k, v, k_cache, v_cache, slots, positions, cos, sin, k_weight, q, q_weight, eps, interleaved):
@@ -306,17 +311,14 @@ def append_kv(k, v, k_cache, v_cache, slots, positions=None, cos=None, sin=None,
     eps, interleaved = float(eps), bool(interleaved)
     if q is None:
         q_weight = None
+    packed = (_pack_tensors or _pack)(k, k_weight, v, q, q_weight, slots, positions, cos, sin, k_cache, v_cache)
     args = (k, v, k_cache, v_cache, slots, positions, cos, sin, k_weight, q, q_weight, eps, interleaved)
-    try:
-        key = (2, _sig(k), _sig(v), _sig(k_cache), _sig(v_cache), _sig(slots), _sig(positions), _sig(cos), _sig(sin),
-               _sig(k_weight), _sig(q), _sig(q_weight), eps, interleaved)
-    except AttributeError:
-        key = None
-    tail = _append_plan(*args) if key is None else _known(key, lambda: _append_plan(*args))
+    if packed is None:
+        _append_plan(*args)
+        raise TypeError("append_kv takes dense tensors")
+    tail = _known((2, packed[0], eps, interleaved), _append_plan, *args)
     qo = None if q is None else _torch().empty(q.shape, dtype=q.dtype, device=q.device)
-    _launch(k, (_bound or _library()).pam_append_kv, _append_ptrs(
-        _ptr(k), _ptr(k_weight), _ptr(v), _ptr(q), _ptr(q_weight), _ptr(qo), _ptr(k_cache), _ptr(v_cache), _ptr(slots),
-        _ptr(positions), _ptr(cos), _ptr(sin)) + tail)
+    _launch(k, (_bound or _library()).pam_append_kv, packed[1] + _append_outs(_ptr(qo)) + tail)
     return qo
 
 
@@ -336,7 +338,7 @@ def _attention_workspace(sizes: tuple) -> int:
     return nbytes
 
 
-_attention_ptrs, _attention_end = struct.Struct("8Q").pack, struct.Struct("=iiq").pack
+_attention_outs, _attention_end = struct.Struct("2Q").pack, struct.Struct("=iiq").pack
 
 
 def _attention_plan(q, k_cache, v_cache, table, kv_lens, q_starts, scale, causal, window, out):
@@ -389,22 +391,21 @@ def paged_attention(q, k_cache, v_cache, table, kv_lens, q_starts=None, max_q: i
     where that is positive; a token without keys gets zeros.  ``scale`` is 1 /
     sqrt(d) if not given.  Tokens of no sequence are left unwritten."""
     causal, window, scale = bool(causal), int(window), None if scale is None else float(scale)
+    packed = (_pack_tensors or _pack)(q, k_cache, v_cache, q_starts, kv_lens, table, out)
     args = (q, k_cache, v_cache, table, kv_lens, q_starts, scale, causal, window, out)
-    try:
-        key = (3, _sig(q), _sig(k_cache), _sig(v_cache), _sig(table), _sig(kv_lens), _sig(q_starts), scale, causal,
-               window, _sig(out))
-    except AttributeError:
-        key = None
-    tail, sizes, reach = _attention_plan(*args) if key is None else _known(key, lambda: _attention_plan(*args))
+    if packed is None:
+        _attention_plan(*args)
+        raise TypeError("paged_attention takes dense tensors")
+    tail, sizes, reach = _known((3, packed[0], scale, causal, window), _attention_plan, *args)
     torch = _torch()
     max_q = 1 if q_starts is None else int(max_q)
     max_kv = reach if max_kv is None else int(max_kv)
     nbytes = _attention_workspace((*sizes, max_q, max_kv))
+    device = q.device
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
-    keep = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
-    _launch(q, (_bound or _library()).pam_paged_attention, _attention_ptrs(
-        _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(q_starts), _ptr(kv_lens), _ptr(table), _ptr(keep))
-        + tail + _attention_end(max_q, max_kv, nbytes))
+        out = torch.empty(q.shape, dtype=torch.float32, device=device)
+    keep = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    _launch(q, (_bound or _library()).pam_paged_attention, packed[1][:-8] + _attention_outs(out.data_ptr(), _ptr(keep))
+            + tail + _attention_end(max_q, max_kv, nbytes))
     del keep
     return out

@@ -4,15 +4,18 @@
 
 compiles csrc/*.hip and csrc/*.cpp with hipcc into paper_2305_17190_amd/libpam.so,
 one object per source (the matrix product kernels in PARTS of their source),
-several at a time.
+several at a time; and csrc/python/pack.cpp with g++ into _pack.so, the part of
+the Python binding that reads torch tensors.
 """
 from __future__ import annotations
 
 import concurrent.futures
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -20,6 +23,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libpam.so")
+PACK = os.path.join(PKG, "_pack.so")
 
 # Device code: gfx950 only; float32 denormals flushed (the GEMM relies on the
 # accumulate treating denormal encodings as zero); no packed-fp32 VALU ops.
@@ -53,7 +57,21 @@ def _run(cmd, verbose: bool) -> None:
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("hipcc failed to build libpam.so")
+        raise RuntimeError(f"{os.path.basename(cmd[0])} failed to build the PAM library")
+
+
+def _build_pack(verbose: bool) -> None:
+    """_pack.so, against the headers and libraries of the installed torch (found
+    without importing it)."""
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    includes = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+                os.path.join(os.path.dirname(os.path.dirname(hipcc())), "include")]
+    tmp = f"{PACK}.{os.getpid()}.tmp"
+    _run(["g++", "-O2", "-std=c++17", "-w", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+          "-I", sysconfig.get_paths()["include"], *(x for path in includes for x in ("-isystem", path)),
+          os.path.join(CSRC, "python", "pack.cpp"), "-o", tmp, "-L", os.path.join(torch, "lib"), "-ltorch_python",
+          "-ltorch_cpu", "-ltorch", "-lc10"], verbose)
+    os.replace(tmp, PACK)
 
 
 def build(verbose: bool = False, extra_flags=()) -> str:
@@ -67,7 +85,8 @@ def build(verbose: bool = False, extra_flags=()) -> str:
                 define = [f"-DPAM_GEMM_PART={part}"] if name in PARTS else []
                 jobs.append(([*flags, *define, "-I", INCLUDE, "-I", CSRC, "-c", src, "-o", obj], obj))
         with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
-            for done in [pool.submit(_run, cmd, verbose) for cmd, _ in jobs]:
+            pack = pool.submit(_build_pack, verbose)
+            for done in [pool.submit(_run, cmd, verbose) for cmd, _ in jobs] + [pack]:
                 done.result()
         tmp = f"{LIB}.{os.getpid()}.tmp"   # per process: concurrent builds never see a partial file
         _run([*flags, "-shared", *(obj for _, obj in jobs), "-o", tmp, "-lhsa-runtime64"], verbose)

@@ -75,7 +75,7 @@ I32, I64, F32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 
 
 def norm_rope(lib, **kw):
-    return call(lib, "pam_norm_rope", ["q_in", "q_out", "q_weight", "k_in", "k_out", "k_weight", "positions", "cos", "sin"],
+    return call(lib, "pam_norm_rope", ["q_in", "q_weight", "k_in", "k_weight", "positions", "cos", "sin", "q_out", "k_out"],
                 [(n, Heads, heads()) for n in ("q_in_heads", "q_out_heads", "k_in_heads", "k_out_heads")]
                 + [("rotation", Rotation, rotation()), ("tokens", I64, 4), ("d", I32, 64), ("eps", F32, 1e-6)], **kw)
 
@@ -113,8 +113,8 @@ def test_nothing_to_do_launches_nothing(lib):
 
 def grad(lib, **kw):
     return call(lib, "pam_norm_rope_grad",
-                ["q_in", "q_weight", "dq_out", "dq_in", "dq_weight", "k_in", "k_weight", "dk_out", "dk_in", "dk_weight",
-                 "positions", "cos", "sin", "workspace"],
+                ["q_in", "q_weight", "dq_out", "k_in", "k_weight", "dk_out", "positions", "cos", "sin", "dq_in", "dq_weight",
+                 "dk_in", "dk_weight", "workspace"],
                 [(n + "_heads", Heads, heads()) for n in ("q_in", "dq_out", "dq_in", "k_in", "dk_out", "dk_in")]
                 + [("rotation", Rotation, rotation()), ("tokens", I64, 4), ("workspace_bytes", I64, 1 << 30),
                    ("d", I32, 64), ("eps", F32, 1e-6)], **kw)
@@ -147,8 +147,7 @@ def test_grad_workspace_sizes(lib):
 
 def append(lib, **kw):
     return call(lib, "pam_append_kv",
-                ["k", "k_weight", "v", "q_in", "q_weight", "q_out", "k_cache", "v_cache", "slots", "positions", "cos",
-                 "sin"],
+                ["k", "k_weight", "v", "q_in", "q_weight", "slots", "positions", "cos", "sin", "k_cache", "v_cache", "q_out"],
                 [(n, Heads, heads()) for n in ("k_heads", "v_heads", "q_in_heads", "q_out_heads")]
                 + [("k_cache_layout", Cache, cache()), ("v_cache_layout", Cache, cache()),
                    ("rotation", Rotation, rotation()), ("tokens", I64, 4), ("d", I32, 64), ("eps", F32, 1e-6)], **kw)
@@ -170,7 +169,7 @@ def test_append_refuses(lib, kw):
 
 def attention(lib, **kw):
     return call(lib, "pam_paged_attention",
-                ["q", "k_cache", "v_cache", "out", "q_starts", "kv_lens", "table", "workspace"],
+                ["q", "k_cache", "v_cache", "q_starts", "kv_lens", "table", "out", "workspace"],
                 [("q_heads", Heads, heads()), ("out_heads", Heads, heads()), ("k_cache_layout", Cache, cache()),
                  ("v_cache_layout", Cache, cache()), ("table_stride", I64, 1250), ("tokens", I64, 40), ("d", I32, 64),
                  ("batch", I32, 4), ("table_width", I32, 1250), ("causal", I32, 1), ("window", I32, 0),
