@@ -3,12 +3,13 @@
 // scores between them in a workspace.
 //
 // A unit is 64 WM rows of one key head (its query heads times the new tokens);
-// a wave owns a 64 x 64 block of outputs, a lane 8 x 8 of them, and each k step
-// of a tile is 64 times one integer addition and one float fma a lane (see
-// pam_attention_device.h for the encodings): keys or values as two planes (1 +
-// M and the power of two), queries or probabilities as one, all staged into
-// LDS a chunk of 16 k steps at a time, transposed to k-major, while the next
-// chunk is on its way into registers.
+// a wave owns a 64 x 64 block of outputs, a lane 8 x 8 of them.  Both operands
+// are staged into LDS a chunk of 16 k steps at a time, k-major, while the next
+// chunk is on its way into registers: keys or values as they are, queries or
+// probabilities less one bias.  Where no element of a chunk is zero, tiny or
+// huge, a term is two additions, one of integers and one of floats; else the
+// chunk's terms take the form of pam_attention_device.h, an integer addition and
+// a float fma, with 1 + M and the power of two taken apart each k step.
 //
 // Scores first: a tile of 64 WM rows and 64 WN keys goes to the workspace
 // key-major, with each row's maximum and sum of exponentials over the tile;
@@ -17,7 +18,10 @@
 // split's keys.  Storing a score costs 8 bytes of traffic, scoring again d
 // PAM-MACs, which take several times as long.
 //
-// Bound by the vector ALU: 2 lane-ops a PAM-MAC.
+// Bound by the vector ALU: 2 lane-ops a PAM-MAC, issued in pairs from four waves a
+// SIMD.  512 tokens x 32 heads of 128 over 4096 keys (8 key heads, bfloat16): 660 us,
+// 24.4 T PAM-MAC/s, 25.2 T without the join's 22 us (the framework's matrix product
+// on such operands: 30.8 T); the causal mask cuts 1% off what the tiles compute.
 
 #include "pam_attention_device.h"
 
