@@ -132,19 +132,19 @@ def _head_tensors(*named):
 # pointers, and what else the call needs.  (Checked anew, each call of
 # append_kv took 21 us of host time, of paged_attention 15.)
 _calls = {}
-_pack_tensors = None
+_pack_tensors = _make = None                         # of csrc/python/pack.cpp
 
 
 def _pack(*tensors):
-    """(key, addresses) of the tensors (``csrc/python/pack.cpp``); None where one is none."""
-    global _pack_tensors
+    """(key, addresses) of the tensors; None where one is none."""
+    global _pack_tensors, _make
     if _pack_tensors is None:
         _torch()                                     # whose libraries _pack.so links
         try:
             from . import _pack as module
         except ImportError as e:
             raise PamError(f"_pack.so is missing: build it with `python -m paper_2305_17190_amd.build` ({e})") from e
-        _pack_tensors = module.pack
+        _pack_tensors, _make = module.pack, module.make
     return _pack_tensors(*tensors)
 
 
@@ -157,13 +157,6 @@ def _known(key, plan, *args):
             _calls.clear()
         _calls[key] = made
     return made
-
-
-def _ptr(t):
-    return 0 if t is None else t.data_ptr()
-
-
-_norm_rope_outs = struct.Struct("2Q").pack
 
 
 def _norm_rope_plan(q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved, out_dtype):
@@ -181,7 +174,7 @@ def _norm_rope_plan(q, k, positions, cos, sin, q_weight, k_weight, eps, interlea
     outs = [_NONE if t is None else (t.shape[1] * d, d, t.shape[1], int(dtype == torch.bfloat16)) for t in (q, k)]
     tail = struct.pack("=" + _HEADS * 4 + _ROTATION + "qif", *_heads(q), *outs[0], *_heads(k), *outs[1], *rot, tokens, d,
                        eps)
-    return tail, dtype
+    return tail, int(dtype == torch.bfloat16)
 
 
 def norm_rope(q, k, positions=None, cos=None, sin=None, q_weight=None, k_weight=None, eps: float = 1e-6,
@@ -205,16 +198,10 @@ def norm_rope(q, k, positions=None, cos=None, sin=None, q_weight=None, k_weight=
     if packed is None:
         _norm_rope_plan(*args)                       # says which argument is none
         raise TypeError("norm_rope takes dense tensors")
-    tail, dtype = _known((0, packed[0], eps, interleaved, out_dtype), _norm_rope_plan, *args)
-    empty = _torch().empty
-    ref = q if q is not None else k
-    device = ref.device
-    qo, ko = (None if t is None else empty(t.shape, dtype=dtype, device=device) for t in (q, k))
-    _launch(ref, (_bound or _library()).pam_norm_rope, packed[1] + _norm_rope_outs(_ptr(qo), _ptr(ko)) + tail)
+    tail, bf16 = _known((0, packed[0], eps, interleaved, out_dtype), _norm_rope_plan, *args)
+    qo, ko, _, outs = _make(bf16, 0, q, k)
+    _launch(q if q is not None else k, (_bound or _library()).pam_norm_rope, packed[1] + outs[:-8] + tail)
     return qo, ko
-
-
-_norm_rope_grad_outs = struct.Struct("5Q").pack
 
 
 def _norm_rope_grad_plan(dq, dk, q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved):
@@ -247,7 +234,6 @@ def norm_rope_grad(dq, dk, q, k, positions=None, cos=None, sin=None, q_weight=No
     """Gradient of ``norm_rope``: from the gradients (dq, dk) of its outputs and
     its inputs, (gradient of q, of k, of q_weight, of k_weight); None for what
     was not given.  Gradients have their input's type, the weights' float32."""
-    torch = _torch()
     eps, interleaved = float(eps), bool(interleaved)
     if q is None:
         q_weight = None
@@ -259,13 +245,8 @@ def norm_rope_grad(dq, dk, q, k, positions=None, cos=None, sin=None, q_weight=No
         _norm_rope_grad_plan(*args)
         raise TypeError("norm_rope_grad takes dense tensors")
     tail, nbytes = _known((1, packed[0], eps, interleaved), _norm_rope_grad_plan, *args)
-    ref = q if q is not None else k
-    empty, device = torch.empty, ref.device
-    gq, gk = (None if t is None else empty(t.shape, dtype=t.dtype, device=device) for t in (q, k))
-    gqw, gkw = (None if w is None else empty(w.shape, dtype=w.dtype, device=device) for w in (q_weight, k_weight))
-    keep = empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-    _launch(ref, (_bound or _library()).pam_norm_rope_grad,
-            packed[1] + _norm_rope_grad_outs(_ptr(gq), _ptr(gqw), _ptr(gk), _ptr(gkw), _ptr(keep)) + tail)
+    gq, gqw, gk, gkw, keep, outs = _make(-1, nbytes, q, q_weight, k, k_weight)
+    _launch(q if q is not None else k, (_bound or _library()).pam_norm_rope_grad, packed[1] + outs + tail)
     del keep
     return gq, gk, gqw, gkw
 
@@ -276,9 +257,6 @@ def _caches(k_cache, v_cache):
     if k_cache.shape != v_cache.shape:
         raise ValueError(f"the caches differ in shape: {tuple(k_cache.shape)} and {tuple(v_cache.shape)}")
     _same_device(k_cache, ("v_cache", v_cache))
-
-
-_append_outs = struct.Struct("Q").pack
 
 
 def _append_plan(k, v, k_cache, v_cache, slots, positions, cos, sin, k_weight, q, q_weight, eps, interleaved):
@@ -317,8 +295,8 @@ def append_kv(k, v, k_cache, v_cache, slots, positions=None, cos=None, sin=None,
         _append_plan(*args)
         raise TypeError("append_kv takes dense tensors")
     tail = _known((2, packed[0], eps, interleaved), _append_plan, *args)
-    qo = None if q is None else _torch().empty(q.shape, dtype=q.dtype, device=q.device)
-    _launch(k, (_bound or _library()).pam_append_kv, packed[1] + _append_outs(_ptr(qo)) + tail)
+    qo, _, outs = _make(-1, 0, q)
+    _launch(k, (_bound or _library()).pam_append_kv, packed[1] + outs[:-8] + tail)
     return qo
 
 
@@ -338,7 +316,7 @@ def _attention_workspace(sizes: tuple) -> int:
     return nbytes
 
 
-_attention_outs, _attention_end = struct.Struct("2Q").pack, struct.Struct("=iiq").pack
+_attention_end = struct.Struct("=iiq").pack
 
 
 def _attention_plan(q, k_cache, v_cache, table, kv_lens, q_starts, scale, causal, window, out):
@@ -397,15 +375,15 @@ def paged_attention(q, k_cache, v_cache, table, kv_lens, q_starts=None, max_q: i
         _attention_plan(*args)
         raise TypeError("paged_attention takes dense tensors")
     tail, sizes, reach = _known((3, packed[0], scale, causal, window), _attention_plan, *args)
-    torch = _torch()
     max_q = 1 if q_starts is None else int(max_q)
     max_kv = reach if max_kv is None else int(max_kv)
     nbytes = _attention_workspace((*sizes, max_q, max_kv))
-    device = q.device
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32, device=device)
-    keep = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-    _launch(q, (_bound or _library()).pam_paged_attention, packed[1][:-8] + _attention_outs(out.data_ptr(), _ptr(keep))
-            + tail + _attention_end(max_q, max_kv, nbytes))
+        out, keep, outs = _make(0, nbytes, q)
+        pointers = packed[1][:-8] + outs
+    else:
+        _, keep, outs = _make(0, nbytes, q[:0])
+        pointers = packed[1] + outs[8:]
+    _launch(q, (_bound or _library()).pam_paged_attention, pointers + tail + _attention_end(max_q, max_kv, nbytes))
     del keep
     return out

@@ -1,13 +1,18 @@
-// Reads the tensors of a call for attention.py: what a call's argument checks
-// depend on, as one hashable key, and the addresses, as the bytes its argument
-// structure begins with.  (In Python, type, shape, strides, device and address of
-// append_kv's eleven tensors took 5 of its 10 us of host time.)
+// The tensors of a call for attention.py.  pack reads the inputs: what a call's
+// argument checks depend on, as one hashable key, and the addresses, as the bytes
+// its argument structure begins with.  (In Python, type, shape, strides, device
+// and address of append_kv's eleven tensors took 5 of its 10 us of host time.)
+// make allocates the results and the workspace.  (torch.empty takes 1.5 us a
+// tensor; the gradient of norm and rotation makes five.)
 
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <ATen/ops/empty.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <memory>
 
 namespace {
 
@@ -52,7 +57,73 @@ PyObject *pack(PyObject *, PyObject *const *args, Py_ssize_t count) {
                          (Py_ssize_t)(count * sizeof(int64_t)));
 }
 
-PyMethodDef methods[] = {{"pack", (PyCFunction)(void *)pack, METH_FASTCALL, "pack(tensor or None, ...) -> (key, addresses)"},
+// make(type, bytes, tensor or None, ...) -> (result or None, ..., workspace or
+// None, addresses): a contiguous tensor like each given one, of float32 (type 0),
+// bfloat16 (1) or its own type (-1), and where bytes > 0 a workspace of as many
+// on the device of the first tensor given; the addresses of all.
+PyObject *make(PyObject *, PyObject *const *args, Py_ssize_t count) {
+    HANDLE_TH_ERRORS
+    if (count < 3 || count > kMostTensors) {
+        PyErr_SetString(PyExc_TypeError, "make takes a type, a number of bytes and tensors");
+        return nullptr;
+    }
+    const long type = PyLong_AsLong(args[0]);
+    const long long bytes = PyLong_AsLongLong(args[1]);
+    if (PyErr_Occurred())
+        return nullptr;
+    int64_t address[kMostTensors];
+    // Of the tensors, then the workspace, then the addresses.
+    std::unique_ptr<PyObject, void (*)(PyObject *)> results(PyTuple_New(count), Py_DecRef);
+    if (!results)
+        return nullptr;
+    const at::Tensor *first = nullptr;
+    auto put = [&](Py_ssize_t i, const at::Tensor &made) {
+        address[i] = (int64_t)made.data_ptr();
+        PyObject *wrapped = THPVariable_Wrap(made);
+        if (wrapped != nullptr)
+            PyTuple_SET_ITEM(results.get(), i, wrapped);
+        return wrapped != nullptr;
+    };
+    auto put_none = [&](Py_ssize_t i) {
+        address[i] = 0;
+        Py_INCREF(Py_None);
+        PyTuple_SET_ITEM(results.get(), i, Py_None);
+    };
+    for (Py_ssize_t i = 0; i + 2 < count; ++i) {
+        PyObject *given = args[i + 2];
+        if (given == Py_None) {
+            put_none(i);
+            continue;
+        }
+        if (!THPVariable_Check(given)) {
+            PyErr_SetString(PyExc_TypeError, "make takes tensors");
+            return nullptr;
+        }
+        const at::Tensor &t = THPVariable_Unpack(given);
+        if (first == nullptr)
+            first = &t;
+        const at::ScalarType made = type < 0 ? t.scalar_type() : type == 0 ? at::kFloat : at::kBFloat16;
+        if (!put(i, at::empty(t.sizes(), t.options().dtype(made))))
+            return nullptr;
+    }
+    const Py_ssize_t last = count - 2;
+    if (bytes > 0 && first != nullptr) {
+        if (!put(last, at::empty({(int64_t)bytes}, first->options().dtype(at::kByte))))
+            return nullptr;
+    } else {
+        put_none(last);
+    }
+    PyObject *addresses = PyBytes_FromStringAndSize((const char *)address, (Py_ssize_t)((last + 1) * sizeof(int64_t)));
+    if (addresses == nullptr)
+        return nullptr;
+    PyTuple_SET_ITEM(results.get(), count - 1, addresses);
+    return results.release();
+    END_HANDLE_TH_ERRORS
+}
+
+PyMethodDef methods[] = {{"make", (PyCFunction)(void *)make, METH_FASTCALL,
+                          "make(type, bytes, tensor or None, ...) -> (result, ..., workspace, addresses)"},
+                         {"pack", (PyCFunction)(void *)pack, METH_FASTCALL, "pack(tensor or None, ...) -> (key, addresses)"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pack", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
