@@ -19,9 +19,10 @@
 // PAM-MACs, which take several times as long.
 //
 // Bound by the vector ALU: 2 lane-ops a PAM-MAC, issued in pairs from four waves a
-// SIMD.  512 tokens x 32 heads of 128 over 4096 keys (8 key heads, bfloat16): 660 us,
-// 24.4 T PAM-MAC/s, 25.2 T without the join's 22 us (the framework's matrix product
-// on such operands: 30.8 T); the causal mask cuts 1% off what the tiles compute.
+// SIMD.  512 tokens x 32 heads of 128 over 4096 keys (8 key heads, bfloat16): 660
+// to 684 us by card, 24 T PAM-MAC/s, 25 T without the join's 22 us (the framework's
+// matrix product on such operands: 30.8 T); the causal mask cuts 1% off what the
+// tiles compute.
 
 #include "pam_attention_device.h"
 
