@@ -188,7 +188,9 @@ pam_status_t pam_append_kv(const pam_append_kv_t *args, hipStream_t stream);
  * followed by a product is: PAM commutes with powers of two only.  A token
  * that sees no key gets zeros, also where all its scores are -inf; a NaN
  * score gives NaN.  Keys and values a token does not see have no influence
- * on it, whatever they hold.  PAM terms below 2^-126 may count in a sum
+ * on it, whatever they hold: none on a bit of its outputs where no token of
+ * its sequence and call sees them, and else, should they be inf or NaN, on
+ * the order of its sums alone.  PAM terms below 2^-126 may count in a sum
  * instead of as zero.
  *
  * max_q: at least every sequence's count of new tokens (tokens past it get

@@ -16,7 +16,8 @@
 // so that a cache line is used by the lanes of one load, and all L loads of the
 // 64 keys are on their way before the first is used.  Lanes past a head's end
 // and keys that are none read something that is there instead, and count for
-// nothing afterwards.  Scores: a lane has the
+// nothing afterwards: a value of theirs, that of a key of the group itself, since
+// its weight of zero would make NaN of an inf elsewhere.  Scores: a lane has the
 // partial sums of its 16 bytes of each key; adding them up over the L lanes
 // halves the number of sums a lane holds with each step (one half goes to the
 // lane's partner, the other half comes), so that lane i ends with one key's
@@ -105,13 +106,14 @@ template <int R> struct Area {
 // group's first at the end of a group, so that the memory always has work of
 // the wave.  next(first) starts to fetch what the group from `first` on needs,
 // keep(buffer) puts it where load(buffer, n) finds load n's offset; use(buffer,
-// n, words) takes load n, done(buffer, first) closes a group.
+// n, words) takes load n, done(buffer, first) closes a group; where live(buffer)
+// says so, which is the same in all lanes, a group's loads go unused.
 // begin() runs once the first loads are out.  Fine groups: all loads of a group
 // at once, one group after the other.
-template <typename T, int L, bool F, typename Next, typename Keep, typename From, typename Begin, typename Use,
-          typename Done>
+template <typename T, int L, bool F, typename Next, typename Keep, typename From, typename Begin, typename Live,
+          typename Use, typename Done>
 __device__ __forceinline__ void stream_keys(const void *data, int first, int end, int step, Next next, Keep keep,
-                                            From from, Begin begin, Use use, Done done) {
+                                            From from, Begin begin, Live live, Use use, Done done) {
     constexpr int B = F ? L / 4 : L / 2 < kLoads ? L / 2 : kLoads;
     constexpr int N = L / B;
     if (first >= end)
@@ -125,9 +127,11 @@ __device__ __forceinline__ void stream_keys(const void *data, int first, int end
     begin();
     if constexpr (F) {
         for (;;) {
+            if (live(0)) {
 #pragma unroll
-            for (int u = 0; u < B; ++u)
-                use(0, u, w[0][u]);
+                for (int u = 0; u < B; ++u)
+                    use(0, u, w[0][u]);
+            }
             done(0, first);
             first += step;
             if (first >= end)
@@ -150,9 +154,11 @@ __device__ __forceinline__ void stream_keys(const void *data, int first, int end
             for (int u = 0; u < B; ++u)
                 w[(i + 1) & 1][u] = load16<T>(data, last ? from(buffer ^ 1, u) : from(buffer, (i + 1) * B + u));
             __builtin_amdgcn_sched_barrier(0);
+            if (live(buffer)) {
 #pragma unroll
-            for (int u = 0; u < B; ++u)
-                use(buffer, i * B + u, w[i & 1][u]);
+                for (int u = 0; u < B; ++u)
+                    use(buffer, i * B + u, w[i & 1][u]);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
         done(buffer, first);
@@ -241,7 +247,7 @@ __device__ __forceinline__ void score_keys(const AttentionParams &p, const Unit 
             wave_sync();
         },
         [&](int buffer, int n) { return area.from[buffer][n * K + lane / L] + reads; },
-        [&]() { load_queries<E, R>(p, unit, at, q); },
+        [&]() { load_queries<E, R>(p, unit, at, q); }, [](int) { return true; },
         [&](int, int n, const u32x4 &w) {
             float sum[R];
 #pragma unroll
@@ -409,6 +415,7 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
             acc[r][i] = 0.0f;
     }
     int64_t place = -1;
+    uint32_t live = 0;                 // bit `buffer`: its group has a key
     float t[R];
     constexpr int G = group_keys<F>();
     stream_keys<T, L, F>(
@@ -420,7 +427,12 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
         },
         [&](int buffer) {
             wave_sync();
-            area.from[buffer][lane] = place >= 0 ? place : 0;   // fine groups: four times over
+            const uint64_t there = __ballot(place >= 0);
+            const int some = there != 0 ? __builtin_ctzll(there) : 0;
+            const int64_t other = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(place >> 32), some) << 32 |
+                                            (uint32_t)__builtin_amdgcn_readlane((int)place, some));
+            live = (live & ~(1u << buffer)) | (there != 0 ? 1u << buffer : 0u);
+            area.from[buffer][lane] = place >= 0 ? place : there != 0 ? other : 0;   // fine groups: four times over
 #pragma unroll
             for (int r = 0; r < R; ++r)
                 t[r] = real(probability(place >= 0 ? exp2_from(t[r], row.m[r]) : 0.0f, inverse[r]));
@@ -428,6 +440,7 @@ __device__ __forceinline__ void value_keys(const AttentionParams &p, const Unit 
             wave_sync();
         },
         [&](int buffer, int n) { return area.from[buffer][n * K + lane / L] + reads; }, []() {},
+        [&](int buffer) { return (live >> buffer & 1) != 0; },
         [&](int buffer, int n, const u32x4 &w) {
             float b[R];
             get<R>(reinterpret_cast<const float *>(area.pr[buffer]) + (n * K + lane / L) * R, b);
