@@ -543,7 +543,7 @@ __global__ void __launch_bounds__(kThreads) attention_scores_kernel(const Attent
     __shared__ Area<R> areas[kThreads / 64];
     __shared__ float top[kMostWaves][R], sum[kMostWaves][R];
     const int units = gridDim.x / p.splits, split = blockIdx.x / units, index = blockIdx.x - split * units;
-    const Unit unit(p, index);
+    const Unit unit(p, p.first_unit + index);
     const int begin = max(unit.lo, split * p.split_keys), end = min(unit.hi, (split + 1) * p.split_keys);
     if (unit.rows == 0 || begin >= end)
         return;
@@ -571,7 +571,7 @@ __global__ void __launch_bounds__(kThreads) attention_values_kernel(const Attent
     __shared__ Area<R> areas[kThreads / 64];
     __shared__ float scratch[kThreads / 64 * R * L * kPer<T>];
     const int units = gridDim.x / p.splits, split = blockIdx.x / units, index = blockIdx.x - split * units;
-    const Unit unit(p, index);
+    const Unit unit(p, p.first_unit + index);
     const int begin = max(unit.lo, split * p.split_keys), end = min(unit.hi, (split + 1) * p.split_keys);
     if (unit.rows == 0 || begin >= end)
         return;
@@ -628,55 +628,54 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(const Attentio
 enum Which { kWhole, kScores, kValues };
 
 template <typename T, int L, int R, bool F>
-hipError_t launch(Which which, const AttentionParams &p, hipStream_t stream) {
-    const unsigned units = (unsigned)(p.batch * p.kv_heads * p.row_blocks);
+hipError_t launch(Which which, const AttentionParams &p, int units, hipStream_t stream) {
     const void *kernel = which == kWhole    ? (const void *)attention_whole_kernel<T, L, R, F>
                          : which == kScores ? (const void *)attention_scores_kernel<T, L, R, F>
                                             : (const void *)attention_values_kernel<T, L, R, F>;
     const int threads = which == kWhole ? whole_waves(p.max_kv, R, F) * 64 : kThreads;
     const size_t lds = which == kWhole ? (size_t)whole_lds(p.max_kv, R, L, sizeof(T) == 2, F) : 0;
-    const unsigned grid = which == kWhole ? units : units * (unsigned)p.splits;
+    const unsigned grid = (unsigned)units * (which == kWhole ? 1u : (unsigned)p.splits);
     void *args[] = {const_cast<AttentionParams *>(&p)};
     return hipLaunchKernel(kernel, dim3(grid), dim3((unsigned)threads), args, lds, stream);
 }
 
-template <typename T, int L, bool F> hipError_t for_rows(Which which, const AttentionParams &p, hipStream_t stream) {
+template <typename T, int L, bool F> hipError_t for_rows(Which which, const AttentionParams &p, int units, hipStream_t stream) {
     switch (p.rows) {
-    case 1: return launch<T, L, 1, F>(which, p, stream);
-    case 2: return launch<T, L, 2, F>(which, p, stream);
-    case 3: return launch<T, L, 3, F>(which, p, stream);
-    case 4: return launch<T, L, 4, F>(which, p, stream);
-    case 6: return launch<T, L, 6, F>(which, p, stream);
-    default: return launch<T, L, 8, F>(which, p, stream);
+    case 1: return launch<T, L, 1, F>(which, p, units, stream);
+    case 2: return launch<T, L, 2, F>(which, p, units, stream);
+    case 3: return launch<T, L, 3, F>(which, p, units, stream);
+    case 4: return launch<T, L, 4, F>(which, p, units, stream);
+    case 6: return launch<T, L, 6, F>(which, p, units, stream);
+    default: return launch<T, L, 8, F>(which, p, units, stream);
     }
 }
 
-template <typename T, int L> hipError_t for_group(Which which, const AttentionParams &p, hipStream_t stream) {
-    return p.fine ? for_rows<T, L, true>(which, p, stream) : for_rows<T, L, false>(which, p, stream);
+template <typename T, int L> hipError_t for_group(Which which, const AttentionParams &p, int units, hipStream_t stream) {
+    return p.fine ? for_rows<T, L, true>(which, p, units, stream) : for_rows<T, L, false>(which, p, units, stream);
 }
 
-hipError_t for_type(Which which, bool bf16, int lanes, const AttentionParams &p, hipStream_t stream) {
+hipError_t for_type(Which which, bool bf16, int lanes, const AttentionParams &p, int units, hipStream_t stream) {
     switch (lanes) {
-    case 4: return bf16 ? for_group<uint16_t, 4>(which, p, stream) : for_group<float, 4>(which, p, stream);
-    case 8: return bf16 ? for_group<uint16_t, 8>(which, p, stream) : for_group<float, 8>(which, p, stream);
-    case 16: return bf16 ? for_group<uint16_t, 16>(which, p, stream) : for_group<float, 16>(which, p, stream);
-    case 32: return bf16 ? for_group<uint16_t, 32>(which, p, stream) : for_group<float, 32>(which, p, stream);
-    default: return for_group<float, 64>(which, p, stream);
+    case 4: return bf16 ? for_group<uint16_t, 4>(which, p, units, stream) : for_group<float, 4>(which, p, units, stream);
+    case 8: return bf16 ? for_group<uint16_t, 8>(which, p, units, stream) : for_group<float, 8>(which, p, units, stream);
+    case 16: return bf16 ? for_group<uint16_t, 16>(which, p, units, stream) : for_group<float, 16>(which, p, units, stream);
+    case 32: return bf16 ? for_group<uint16_t, 32>(which, p, units, stream) : for_group<float, 32>(which, p, units, stream);
+    default: return for_group<float, 64>(which, p, units, stream);
     }
 }
 
 }  // namespace
 
 hipError_t launch_attention_whole(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream) {
-    return for_type(kWhole, bf16, lanes, p, stream);
+    return for_type(kWhole, bf16, lanes, p, p.batch * p.kv_heads * p.row_blocks, stream);
 }
 
-hipError_t launch_attention_scores(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream) {
-    return for_type(kScores, bf16, lanes, p, stream);
+hipError_t launch_attention_scores(bool bf16, int lanes, const AttentionParams &p, int units, hipStream_t stream) {
+    return for_type(kScores, bf16, lanes, p, units, stream);
 }
 
-hipError_t launch_attention_values(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream) {
-    return for_type(kValues, bf16, lanes, p, stream);
+hipError_t launch_attention_values(bool bf16, int lanes, const AttentionParams &p, int units, hipStream_t stream) {
+    return for_type(kValues, bf16, lanes, p, units, stream);
 }
 
 hipError_t launch_attention_join(const AttentionParams &p, int units, hipStream_t stream) {

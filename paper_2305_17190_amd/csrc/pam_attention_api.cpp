@@ -167,7 +167,7 @@ struct AttentionPlan {
     size_t bytes() const { return scores + stats + partial; }
 };
 
-constexpr int64_t kSlabBytes = (int64_t)512 << 20;   // scores of one round of launches, about
+constexpr int64_t kSlabBytes = (int64_t)512 << 20;   // workspace of one round of launches, about
 
 AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool bf16, int32_t batch, int32_t max_q,
                              int32_t max_kv) {
@@ -230,6 +230,15 @@ AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool 
             a.split_keys = 64;
     }
     a.splits = (int)ceil_div(std::max(max_kv, 1), a.split_keys);
+    if (a.form == Form::split) {
+        // Rounds of equal size: max_kv may be the whole reach of a table of short
+        // sequences (128 of up to 1024 keys, 8 heads x 4 rows, a reach of 131072:
+        // 2310 MiB and 321 us at once, 464 MiB and 338 us in five rounds; of up to
+        // 8192 keys 827 us either way).
+        const int64_t unit = (int64_t)a.splits * a.rows * (a.split_keys + d) * (int64_t)sizeof(float);
+        const int64_t rounds = ceil_div(a.units, std::max<int64_t>(kSlabBytes / unit, 1));
+        a.slab = ceil_div(a.units, rounds);
+    }
     const int64_t parts = a.slab * a.splits;
     const int64_t stats = parts * (a.form == Form::tiles ? a.split_keys / 128 : 1) * 2 * a.rows;
     a.scores = (size_t)(parts * a.split_keys * a.rows) * sizeof(float);
@@ -480,8 +489,7 @@ pam_status_t pam_paged_attention(const pam_paged_attention_t *args, hipStream_t 
         return invalid("kv_lens and table must be non-NULL");
     const bool bf16 = is_bf16(kc.type);
     const AttentionPlan plan = attention_plan(s.d, s.q_heads.heads, kc.heads, bf16, s.batch, s.max_q, s.max_kv);
-    const int64_t most_groups = plan.form == Form::tiles ? plan.slab * plan.splits * std::max(plan.split_keys / 128, 2)
-                                                         : plan.units * plan.splits;
+    const int64_t most_groups = plan.slab * plan.splits * (plan.form == Form::tiles ? std::max(plan.split_keys / 128, 2) : 1);
     if (plan.units > kMaxLaunchGroups || most_groups > kMaxLaunchGroups)
         return invalid("too many workgroups (batch * heads * rows * keys too large)");
     if (plan.bytes() > 0) {
@@ -536,19 +544,16 @@ pam_status_t pam_paged_attention(const pam_paged_attention_t *args, hipStream_t 
     hipError_t e = hipSuccess;
     if (plan.form == Form::whole) {
         e = pamk::launch_attention_whole(bf16, plan.lanes, p, stream);
-    } else if (plan.form == Form::split) {
-        e = pamk::launch_attention_scores(bf16, plan.lanes, p, stream);
-        if (e == hipSuccess)
-            e = pamk::launch_attention_values(bf16, plan.lanes, p, stream);
-        if (e == hipSuccess)
-            e = pamk::launch_attention_join(p, (int)plan.units, stream);
     } else {
+        const bool tiles = plan.form == Form::tiles;
         for (int64_t first = 0; first < plan.units && e == hipSuccess; first += plan.slab) {
             const int units = (int)std::min(plan.slab, plan.units - first);
             p.first_unit = (int32_t)first;
-            e = pamk::launch_tile_scores(bf16, p, units, stream);
+            e = tiles ? pamk::launch_tile_scores(bf16, p, units, stream)
+                      : pamk::launch_attention_scores(bf16, plan.lanes, p, units, stream);
             if (e == hipSuccess)
-                e = pamk::launch_tile_values(bf16, p, units, stream);
+                e = tiles ? pamk::launch_tile_values(bf16, p, units, stream)
+                          : pamk::launch_attention_values(bf16, plan.lanes, p, units, stream);
             if (e == hipSuccess && p.partial != nullptr)
                 e = pamk::launch_attention_join(p, units, stream);
         }

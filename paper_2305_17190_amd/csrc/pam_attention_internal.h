@@ -114,7 +114,7 @@ struct AttentionParams {
 };
 
 // Few rows a unit (pam_attention.hip), `lanes` lanes a key: one launch with
-// the scores in LDS, or two with the keys split.
+// the scores in LDS, or two with the keys split, of `units` units from first_unit on.
 // The one launch's waves: of 16 keys each (fine) or of 64; 16 at most with up to
 // 4 rows (128 registers a lane), else 8.
 constexpr int whole_most_waves(int rows) { return rows <= 4 ? 16 : 8; }
@@ -131,8 +131,8 @@ inline int64_t whole_lds(int64_t max_kv, int rows, int lanes, bool bf16, bool fi
 }
 constexpr int64_t kWholeLds = 131072;   // at most
 hipError_t launch_attention_whole(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream);
-hipError_t launch_attention_scores(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream);
-hipError_t launch_attention_values(bool bf16, int lanes, const AttentionParams &p, hipStream_t stream);
+hipError_t launch_attention_scores(bool bf16, int lanes, const AttentionParams &p, int units, hipStream_t stream);
+hipError_t launch_attention_values(bool bf16, int lanes, const AttentionParams &p, int units, hipStream_t stream);
 // Units of 64 or 128 rows (pam_attention_tile.hip); split_keys a multiple of 128.
 hipError_t launch_tile_scores(bool bf16, const AttentionParams &p, int units, hipStream_t stream);
 hipError_t launch_tile_values(bool bf16, const AttentionParams &p, int units, hipStream_t stream);

@@ -46,11 +46,11 @@ int head_grad_groups(bool, int64_t, int, int, int most) { return most; }
 hipError_t launch_attention_whole(bool bf16, int lanes, const AttentionParams &p, hipStream_t) {
     return record(1, bf16, lanes, p, all_units(p), whole_waves(p.max_kv, p.rows, p.fine) * 64);
 }
-hipError_t launch_attention_scores(bool bf16, int lanes, const AttentionParams &p, hipStream_t) {
-    return record(2, bf16, lanes, p, all_units(p), 256);
+hipError_t launch_attention_scores(bool bf16, int lanes, const AttentionParams &p, int units, hipStream_t) {
+    return record(2, bf16, lanes, p, units, 256);
 }
-hipError_t launch_attention_values(bool bf16, int lanes, const AttentionParams &p, hipStream_t) {
-    return record(3, bf16, lanes, p, all_units(p), 256);
+hipError_t launch_attention_values(bool bf16, int lanes, const AttentionParams &p, int units, hipStream_t) {
+    return record(3, bf16, lanes, p, units, 256);
 }
 hipError_t launch_attention_join(const AttentionParams &p, int units, hipStream_t) {
     return record(4, false, 0, p, units, 256);

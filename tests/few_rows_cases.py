@@ -57,3 +57,9 @@ OUTSIDE = [
         ("whole", True, [250, 77, 16, 3], 1, 0), ("whole", False, SHORT, 3, 0), ("split", True, [300, 77], 2, 0),
         ("split", False, LONG, 2, 4500))
 ]
+
+# Bounds whose workspace passes a round's: the units take turns in it.
+ROUNDS = [
+    Case("split", False, sequences(1, LONG), 16, 2, 8, 64, True, 4000000),
+    Case("split", False, sequences(2, [300, 5, 1200]), 1024, 3, 2, 128, False, 9000000, window=50),
+]

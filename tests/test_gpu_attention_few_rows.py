@@ -33,3 +33,15 @@ def test_values_of_no_key_have_no_influence(case):
     for value in (np.inf, -np.inf, np.nan):
         cache.k[0], cache.v[0] = value, value
         assert np.array_equal(result(case, cache, q).cpu().numpy().view(np.uint32), clean), value
+
+
+@pytest.mark.parametrize("case", cases.ROUNDS, ids=repr)
+def test_several_rounds(case):
+    """Workspaces of more than a round: the units take turns in it."""
+    note(f"rounds {case}")
+    rng = np.random.default_rng(42)
+    cache = case.cache(rng)
+    q = case.queries(rng)
+    out = result(case, cache, q)
+    compare(cache, q, case.counts, out, "rounds", causal=case.causal, window=case.window)
+    assert np.array_equal(result(case, cache, q).cpu().numpy(), out.cpu().numpy())
