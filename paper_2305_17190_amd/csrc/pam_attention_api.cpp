@@ -31,7 +31,8 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kMaxRows = 0x7FFFFFFF;         // slots of a cache, positions of a table
 constexpr int64_t kMaxHeadRows = (int64_t)1 << 25;  // a launch of them, 4 a workgroup, stays below 2^32 threads
 constexpr int64_t kMaxStride = (int64_t)1 << 31; // times a count below 2^31: offsets stay inside int64
-constexpr int64_t kMaxLaunchGroups = 16777215;   // workgroups of 256 threads: below 2^32 threads
+constexpr int64_t kMaxLaunchThreads = ((int64_t)1 << 32) - 1;
+constexpr int64_t kMaxLaunchGroups = kMaxLaunchThreads / 256;
 
 bool is_bf16(pam_type_t t) { return t == PAM_TYPE_BF16; }
 
@@ -490,7 +491,10 @@ pam_status_t pam_paged_attention(const pam_paged_attention_t *args, hipStream_t 
     const bool bf16 = is_bf16(kc.type);
     const AttentionPlan plan = attention_plan(s.d, s.q_heads.heads, kc.heads, bf16, s.batch, s.max_q, s.max_kv);
     const int64_t most_groups = plan.slab * plan.splits * (plan.form == Form::tiles ? std::max(plan.split_keys / 128, 2) : 1);
-    if (plan.units > kMaxLaunchGroups || most_groups > kMaxLaunchGroups)
+    // The one launch has up to 1024 threads a workgroup, all others at most 256.
+    const int64_t whole_threads =
+        plan.form == Form::whole ? plan.units * pamk::whole_waves(s.max_kv, plan.rows, plan.fine) * 64 : 0;
+    if (plan.units > kMaxLaunchGroups || most_groups > kMaxLaunchGroups || whole_threads > kMaxLaunchThreads)
         return invalid("too many workgroups (batch * heads * rows * keys too large)");
     if (plan.bytes() > 0) {
         if (s.workspace == nullptr || s.workspace_bytes < 0 || (size_t)s.workspace_bytes < plan.bytes())

@@ -60,3 +60,18 @@ def test_split_workspace_is_bounded_by_a_round_or_a_unit():
         x = launches[0]
         one = x.splits * x.rows * (x.split_keys + d + 4) * 4
         assert probe.workspace(d, heads, group, bf16, batch, new, keys) <= max(ROUND * (1 + 4 / (x.split_keys + d)), one) + 16
+
+
+@pytest.mark.parametrize("keys", [200, 1000, 4000])
+def test_launches_stay_below_the_grid_limit(keys):
+    """Less than 2^32 threads a launch; the one launch of short contexts has up to
+    1024 a workgroup, and with more units is refused."""
+    for batch in (1 << 20, (1 << 22) - 1, 1 << 22, (1 << 24) - 1, 1 << 24, 1 << 26):
+        status, launches = probe.attention(64, 1, 1, False, batch, 1, keys)
+        assert (status == 0) == bool(launches) and status in (0, 1)
+        for x in launches:
+            groups = x.units * (x.splits if x.name in ("scores", "values") else 1)
+            assert groups * x.threads < 1 << 32, (batch, x.name)
+            if x.name == "whole":
+                assert x.units == batch
+    assert probe.attention(64, 1, 1, False, 1 << 26, 1, 1000)[0] == 1      # 16 waves a unit
