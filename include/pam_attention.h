@@ -11,10 +11,12 @@
  * The conventions of pam.h hold: device pointers, strides in elements, every
  * call asynchronous on `stream`, no allocation, arguments validated before
  * anything is launched.  A call's arguments are one structure, read before the
- * call returns: the pointers, then the layouts and sizes.  What lies in device memory (positions, slots,
- * lengths, page tables) cannot be validated by the host: each call says what
- * a value out of range does, and none makes a kernel leave its buffers as
- * long as the arrays have the stated sizes.
+ * call returns: the pointers, then the layouts and sizes.  The rows of a
+ * written operand may not share memory: each of its strides is at least the
+ * extent of the dimensions of smaller stride.  What lies in device memory
+ * (positions, slots, lengths, page tables) cannot be validated by the host:
+ * each call says what a value out of range does, and none makes a kernel leave
+ * its buffers as long as the arrays have the stated sizes.
  */
 #ifndef PAM_ATTENTION_H_
 #define PAM_ATTENTION_H_
@@ -148,7 +150,8 @@ pam_status_t pam_norm_rope_grad(const pam_norm_rope_grad_t *args, hipStream_t st
  * pam_norm_rope, values stored as they are; both are rounded to the cache's
  * type (nearest even).  q_in / q_out (optional): the same tokens' queries,
  * normed and rotated in the same launch.  k, v and q_in have one type, k and
- * v as many heads as the caches.  Two tokens with one slot race.
+ * v as many heads as the caches.  Two tokens with one slot race, and so do
+ * caches that share memory.
  */
 typedef struct {
     const void *k;

@@ -26,6 +26,12 @@ pam_status_t invalid(const char *name, const char *why) {
     return invalid(buf);
 }
 
+#define PAM_TRY(call)                                       \
+    do {                                                    \
+        if (pam_status_t st_ = (call); st_ != PAM_SUCCESS)  \
+            return st_;                                     \
+    } while (0)
+
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 constexpr int64_t kMaxRows = 0x7FFFFFFF;         // slots of a cache, positions of a table
@@ -48,11 +54,30 @@ pam_status_t check_heads(const void *data, const pam_heads_t &h, const char *nam
     return PAM_SUCCESS;
 }
 
+struct Dim {
+    int64_t count, stride;
+};
+
+// Whether rows of d values share no memory: each stride at least the extent of
+// all dimensions of smaller stride.  Strides lie in [0, 2^31].
+template <int N> bool rows_apart(int32_t d, Dim (&dims)[N]) {
+    std::sort(dims, dims + N, [](const Dim &a, const Dim &b) { return a.stride < b.stride; });
+    int64_t extent = d;
+    for (const Dim &dim : dims) {
+        if (dim.count <= 1)
+            continue;
+        if (dim.stride < extent)
+            return false;
+        extent += dim.stride * (std::min(dim.count, kMaxRows) - 1);   // past 2^31 no stride reaches it
+    }
+    return true;
+}
+
 // A written operand: its rows may not share memory.
 pam_status_t check_written(const void *data, const pam_heads_t &h, const char *name, int64_t tokens, int32_t d) {
-    if ((tokens > 1 && h.stride_token < d) || (h.heads > 1 && h.stride_head < d))
-        return invalid(name, ": rows of a written operand overlap");
-    return check_heads(data, h, name, tokens);
+    PAM_TRY(check_heads(data, h, name, tokens));
+    Dim dims[] = {{tokens, h.stride_token}, {h.heads, h.stride_head}};
+    return rows_apart(d, dims) ? PAM_SUCCESS : invalid(name, ": rows of a written operand overlap");
 }
 
 pam_status_t check_cache(const void *data, const pam_cache_t &c, const char *name, bool must_have_data) {
@@ -68,6 +93,13 @@ pam_status_t check_cache(const void *data, const pam_cache_t &c, const char *nam
     if (must_have_data && c.pages > 0 && data == nullptr)
         return invalid(name, ": data is NULL");
     return PAM_SUCCESS;
+}
+
+// A cache that is written.
+pam_status_t check_written_cache(const void *data, const pam_cache_t &c, const char *name, int64_t tokens, int32_t d) {
+    PAM_TRY(check_cache(data, c, name, tokens > 0));
+    Dim dims[] = {{c.pages, c.stride_page}, {c.page_size, c.stride_slot}, {c.heads, c.stride_head}};
+    return rows_apart(d, dims) ? PAM_SUCCESS : invalid(name, ": slots of a written cache overlap");
 }
 
 pam_status_t check_dim(int64_t tokens, int32_t d, float eps) {
@@ -139,12 +171,6 @@ void to_cache(pamk::HeadPart &part, void *data, const pam_cache_t &c) {
     part.out_bf16 = is_bf16(c.type);
     part.paged = 1;
 }
-
-#define PAM_TRY(call)                                       \
-    do {                                                    \
-        if (pam_status_t st_ = (call); st_ != PAM_SUCCESS)  \
-            return st_;                                     \
-    } while (0)
 
 // Workgroups, and partial rows, of the two parts of a gradient: the budget
 // shared in proportion to the rows.
@@ -411,8 +437,8 @@ pam_status_t pam_append_kv(const pam_append_kv_t *args, hipStream_t stream) {
     const pam_cache_t &kc = a.k_cache_layout, &vc = a.v_cache_layout;
     PAM_TRY(check_heads(a.k, a.k_heads, "k", a.tokens));
     PAM_TRY(check_heads(a.v, a.v_heads, "v", a.tokens));
-    PAM_TRY(check_cache(a.k_cache, kc, "k_cache", a.tokens > 0));
-    PAM_TRY(check_cache(a.v_cache, vc, "v_cache", a.tokens > 0));
+    PAM_TRY(check_written_cache(a.k_cache, kc, "k_cache", a.tokens, a.d));
+    PAM_TRY(check_written_cache(a.v_cache, vc, "v_cache", a.tokens, a.d));
     if (a.k_heads.type != a.v_heads.type || (has_q && a.q_in_heads.type != a.k_heads.type))
         return invalid("k, v and q_in must have one type");
     if (a.k_heads.heads != kc.heads || a.v_heads.heads != vc.heads || a.k_heads.heads != a.v_heads.heads)
