@@ -37,6 +37,26 @@ from . import norm_rope_grad as _norm_rope_grad
 __all__ = ["pam_linear", "pam_matmul", "pam_norm_rope", "PAMLinear"]
 
 
+class _FirstOrder(torch.autograd.Function):
+    """A backward pass's own kernels under ``create_graph``: they record nothing,
+    so that a second derivative would count their results as constants."""
+
+    @staticmethod
+    def forward(ctx, gradients, *tensors):
+        return gradients(*tensors)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the PAM wrappers have first derivatives only")
+
+
+def _first_order(gradients, *tensors):
+    """gradients(*tensors); differentiating the results raises."""
+    if torch.is_grad_enabled():
+        return _FirstOrder.apply(gradients, *tensors)
+    return gradients(*tensors)
+
+
 def _float32(**named) -> None:
     """The wrappers' gradients are float32 products: refuse other dtypes up
     front rather than in the backward pass."""
@@ -149,8 +169,8 @@ class _NormRopeFn(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dq, dk):
-        q, k, *rest = ctx.saved_tensors
-        gq, gk, gqw, gkw = _norm_rope_grad(_dense_heads(dq), _dense_heads(dk), q, k, *rest, *ctx.rest)
+        gq, gk, gqw, gkw = _first_order(lambda *tensors: _norm_rope_grad(*tensors, *ctx.rest), _dense_heads(dq),
+                                        _dense_heads(dk), *ctx.saved_tensors)
         return gq, gk, None, None, None, gqw, gkw, None, None
 
 
@@ -158,7 +178,8 @@ def pam_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor = No
                   sin: torch.Tensor = None, q_weight: torch.Tensor = None, k_weight: torch.Tensor = None,
                   eps: float = 1e-6, interleaved: bool = False):
     """``pam.norm_rope`` of queries and keys (tokens, heads, d) with gradients for
-    q, k and the weights; the tables of angles are constants."""
+    q, k and the weights; the tables of angles are constants.  Second derivatives
+    raise."""
     if q is None or k is None:
         raise ValueError("pam_norm_rope takes queries and keys; norm_rope takes one of them")
     return _NormRopeFn.apply(q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved)
