@@ -169,8 +169,14 @@ class _NormRopeFn(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dq, dk):
+        q, k, positions, cos, sin, qw, kw = ctx.saved_tensors
+        needs = ctx.needs_input_grad
+        if not (needs[0] or needs[5]):
+            dq = q = qw = None
+        if not (needs[1] or needs[6]):
+            dk = k = kw = None
         gq, gk, gqw, gkw = _first_order(lambda *tensors: _norm_rope_grad(*tensors, *ctx.rest), _dense_heads(dq),
-                                        _dense_heads(dk), *ctx.saved_tensors)
+                                        _dense_heads(dk), q, k, positions, cos, sin, qw, kw)
         return gq, gk, None, None, None, gqw, gkw, None, None
 
 

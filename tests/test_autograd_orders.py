@@ -75,3 +75,22 @@ def test_second_derivatives_of_norm_rope_raise(norm_rope, loss):
         assert torch.allclose(g, torch.autograd.grad(total, x, retain_graph=True)[0])     # itself right, and of use
         with pytest.raises(RuntimeError, match="first derivatives only"):
             (total + g.pow(2).sum()).backward(retain_graph=True)
+
+
+@pytest.mark.parametrize("needed", [(0,), (1,), (5,), (6,), (0, 5), (0, 1), (1, 5), (0, 1, 5, 6)])
+@pytest.mark.parametrize("create_graph", [False, True])
+def test_norm_rope_works_on_the_sides_needed_alone(norm_rope, needed, create_graph):
+    """Queries (inputs 0 and 5) or keys (1 and 6) that need no gradient are not worked on."""
+    args = [t.detach() for t in inputs()]
+    for i in needed:
+        args[i].requires_grad_()
+    zq, zk = autograd.pam_norm_rope(*args, EPS)
+    got = torch.autograd.grad(zq.pow(2).sum() + zk.exp().sum(), [args[i] for i in needed], create_graph=create_graph)
+    q, k, pos, cos, sin, qw, kw = args
+    total = plain(q, qw, cos, sin, pos).pow(2).sum() + plain(k, kw, cos, sin, pos).exp().sum()
+    want = torch.autograd.grad(total, [args[i] for i in needed])
+    assert all(torch.allclose(a, b) for a, b in zip(got, want))
+    (call,) = norm_rope
+    for side, at in (("q", (0, 5)), ("k", (1, 6))):
+        given = bool(set(at) & set(needed))
+        assert all((call[name] is not None) == given for name in (side, "d" + side, side + "_weight"))
