@@ -17,7 +17,8 @@ and dW likewise, through ``pam.exact_grad``.  With
 ``mantissa_bits`` < 23 every product, forward and backward, first rounds its
 two operands to that many mantissa bits (App. "PAM with Narrower
 Mantissas"); the tensors themselves are not modified.  Inputs must be float32
-HIP tensors; there is no CPU path.
+HIP tensors; there is no CPU path.  First derivatives only: what a second one
+would need of a backward pass's products raises.
 
 ``pam_norm_rope`` is the attention's norm of queries and keys with the position
 rotation (``pam.norm_rope``), ordinary arithmetic, float32 or bfloat16.
@@ -91,16 +92,18 @@ class _PAMLinearFn(torch.autograd.Function):
         x2d, weight = ctx.saved_tensors
         dy = _last_contiguous(dy)
         dx = dw = db = None
+        # Under create_graph each result's first two operands count as what it depends
+        # on: the exact derivative is constant in the operand it is taken by.
         if ctx.exact:
-            if ctx.needs_input_grad[0]:
-                dx = _exact_grad(dy, weight, x2d)                           # sum_j dY d(X .^ W)/dX
-            if ctx.needs_input_grad[1]:
-                dw = _exact_grad(dy, x2d, weight, trans_a=True)             # sum_i dY d(W .^ X)/dW
+            if ctx.needs_input_grad[0]:                                     # sum_j dY d(X .^ W)/dX
+                dx = _first_order(lambda d, w: _exact_grad(d, w, x2d), dy, weight)
+            if ctx.needs_input_grad[1]:                                     # sum_i dY d(W .^ X)/dW
+                dw = _first_order(lambda d, x: _exact_grad(d, x, weight, trans_a=True), dy, x2d)
         else:
-            if ctx.needs_input_grad[0]:
-                dx = _gemm(dy, weight, mantissa_bits=ctx.bits)              # dX = dY .^ W
-            if ctx.needs_input_grad[1]:
-                dw = _gemm(dy, x2d, trans_a=True, mantissa_bits=ctx.bits)   # dW = dY^T .^ X
+            if ctx.needs_input_grad[0]:                                     # dX = dY .^ W
+                dx = _first_order(lambda d, w: _gemm(d, w, mantissa_bits=ctx.bits), dy, weight)
+            if ctx.needs_input_grad[1]:                                     # dW = dY^T .^ X
+                dw = _first_order(lambda d, x: _gemm(d, x, trans_a=True, mantissa_bits=ctx.bits), dy, x2d)
         if ctx.has_bias and ctx.needs_input_grad[2]:
             db = dy.sum(dim=0)
         return dx, dw, db, None, None
@@ -139,9 +142,9 @@ class _PAMBmmFn(torch.autograd.Function):
         dc = _last_contiguous(dc)
         da = db = None
         if ctx.needs_input_grad[0]:
-            da = _bmm(dc, b, trans_b=True, mantissa_bits=ctx.bits)     # dA = dC .^ B^T
+            da = _first_order(lambda d, b: _bmm(d, b, trans_b=True, mantissa_bits=ctx.bits), dc, b)     # dA = dC .^ B^T
         if ctx.needs_input_grad[1]:
-            db = _bmm(a, dc, trans_a=True, mantissa_bits=ctx.bits)     # dB = A^T .^ dC
+            db = _first_order(lambda a, d: _bmm(a, d, trans_a=True, mantissa_bits=ctx.bits), a, dc)     # dB = A^T .^ dC
         return da, db, None
 
 
@@ -184,8 +187,7 @@ def pam_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor = No
                   sin: torch.Tensor = None, q_weight: torch.Tensor = None, k_weight: torch.Tensor = None,
                   eps: float = 1e-6, interleaved: bool = False):
     """``pam.norm_rope`` of queries and keys (tokens, heads, d) with gradients for
-    q, k and the weights; the tables of angles are constants.  Second derivatives
-    raise."""
+    q, k and the weights; the tables of angles are constants."""
     if q is None or k is None:
         raise ValueError("pam_norm_rope takes queries and keys; norm_rope takes one of them")
     return _NormRopeFn.apply(q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved)

@@ -94,3 +94,50 @@ def test_norm_rope_works_on_the_sides_needed_alone(norm_rope, needed, create_gra
     for side, at in (("q", (0, 5)), ("k", (1, 6))):
         given = bool(set(at) & set(needed))
         assert all((call[name] is not None) == given for name in (side, "d" + side, side + "_weight"))
+
+
+@pytest.fixture
+def products(monkeypatch):
+    """The wrappers of the products over stand-ins with ordinary products."""
+    def turned(t, trans):
+        return t.transpose(-1, -2) if trans else t
+
+    def product(a, b, trans_a=False, trans_b=False, mantissa_bits=23):
+        with torch.no_grad():
+            return turned(a, trans_a) @ turned(b, trans_b)
+
+    for name in ("_gemm", "_bmm"):
+        monkeypatch.setattr(autograd, name, product)
+    monkeypatch.setattr(autograd, "_exact_grad", lambda a, b, mod, trans_a=False: product(a, b, trans_a))
+
+
+def floats(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)).requires_grad_()
+
+
+@pytest.mark.parametrize("derivative", ["approximate", "exact"])
+def test_second_derivatives_of_linear_raise(products, derivative):
+    x, w, bias = floats(0, 4, 6), floats(1, 5, 6), floats(2, 5)
+    y = autograd.pam_linear(x, w, bias, derivative=derivative)
+    want = torch.autograd.grad((x @ w.T + bias).pow(2).sum(), (x, w, bias))
+    got = torch.autograd.grad(y.pow(2).sum(), (x, w, bias), create_graph=True)
+    assert all(torch.allclose(a, b, rtol=1e-5) for a, b in zip(got, want))
+    for g in got[:2]:
+        with pytest.raises(RuntimeError, match="first derivatives only"):
+            (y.sum() + g.pow(2).sum()).backward(retain_graph=True)
+    got[2].sum().backward(retain_graph=True, inputs=[bias])       # torch's own sum
+    # Gradients that depend on no other tracked tensor are constants, as they should be.
+    y = autograd.pam_linear(x, w.detach(), derivative=derivative)
+    (g,) = torch.autograd.grad(y.sum(), x, create_graph=True)
+    assert not g.requires_grad
+
+
+def test_second_derivatives_of_matmul_raise(products):
+    a, b = floats(3, 2, 4, 6), floats(4, 2, 6, 5)
+    c = autograd.pam_matmul(a, b)
+    want = torch.autograd.grad((a @ b).pow(2).sum(), (a, b))
+    got = torch.autograd.grad(c.pow(2).sum(), (a, b), create_graph=True)
+    assert all(torch.allclose(x, y, rtol=1e-5) for x, y in zip(got, want))
+    for g in got:
+        with pytest.raises(RuntimeError, match="first derivatives only"):
+            (c.sum() + g.pow(2).sum()).backward(retain_graph=True)
