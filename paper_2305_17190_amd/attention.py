@@ -353,21 +353,22 @@ def _attention_plan(q, k_cache, v_cache, table, kv_lens, q_starts, scale, causal
     return tail, (d, heads, kv_heads, _is_bf16(k_cache), batch), width * page_size
 
 
-def paged_attention(q, k_cache, v_cache, table, kv_lens, q_starts=None, max_q: int = 1, max_kv: int | None = None,
-                    scale: float | None = None, causal: bool = True, window: int = 0, out=None):
+def paged_attention(q, k_cache, v_cache, table, kv_lens, q_starts=None, max_q: int | None = None,
+                    max_kv: int | None = None, scale: float | None = None, causal: bool = True, window: int = 0, out=None):
     """softmax(scale Q .^ K^T) .^ V of new tokens over a paged cache, as float32
     (tokens, heads, d).
 
     ``q`` (tokens, heads, d) holds the new tokens of all sequences in order;
     sequence b's are ``q_starts[b] : q_starts[b + 1]`` (int32, batch + 1
-    entries), at most ``max_q`` of them; without ``q_starts`` every sequence has
-    one.  ``kv_lens`` (int32) counts each sequence's cached keys, its new ones
-    among them as the last; ``table`` (int32, batch x pages a row) names their
-    pages.  ``max_kv`` (the table's whole reach) bounds ``kv_lens``: the nearer
-    it is, the better the work is cut.  A token sees its sequence's keys up to
-    its own position (all, without ``causal``), the last ``window`` of them
-    where that is positive; a token without keys gets zeros.  ``scale`` is 1 /
-    sqrt(d) if not given.  Tokens of no sequence are left unwritten."""
+    entries), at most ``max_q`` (all of q) of them; without ``q_starts`` every
+    sequence has one.  ``kv_lens`` (int32) counts each sequence's cached keys, its
+    new ones among them as the last; ``table`` (int32, batch x pages a row) names
+    their pages.  ``max_kv`` (the table's whole reach) bounds ``kv_lens``: the
+    nearer the two bounds are, the better the work is cut.  A token sees its
+    sequence's keys up to its own position (all, without ``causal``), the last
+    ``window`` of them where that is positive; a token without keys gets zeros.
+    ``scale`` is 1 / sqrt(d) if not given.  Tokens of no sequence are left
+    unwritten."""
     causal, window, scale = bool(causal), int(window), None if scale is None else float(scale)
     packed = (_pack_tensors or _pack)(q, k_cache, v_cache, q_starts, kv_lens, table, out)
     args = (q, k_cache, v_cache, table, kv_lens, q_starts, scale, causal, window, out)
@@ -375,7 +376,7 @@ def paged_attention(q, k_cache, v_cache, table, kv_lens, q_starts=None, max_q: i
         _attention_plan(*args)
         raise TypeError("paged_attention takes dense tensors")
     tail, sizes, reach = _known((3, packed[0], scale, causal, window), _attention_plan, *args)
-    max_q = 1 if q_starts is None else int(max_q)
+    max_q = 1 if q_starts is None else q.shape[0] if max_q is None else int(max_q)
     max_kv = reach if max_kv is None else int(max_kv)
     nbytes = _attention_workspace((*sizes, max_q, max_kv))
     if out is None:

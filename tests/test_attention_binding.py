@@ -1,0 +1,50 @@
+"""The Python binding of the attention-side operators around its calls of the
+library (CPU: the checks' results and the library are stand-ins)."""
+import struct
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2305_17190_amd import attention as att  # noqa: E402
+
+
+@pytest.fixture
+def launched(monkeypatch):
+    """paged_attention on CPU tensors up to its call of the library: the (max_q,
+    max_kv) it hands over and those it sizes the workspace by."""
+    seen = []
+
+    def plan(q, k_cache, v_cache, table, kv_lens, q_starts, scale, causal, window, out):
+        return b"", (q.shape[2], q.shape[1], k_cache.shape[2], 0, kv_lens.shape[0]), table.shape[1] * k_cache.shape[1]
+
+    def workspace(sizes):
+        seen.append(sizes[-2:])
+        return 0
+
+    monkeypatch.setattr(att, "_attention_plan", plan)
+    monkeypatch.setattr(att, "_calls", {})
+    monkeypatch.setattr(att, "_attention_workspace", workspace)
+    monkeypatch.setattr(att, "_library", lambda: type("library", (), {"pam_paged_attention": None}))
+    monkeypatch.setattr(att, "_bound", None)
+    monkeypatch.setattr(att, "_launch", lambda t, fn, args: seen.append(struct.unpack("=iiq", args[-16:])[:2]))
+    return seen
+
+
+def call(tokens, batch, width=3, page=16, **kw):
+    cache = torch.zeros(4, page, 1, 8)
+    return att.paged_attention(torch.zeros(tokens, 2, 8), cache, cache, torch.zeros(batch, width, dtype=torch.int32),
+                               torch.ones(batch, dtype=torch.int32), **kw)
+
+
+def test_bounds_left_out_hold_for_every_call(launched):
+    """Without max_q a sequence may have all of q's tokens, without max_kv all the
+    table reaches."""
+    starts = torch.tensor([0, 1, 6], dtype=torch.int32)
+    call(6, 2, q_starts=starts)
+    assert launched == [(6, 48), (6, 48)]
+    del launched[:]
+    call(6, 2, q_starts=starts, max_q=5, max_kv=20)
+    call(2, 2)
+    call(2, 2, max_q=7)
+    assert launched == [(5, 20), (5, 20), (1, 48), (1, 48), (1, 48), (1, 48)]
