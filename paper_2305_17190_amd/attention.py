@@ -144,7 +144,8 @@ def _pack(*tensors):
             from . import _pack as module
         except ImportError as e:
             raise PamError(f"_pack.so is missing: build it with `python -m paper_2305_17190_amd.build` ({e})") from e
-        _pack_tensors, _make = module.pack, module.make
+        _make = module.make                          # first: the calls look at _pack_tensors alone
+        _pack_tensors = module.pack
     return _pack_tensors(*tensors)
 
 

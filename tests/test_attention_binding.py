@@ -1,6 +1,7 @@
 """The Python binding of the attention-side operators around its calls of the
 library (CPU: the checks' results and the library are stand-ins)."""
 import struct
+import sys
 
 import pytest
 
@@ -48,3 +49,28 @@ def test_bounds_left_out_hold_for_every_call(launched):
     call(2, 2)
     call(2, 2, max_q=7)
     assert launched == [(5, 20), (5, 20), (1, 48), (1, 48), (1, 48), (1, 48)]
+
+
+def test_a_first_call_is_whole_at_every_step(monkeypatch):
+    """Another thread may see the binding between any two steps of a first call:
+    what pack goes through must find make."""
+    monkeypatch.setattr(att, "_pack_tensors", None)
+    monkeypatch.setattr(att, "_make", None)
+    steps = []
+
+    def trace(frame, event, arg):
+        if frame.f_code is not att._pack.__code__:
+            return None
+        frame.f_trace_opcodes = True
+        if event == "opcode":
+            steps.append((att._pack_tensors is not None, att._make is not None))
+        return trace
+
+    before = sys.gettrace()
+    sys.settrace(trace)
+    try:
+        assert att._pack(torch.zeros(2)) is not None
+    finally:
+        sys.settrace(before)
+    assert steps[0] == (False, False) and steps[-1] == (True, True)
+    assert (True, False) not in steps
