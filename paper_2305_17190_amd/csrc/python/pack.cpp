@@ -2,13 +2,15 @@
 // argument checks depend on, as one hashable key, and the addresses, as the bytes
 // its argument structure begins with.  (In Python, type, shape, strides, device
 // and address of append_kv's eleven tensors took 5 of its 10 us of host time.)
-// make allocates the results and the workspace.  (torch.empty takes 1.5 us a
-// tensor; the gradient of norm and rotation makes five.)
+// make allocates the results and the workspace, and like torch.empty lets other
+// threads run meanwhile: an allocation may wait for the device.  (torch.empty takes
+// 1.5 us a tensor; the gradient of norm and rotation makes five.)
 
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/Exceptions.h>
+#include <pybind11/pybind11.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -71,47 +73,41 @@ PyObject *make(PyObject *, PyObject *const *args, Py_ssize_t count) {
     const long long bytes = PyLong_AsLongLong(args[1]);
     if (PyErr_Occurred())
         return nullptr;
-    int64_t address[kMostTensors];
-    // Of the tensors, then the workspace, then the addresses.
-    std::unique_ptr<PyObject, void (*)(PyObject *)> results(PyTuple_New(count), Py_DecRef);
-    if (!results)
-        return nullptr;
+    // Of the tensors, then the workspace; the results end with the addresses.
+    const Py_ssize_t last = count - 2;
+    at::Tensor like[kMostTensors], made[kMostTensors];
     const at::Tensor *first = nullptr;
-    auto put = [&](Py_ssize_t i, const at::Tensor &made) {
-        address[i] = (int64_t)made.data_ptr();
-        PyObject *wrapped = THPVariable_Wrap(made);
-        if (wrapped != nullptr)
-            PyTuple_SET_ITEM(results.get(), i, wrapped);
-        return wrapped != nullptr;
-    };
-    auto put_none = [&](Py_ssize_t i) {
-        address[i] = 0;
-        Py_INCREF(Py_None);
-        PyTuple_SET_ITEM(results.get(), i, Py_None);
-    };
-    for (Py_ssize_t i = 0; i + 2 < count; ++i) {
-        PyObject *given = args[i + 2];
-        if (given == Py_None) {
-            put_none(i);
+    for (Py_ssize_t i = 0; i < last; ++i) {
+        if (args[i + 2] == Py_None)
             continue;
-        }
-        if (!THPVariable_Check(given)) {
+        if (!THPVariable_Check(args[i + 2])) {
             PyErr_SetString(PyExc_TypeError, "make takes tensors");
             return nullptr;
         }
-        const at::Tensor &t = THPVariable_Unpack(given);
+        like[i] = THPVariable_Unpack(args[i + 2]);
         if (first == nullptr)
-            first = &t;
-        const at::ScalarType made = type < 0 ? t.scalar_type() : type == 0 ? at::kFloat : at::kBFloat16;
-        if (!put(i, at::empty(t.sizes(), t.options().dtype(made))))
-            return nullptr;
+            first = &like[i];
     }
-    const Py_ssize_t last = count - 2;
-    if (bytes > 0 && first != nullptr) {
-        if (!put(last, at::empty({(int64_t)bytes}, first->options().dtype(at::kByte))))
+    {
+        pybind11::gil_scoped_release others;
+        for (Py_ssize_t i = 0; i < last; ++i)
+            if (like[i].defined())
+                made[i] = at::empty(like[i].sizes(), like[i].options().dtype(type < 0    ? like[i].scalar_type()
+                                                                             : type == 0 ? at::kFloat
+                                                                                         : at::kBFloat16));
+        if (bytes > 0 && first != nullptr)
+            made[last] = at::empty({(int64_t)bytes}, first->options().dtype(at::kByte));
+    }
+    int64_t address[kMostTensors];
+    std::unique_ptr<PyObject, void (*)(PyObject *)> results(PyTuple_New(count), Py_DecRef);
+    if (!results)
+        return nullptr;
+    for (Py_ssize_t i = 0; i <= last; ++i) {
+        address[i] = made[i].defined() ? (int64_t)made[i].data_ptr() : 0;
+        PyObject *item = THPVariable_Wrap(made[i]);   // None where none was made
+        if (item == nullptr)
             return nullptr;
-    } else {
-        put_none(last);
+        PyTuple_SET_ITEM(results.get(), i, item);
     }
     PyObject *addresses = PyBytes_FromStringAndSize((const char *)address, (Py_ssize_t)((last + 1) * sizeof(int64_t)));
     if (addresses == nullptr)

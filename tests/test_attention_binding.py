@@ -2,6 +2,8 @@
 library (CPU: the checks' results and the library are stand-ins)."""
 import struct
 import sys
+import threading
+import time
 
 import pytest
 
@@ -74,3 +76,50 @@ def test_a_first_call_is_whole_at_every_step(monkeypatch):
         sys.settrace(before)
     assert steps[0] == (False, False) and steps[-1] == (True, True)
     assert (True, False) not in steps
+
+
+def test_other_threads_run_during_the_allocations():
+    """With a switch interval past the test's length another thread runs only where
+    this one lets go of the interpreter."""
+    att._pack(torch.zeros(2))
+    like = torch.zeros(4, 3, 8)
+    ran, stop = [0], threading.Event()
+
+    def count():
+        while not stop.is_set():
+            ran[0] += 1
+            time.sleep(0)                             # lets go, in turn
+
+    interval = sys.getswitchinterval()
+    thread = threading.Thread(target=count, daemon=True)
+    sys.setswitchinterval(100)                        # before the thread first waits its turn
+    thread.start()
+    try:
+        kept, before = [], ran[0]                     # kept: a tensor's end lets go as well
+        while ran[0] == before and len(kept) < 20000:
+            kept.append(att._make(-1, 16, like, None, like))
+        assert ran[0] > before
+    finally:
+        sys.setswitchinterval(interval)
+        stop.set()
+        thread.join()
+
+
+def test_what_is_made():
+    att._pack(torch.zeros(2))
+    like = torch.zeros(4, 3, 8).transpose(0, 1)
+    a, none, b, room, addresses = att._make(-1, 48, like, None, like.bfloat16())
+    assert none is None and a.shape == b.shape == like.shape and a.is_contiguous() and b.is_contiguous()
+    assert (a.dtype, b.dtype, room.dtype, room.numel()) == (torch.float32, torch.bfloat16, torch.uint8, 48)
+    assert struct.unpack("=4q", addresses) == (a.data_ptr(), 0, b.data_ptr(), room.data_ptr())
+    a, room, addresses = att._make(1, 0, like)
+    assert a.dtype == torch.bfloat16 and room is None and struct.unpack("=2q", addresses) == (a.data_ptr(), 0)
+    assert att._make(0, 0, like)[0].dtype == torch.float32
+    none, room, _ = att._make(0, 16, None)                # no tensor whose device would do
+    assert none is None and room is None
+    with pytest.raises(TypeError):
+        att._make(0, 0, 3)
+    with pytest.raises(TypeError):
+        att._make(0, 0)
+    with pytest.raises(TypeError):
+        att._make("float", 0, like)
