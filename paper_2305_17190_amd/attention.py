@@ -318,6 +318,14 @@ def _attention_workspace(sizes: tuple) -> int:
 
 
 _attention_end = struct.Struct("=iiq").pack
+_MOST_INT = 2 ** 31 - 1
+
+
+def _count(value, name: str) -> int:
+    value = int(value)
+    if not 0 <= value <= _MOST_INT:
+        raise ValueError(f"{name} must be in [0, 2^31), got {value}")
+    return value
 
 
 def _attention_plan(q, k_cache, v_cache, table, kv_lens, q_starts, scale, causal, window, out):
@@ -370,15 +378,16 @@ def paged_attention(q, k_cache, v_cache, table, kv_lens, q_starts=None, max_q: i
     ``window`` of them where that is positive; a token without keys gets zeros.
     ``scale`` is 1 / sqrt(d) if not given.  Tokens of no sequence are left
     unwritten."""
-    causal, window, scale = bool(causal), int(window), None if scale is None else float(scale)
+    # Keys count to below 2^31: a window of as many is as good as a wider one.
+    causal, window, scale = bool(causal), min(int(window), _MOST_INT), None if scale is None else float(scale)
     packed = (_pack_tensors or _pack)(q, k_cache, v_cache, q_starts, kv_lens, table, out)
     args = (q, k_cache, v_cache, table, kv_lens, q_starts, scale, causal, window, out)
     if packed is None:
         _attention_plan(*args)
         raise TypeError("paged_attention takes dense tensors")
     tail, sizes, reach = _known((3, packed[0], scale, causal, window), _attention_plan, *args)
-    max_q = 1 if q_starts is None else q.shape[0] if max_q is None else int(max_q)
-    max_kv = reach if max_kv is None else int(max_kv)
+    max_q = 1 if q_starts is None else q.shape[0] if max_q is None else _count(max_q, "max_q")
+    max_kv = min(reach, _MOST_INT) if max_kv is None else _count(max_kv, "max_kv")
     nbytes = _attention_workspace((*sizes, max_q, max_kv))
     if out is None:
         out, keep, outs = _make(0, nbytes, q)

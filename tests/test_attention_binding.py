@@ -123,3 +123,18 @@ def test_what_is_made():
         att._make(0, 0)
     with pytest.raises(TypeError):
         att._make("float", 0, like)
+
+
+def test_bounds_past_32_bits(launched, monkeypatch):
+    """A reach of 2^31 keys and more bounds lengths that are int32 all the same, a
+    window of as many hides nothing; other bounds past the range are refused."""
+    windows = []
+    plan = att._attention_plan
+    monkeypatch.setattr(att, "_attention_plan", lambda *args: windows.append(args[8]) or plan(*args))
+    cache = torch.zeros(1, 1, 1, 8).expand(1, 2 ** 30, 1, 8)
+    table, lens = torch.zeros(1, 3, dtype=torch.int32), torch.ones(1, dtype=torch.int32)
+    att.paged_attention(torch.zeros(1, 2, 8), cache, cache, table, lens, window=2 ** 40)
+    assert launched == [(1, 2 ** 31 - 1)] * 2 and windows == [2 ** 31 - 1]
+    for bounds in (dict(max_kv=2 ** 31), dict(max_q=2 ** 32 + 1), dict(max_q=-1), dict(max_kv=-2 ** 40)):
+        with pytest.raises(ValueError, match="must be in"):
+            call(2, 2, q_starts=torch.tensor([0, 1, 2], dtype=torch.int32), **bounds)
