@@ -63,3 +63,32 @@ ROUNDS = [
     Case("split", False, sequences(1, LONG), 16, 2, 8, 64, True, 4000000),
     Case("split", False, sequences(2, [300, 5, 1200]), 1024, 3, 2, 128, False, 9000000, window=50),
 ]
+
+# Head sizes by the lanes a key takes: (d, bfloat16 cache), whole and with a part of
+# the last lanes' 16 bytes past the head's end.
+HEADS = [(16, False), (8, True), (32, False), (64, True), (56, True), (64, False), (48, False), (128, True), (72, True),
+         (128, False), (96, False), (256, True), (200, True), (256, False), (136, False)]
+# (new tokens, query heads a key head): every count of rows a unit can have, 5 and 7
+# among those that a unit of the next one takes.
+ROWS = [(1, 1), (2, 1), (1, 3), (2, 2), (1, 5), (3, 2), (1, 7), (2, 4)]
+
+
+def every_kernel(fine, layouts):
+    """One case for each lane count, type and count of rows in both forms; every
+    second with a window, every third without the causal mask."""
+    return [Case(form, fine, sequences(new, lengths), pages[i % 3], heads, group, d, bf16, reach[i % 2], i % 3 != 1,
+                 (0, 50)[i // 2 % 2])
+            for form, heads, lengths, pages, reach in layouts
+            for i, (d, bf16, new, group) in enumerate((d, bf16, new, group) for d, bf16 in HEADS for new, group in ROWS)]
+
+
+FINE = every_kernel(True, (("whole", 1, [250, 77, 16, 3], (16, 1, 32), (0, 0)), ("split", 2, [300, 77], (16, 1, 48), (0, 3000))))
+# The far bounds give splits of 256 and of 1024 keys.
+WIDE = every_kernel(False, (("whole", 3, SHORT, (16, 1, 32), (0, 0)), ("split", 2, LONG, (16, 1, 48), (4500, 140000))))
+# Many units whose scores fit half of LDS take one launch past 256 keys as well.
+WIDE += [Case("whole", False, sequences(1, [1000, 3, 0, 64] + SHORT * 2), 16, 3, group, d, bf16)
+         for d, bf16 in ((64, False), (128, True)) for group in (1, 4)]
+
+# Where it goes wrong most easily, in one and in three launches, float32 and bfloat16.
+CORNERS = [case for case in WIDE if case.form == "split" and case.d in (64, 128) and max(case.counts) * case.group in (3, 8)]
+CORNERS += [case for case in WIDE if case.form == "whole" and case.d in (64, 128) and max(case.counts) * case.group in (2, 7)]

@@ -19,11 +19,20 @@ def lanes_of(d, bf16):
     return lanes
 
 
-@pytest.mark.parametrize("case", cases.OUTSIDE + cases.ROUNDS, ids=repr)
+@pytest.mark.parametrize("case", cases.OUTSIDE + cases.ROUNDS + cases.FINE + cases.WIDE, ids=repr)
 def test_cases_take_their_form(case):
     new = max(case.counts)
     assert probe.form(case.d, case.heads, case.group, case.bf16, len(case.seqs), new, case.width * case.page) == (
         case.form, case.fine, rows_of(new * case.group), lanes_of(case.d, case.bf16))
+
+
+@pytest.mark.parametrize("some", [cases.FINE, cases.WIDE], ids=["fine", "wide"])
+def test_cases_reach_every_kernel(some):
+    """Rows a unit times lanes a key, in both types and forms."""
+    reached = {(case.form, case.bf16, rows_of(max(case.counts) * case.group), lanes_of(case.d, case.bf16))
+               for case in some}
+    assert reached == {(form, bf16, rows, lanes) for form in ("whole", "split") for bf16 in (False, True)
+                       for rows in (1, 2, 3, 4, 6, 8) for lanes in (4, 8, 16, 32) + (() if bf16 else (64,))}
 
 
 ROUND = 512 << 20
