@@ -80,7 +80,9 @@ typedef struct {
  * head h, with x = in[t][h] and w the weight of d values:
  *   y = x w / sqrt(mean(x^2) + eps)      (weight NULL: y = x)
  *   out[t][h] = rotation of y at the token's position
- * in float32, rounded once to out's type (nearest even).  d even, 2 .. 256.
+ * in float32, rounded once to out's type (nearest even).  Squares and eps below
+ * 2^-126 count as zero; a mean past the float32 range gives zeros.  d even,
+ * 2 .. 256.
  * q and k are each a pair of in and out with equal head counts (out may be
  * in); both or one of them given.  q_in and k_in have one type.  tokens == 0
  * launches nothing.  eps >= 0 and finite.

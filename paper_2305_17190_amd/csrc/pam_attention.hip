@@ -29,9 +29,10 @@
 // bfloat16 value read, 2 full-rate ops a row and 2.5 half-rate ones to take it
 // apart.  128 sequences of up to 8192 keys, 8 heads of 128 x 4 rows, bfloat16 (2.66
 // GB): 615 us, 4.3 TB/s (a 1 GiB copy: 5.1-5.2); one of 131071 keys (537 MB): 133 us,
-// 4.0 TB/s; float32 caches up to 5.8 TB/s.  One of 1000 keys: 16.4 us, three launches
-// of 7.6, 5.7 and 2.5 us, each most of it the latency of its chain of loads.  With 8
-// rows a unit 12-14 T PAM-MAC/s.
+// 4.0 TB/s.  64 sequences of 4096 keys, 8 heads of 128: with one row in float32 (2.15 GB)
+// 348 us, 6.2 TB/s, in bfloat16 184 us, 5.8; with 8 rows 461 and 365 us, 4.7 and 2.9
+// TB/s, 9.3 and 11.8 T PAM-MAC/s.  One of 1000 keys: 16.4 us, three launches of 7.5, 6
+// and 3 us, each most of it the latency of its chain of loads.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -679,7 +680,9 @@ hipError_t launch_attention_values(bool bf16, int lanes, const AttentionParams &
 }
 
 hipError_t launch_attention_join(const AttentionParams &p, int units, hipStream_t stream) {
-    // Many splits of few outputs: 16 threads an output.
+    // Many splits of few outputs: 16 threads an output (131071 keys, 8 units of 4 rows
+    // of 128: 132 us the call, with one thread 139; 128 sequences of 8192 keys, 1024
+    // such units: 934 with 16, 924 with one).
     const bool shared = p.splits > 8 && (int64_t)units * p.rows * p.d <= 1 << 17;
     const int items = shared ? kThreads / 16 : kThreads;
     const int parts = (p.rows * p.d / 4 + items - 1) / items;

@@ -194,7 +194,9 @@ struct AttentionPlan {
     size_t bytes() const { return scores + stats + partial; }
 };
 
-constexpr int64_t kSlabBytes = (int64_t)512 << 20;   // workspace of one round of launches, about
+// Workspace of one round of launches, about: tiles of 512 x 4 rows of 8 heads over 32768
+// keys of 128 take 5.51 ms in rounds of 512 MiB, 5.75 of 128, 5.53 in one of 2 GiB.
+constexpr int64_t kSlabBytes = (int64_t)512 << 20;
 
 AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool bf16, int32_t batch, int32_t max_q,
                              int32_t max_kv) {
@@ -219,7 +221,11 @@ AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool 
     const bool tiled = tile_us < few_us;
     if (tiled) {
         // 128 rows a unit where that leaves two rounds of score tiles, four
-        // workgroups a compute unit; else 64, which waste less.
+        // workgroups a compute unit; else 64, which waste less.  Over 4096 keys of
+        // 128 x 8 heads, 512 x 4 rows a head: 653 us, in units of 64 762; 256 x 4
+        // rows: 343 and 418.  Heads of 64 differ little (415 and 403 us), and the
+        // limit is on the safe side: 128 x 4 rows, 1024 tiles, 195 us in units of
+        // 128, 232 of 64.
         const int64_t tiles = heads * ceil_div(rows, 128) * ceil_div(max_kv, 128);
         a.rows = rows > 64 && tiles >= 2048 ? 128 : 64;
     } else {
@@ -232,8 +238,13 @@ AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool 
     // one (1000 keys x 8 heads of 128: 20.5 -> 16.4 us; 15006 keys x 4 units of 6 rows
     // of 256, 940 waves of 64: 39 us, in waves of 16 52).
     a.fine = a.units * ceil_div(max_kv, 64) <= 512;
-    // One launch for short contexts (one of 1000 keys in 16 waves: 35 us, split 21),
-    // and where the units fill the chip and their scores fit in LDS.
+    // One launch for short contexts (32 of 256 keys, 8 heads of 64 in float32: 7.7 us,
+    // split 13.4; not of 1000: 35 in 16 waves, 21), and where the units fill the chip
+    // and their scores fit in half of LDS, so that two are resident (64 sequences of
+    // 1000 keys, 8 heads of 64: 41 us, split 50; 32 of 1024, 8 heads of 128 x 4 rows in
+    // bfloat16: 37 and 40; 16 of them, half the units: 36 and 29).  Few units of 4
+    // rows over 256 keys would be faster split (8 units of 128: 21.5 and 15.7), more
+    // keys than fit in half of LDS sometimes in one launch (2048: 55.9, split 61.5).
     const int64_t lds = pamk::whole_lds(max_kv, a.rows, a.lanes, bf16, a.fine);
     const bool whole = (max_kv <= 256 && lds <= pamk::kWholeLds) || (a.units >= 256 && lds <= pamk::kWholeLds / 2);
     a.form = tiled ? Form::tiles : whole ? Form::whole : Form::split;
@@ -250,7 +261,11 @@ AttentionPlan attention_plan(int32_t d, int32_t q_heads, int32_t kv_heads, bool 
         const int64_t per = ceil_div(keys * a.slab * columns * waves, 4096);
         a.split_keys = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(per, 128) * 128, 128), 256);
     } else {
-        // About 1024 workgroups, of 256 to 1024 keys; of 64 in waves of 16.
+        // About 1024 workgroups, of 256 to 1024 keys; of 64 in waves of 16.  Short
+        // splits cost a launch's start and a partial sum each (8 heads of 128 x 4 rows
+        // in bfloat16, 16 sequences of 8192 keys in splits of 128, 256, 512, 1024 and
+        // 2048: 195, 143, 129, 130, 125 us), long ones leave the chip empty (one sequence
+        // of 32768 keys: 59, 42, 40, 44, 71).
         const int64_t keys = ceil_div((int64_t)max_kv * a.units, 1024);
         a.split_keys = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(keys, 256) * 256, 256), 1024);
         if (a.fine)

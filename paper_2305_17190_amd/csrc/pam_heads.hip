@@ -15,7 +15,8 @@
 // keys of 8192 tokens, 8 + 8 heads of 64 in float32 (68 MB) 12.3 us, 5.5 TB/s; the
 // gradient (102 MB) 23.3 us, of which 4 add up the weights' gradients; that of 16384
 // tokens, 32 + 8 heads of 128 in bfloat16 (505 MB) 103 us, 4.9 TB/s; their append to
-// a bfloat16 cache from float32 (740 MB) 137 us, 5.4 TB/s.  A 1 GiB copy runs at 5.1-5.2
+// a bfloat16 cache from float32 (740 MB) 137 us, 5.4 TB/s, from bfloat16 (403 MB) 83 us,
+// 4.8 TB/s; their norms and rotation alone in bfloat16 (336 MB) 68 us, 5.0 TB/s.  A 1 GiB copy runs at 5.1-5.2
 // TB/s.  Eight tokens: 4 us on the GPU.
 
 #include <hip/hip_runtime.h>
