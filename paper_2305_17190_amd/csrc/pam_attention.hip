@@ -98,7 +98,7 @@ constexpr int log2_of(int x) { return x <= 1 ? 0 : 1 + log2_of(x / 2); }
 
 // What a wave keeps in LDS of its 64 keys, and of the next 64.
 template <int R> struct Area {
-    int64_t from[2][kGroup];          // offsets in the cache (0 where there is none)
+    int64_t from[2][kGroup];          // offsets in the cache; of something there where there is no key
     uint32_t pr[2][kGroup * R];       // probabilities, as b'
 };
 
@@ -106,9 +106,9 @@ template <int R> struct Area {
 // batches of B: while one batch is used the next is on its way, the next
 // group's first at the end of a group, so that the memory always has work of
 // the wave.  next(first) starts to fetch what the group from `first` on needs,
-// keep(buffer) puts it where load(buffer, n) finds load n's offset; use(buffer,
-// n, words) takes load n, done(buffer, first) closes a group; where live(buffer)
-// says so, which is the same in all lanes, a group's loads go unused.
+// keep(buffer) puts it where from(buffer, n) finds load n's offset; use(buffer,
+// n, words) takes load n, done(buffer, first) closes a group; unless live(buffer),
+// which is the same in all lanes, a group's loads go unused.
 // begin() runs once the first loads are out.  Fine groups: all loads of a group
 // at once, one group after the other.
 template <typename T, int L, bool F, typename Next, typename Keep, typename From, typename Begin, typename Live,
