@@ -17,6 +17,9 @@ device every call raises.
                                                the attention side (``attention.py``): norms of queries and keys
                                                with the position rotation, a paged key/value cache, PAM
                                                attention over it
+    linear, activation_grad, grad_norm, adamw_step
+                                               the layer-and-step side (``training.py``): linear layers with bias,
+                                               activation and residual, their gradient, the optimizer's step
 
 Matrix arguments are float32 HIP tensors whose last dimension is contiguous
 (row stride = leading dimension).  Products that split K take their
@@ -33,7 +36,8 @@ import ctypes
 import os
 
 __all__ = ["mul", "pad", "palog2", "paexp2", "round_mantissa", "gemm", "bmm", "exact_grad", "plan",
-           "device_info", "library_path", "load", "PamError", "norm_rope", "norm_rope_grad", "append_kv", "paged_attention"]
+           "device_info", "library_path", "load", "PamError", "norm_rope", "norm_rope_grad", "append_kv", "paged_attention",
+           "linear", "activation_grad", "grad_norm", "adamw_step"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpam.so")
@@ -428,3 +432,4 @@ def device_info(device: int = 0) -> dict:
 
 
 from .attention import append_kv, norm_rope, norm_rope_grad, paged_attention  # noqa: E402
+from .training import activation_grad, adamw_step, grad_norm, linear  # noqa: E402

@@ -10,7 +10,10 @@ matrix multiply's gradients are ordinary products.
     C = A .^ B (batched)   dA = dC .^ B^T     dB = A^T .^ dC
 
 Every product runs in the library's HIP kernels (``pam.gemm`` / ``pam.bmm``);
-the bias gradient is an ordinary sum (no multiplication).  ``pam_linear``
+the bias gradient is an ordinary sum (no multiplication).  With an activation or
+a residual, Y = f(X .^ W^T + b) + R, what the layer adds runs in its product's
+launches (``pam.linear``), and dZ = dY f'(Z) and db in a pass of their own
+(``pam.activation_grad``); dX and dW are then products with dZ.  ``pam_linear``
 and ``PAMLinear`` also offer Table 1's exact derivative
 (``derivative="exact"``): dX[i,k] = sum_j dY[i,j] d(X[i,k] .^ W[j,k])/dX[i,k]
 and dW likewise, through ``pam.exact_grad``.  With
@@ -29,9 +32,11 @@ import math
 
 import torch
 
+from . import activation_grad as _activation_grad
 from . import bmm as _bmm
 from . import exact_grad as _exact_grad
 from . import gemm as _gemm
+from . import linear as _linear
 from . import norm_rope as _norm_rope
 from . import norm_rope_grad as _norm_rope_grad
 
@@ -75,23 +80,43 @@ def _last_contiguous(t: torch.Tensor) -> torch.Tensor:
 
 class _PAMLinearFn(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x2d, weight, bias, bits, exact):
+    def forward(ctx, x2d, weight, bias, bits, exact, activation=None, residual=None, grad=True):
         x2d = _last_contiguous(x2d)
         weight = _last_contiguous(weight)
-        ctx.save_for_backward(x2d, weight)
         ctx.has_bias = bias is not None
         ctx.bits = bits
         ctx.exact = exact
-        y = _gemm(x2d, weight, trans_b=True, mantissa_bits=bits)   # Y = X .^ W^T
-        if bias is not None:
-            y += bias
+        ctx.activation = activation
+        ctx.added = activation is not None or residual is not None
+        z = None
+        if not ctx.added:
+            y = _gemm(x2d, weight, trans_b=True, mantissa_bits=bits)   # Y = X .^ W^T
+            if bias is not None:
+                y += bias
+        else:
+            residual = None if residual is None else _last_contiguous(residual)
+            keep = grad and activation is not None and any(ctx.needs_input_grad[:3])
+            # relu's own result says where z was positive.
+            save = keep and not (activation == "relu" and residual is None)
+            y = _linear(x2d, weight, None if bias is None else bias.contiguous(), activation, residual, save_z=save,
+                        mantissa_bits=bits)
+            y, z = y if save else (y, y if keep else None)
+        ctx.save_for_backward(x2d, weight, z)
         return y
 
     @staticmethod
     def backward(ctx, dy):
-        x2d, weight = ctx.saved_tensors
+        x2d, weight, z = ctx.saved_tensors
+        needs = ctx.needs_input_grad
+        dres = dy if ctx.added and needs[6] else None
         dy = _last_contiguous(dy)
         dx = dw = db = None
+        if ctx.added and any(needs[:3]):
+            product, bias = needs[0] or needs[1], ctx.has_bias and needs[2]
+            if ctx.activation is not None:                                  # dZ = dY f'(Z), db = sum dZ
+                dy, db = _first_order(lambda d, z: _activation_grad(d, z, ctx.activation, bias, product), dy, z)
+            elif bias:
+                db = _first_order(lambda d: _activation_grad(d, None, None, True, False)[1], dy)
         # Under create_graph each result's first two operands count as what it depends
         # on: the exact derivative is constant in the operand it is taken by.
         if ctx.exact:
@@ -104,14 +129,17 @@ class _PAMLinearFn(torch.autograd.Function):
                 dx = _first_order(lambda d, w: _gemm(d, w, mantissa_bits=ctx.bits), dy, weight)
             if ctx.needs_input_grad[1]:                                     # dW = dY^T .^ X
                 dw = _first_order(lambda d, x: _gemm(d, x, trans_a=True, mantissa_bits=ctx.bits), dy, x2d)
-        if ctx.has_bias and ctx.needs_input_grad[2]:
+        if ctx.has_bias and not ctx.added and ctx.needs_input_grad[2]:
             db = dy.sum(dim=0)
-        return dx, dw, db, None, None
+        return dx, dw, db, None, None, None, dres, None
 
 
 def pam_linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor = None,
-               mantissa_bits: int = 23, derivative: str = "approximate") -> torch.Tensor:
-    """``x .^ weight^T + bias`` over the last dimension of x (any leading dims).
+               mantissa_bits: int = 23, derivative: str = "approximate", activation: str = None,
+               residual: torch.Tensor = None) -> torch.Tensor:
+    """``f(x .^ weight^T + bias) + residual`` over the last dimension of x (any
+    leading dims); ``activation`` f as in ``pam.linear`` (None: the identity),
+    ``residual`` of the result's shape.
 
     ``derivative``: "approximate" (Table 1's approximate derivative, PAM
     products) or "exact" (Table 1's exact derivative)."""
@@ -121,9 +149,14 @@ def pam_linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor = None,
         raise ValueError('derivative must be "approximate" or "exact"')
     if derivative == "exact" and mantissa_bits != 23:
         raise ValueError("the exact derivative takes full float32 mantissas")
-    _float32(x=x, weight=weight, bias=bias)
+    _float32(x=x, weight=weight, bias=bias, residual=residual)
     lead = x.shape[:-1]
-    y = _PAMLinearFn.apply(x.reshape(-1, x.shape[-1]), weight, bias, int(mantissa_bits), derivative == "exact")
+    if residual is not None:
+        if residual.shape != (*lead, weight.shape[0]):
+            raise ValueError(f"residual must have shape {(*lead, weight.shape[0])}, got {tuple(residual.shape)}")
+        residual = residual.reshape(-1, weight.shape[0])
+    y = _PAMLinearFn.apply(x.reshape(-1, x.shape[-1]), weight, bias, int(mantissa_bits), derivative == "exact",
+                           activation, residual, torch.is_grad_enabled())
     return y.reshape(*lead, weight.shape[0])
 
 
@@ -194,15 +227,17 @@ def pam_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor = No
 
 
 class PAMLinear(torch.nn.Module):
-    """A linear layer whose products are PAM (forward and approximate-derivative backward)."""
+    """A linear layer whose products are PAM (forward and approximate-derivative backward),
+    with an activation and, in a call, a residual (``pam_linear``)."""
 
     def __init__(self, in_features: int, out_features: int, bias: bool = True, device=None,
-                 mantissa_bits: int = 23, derivative: str = "approximate"):
+                 mantissa_bits: int = 23, derivative: str = "approximate", activation: str = None):
         super().__init__()
         self.in_features = in_features
         self.out_features = out_features
         self.mantissa_bits = mantissa_bits
         self.derivative = derivative
+        self.activation = activation
         self.weight = torch.nn.Parameter(torch.empty(out_features, in_features, device=device))
         self.bias = torch.nn.Parameter(torch.empty(out_features, device=device)) if bias else None
         self.reset_parameters()
@@ -214,9 +249,10 @@ class PAMLinear(torch.nn.Module):
             if self.bias is not None:
                 self.bias.uniform_(-bound, bound)
 
-    def forward(self, x: torch.Tensor) -> torch.Tensor:
-        return pam_linear(x, self.weight, self.bias, self.mantissa_bits, self.derivative)
+    def forward(self, x: torch.Tensor, residual: torch.Tensor = None) -> torch.Tensor:
+        return pam_linear(x, self.weight, self.bias, self.mantissa_bits, self.derivative, self.activation, residual)
 
     def extra_repr(self) -> str:
         return (f"in_features={self.in_features}, out_features={self.out_features}, bias={self.bias is not None}, "
-                f"mantissa_bits={self.mantissa_bits}, derivative={self.derivative}")
+                f"mantissa_bits={self.mantissa_bits}, derivative={self.derivative}"
+                + (f", activation={self.activation}" if self.activation is not None else ""))

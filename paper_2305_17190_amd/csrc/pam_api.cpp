@@ -507,11 +507,11 @@ bool small_product(const Plan &plan, PlanOf whose, int64_t m, int64_t n, int64_t
 pam_status_t run_gemm(pam_op_t ta, pam_op_t tb, int64_t m, int64_t n, int64_t k, const float *A, int64_t lda,
                       int64_t sa, const float *B, int64_t ldb, int64_t sb, float *C, int64_t ldc, int64_t sc,
                       int64_t batch, const Plan &plan, PlanOf whose, hipStream_t stream, int round_drop = 0,
-                      const Workspace *ext = nullptr, bool bf16 = false) {
+                      const Workspace *ext = nullptr, bool bf16 = false, const pamk::Epilogue *epi = nullptr) {
     if (m == 0 || n == 0 || batch == 0)
         return PAM_SUCCESS;
     Layout L{};
-    if (k > 0) {
+    if (k > 0 || epi != nullptr) {
         pam_status_t st = layout_of(plan, m, n, batch, &L);
         if (st != PAM_SUCCESS)
             return st;
@@ -522,12 +522,14 @@ pam_status_t run_gemm(pam_op_t ta, pam_op_t tb, int64_t m, int64_t n, int64_t k,
     pam_status_t st = check_device();
     if (st != PAM_SUCCESS)
         return st;
-    if (k == 0) {
+    if (k == 0 && epi == nullptr) {
         hipError_t e = pamk::launch_fill_zero(C, (int32_t)m, (int32_t)n, ldc, sc, batch, stream);
         return e == hipSuccess ? PAM_SUCCESS : fail_hip(e, "fill kernel launch");
     }
 
     pamk::GemmParams p{};
+    if (epi != nullptr)
+        p.epi = *epi;
     p.lda = lda;
     p.ldb = ldb;
     p.ldc = ldc;
@@ -544,14 +546,14 @@ pam_status_t run_gemm(pam_op_t ta, pam_op_t tb, int64_t m, int64_t n, int64_t k,
     p.splits = (int32_t)L.splits;
     float *ws = L.ws_bytes > 0 ? static_cast<float *>(ext->ptr) : nullptr;
 
-    if (whose != PlanOf::kCaller && skinny_product(ta, tb, plan, m, n, k, batch)) {
+    if (k > 0 && whose != PlanOf::kCaller && skinny_product(ta, tb, plan, m, n, k, batch)) {
         p.A = A;
         p.B = B;
         p.C = C;
         const hipError_t e = pamk::launch_pam_skinny(m <= n, bf16, p, batch, stream);
         return e == hipSuccess ? PAM_SUCCESS : fail_hip(e, "skinny product kernel launch");
     }
-    if (whose != PlanOf::kCaller && small_product(plan, whose, m, n, k, batch)) {
+    if (k > 0 && whose != PlanOf::kCaller && small_product(plan, whose, m, n, k, batch)) {
         p.A = A;
         p.B = B;
         p.C = C;
@@ -740,6 +742,20 @@ namespace pamk {
 pam_status_t api_fail(pam_status_t status, const char *message) { return fail(status, message); }
 pam_status_t api_fail_hip(hipError_t error, const char *what) { return fail_hip(error, what); }
 pam_status_t api_check_device() { return check_device(); }
+
+pam_status_t api_linear(int64_t m, int64_t n, int64_t k, const void *x, int64_t ldx, const void *w, int64_t ldw,
+                        const Epilogue &epi, bool bf16, int round_drop, void *workspace, size_t workspace_bytes,
+                        hipStream_t stream) {
+    const float *a = static_cast<const float *>(x), *b = static_cast<const float *>(w);
+    float *c = static_cast<float *>(epi.y);   // never written as such: outputs go by epi
+    const pam_status_t st = validate(PAM_OP_N, PAM_OP_T, m, n, k, a, ldx, 0, b, ldw, 0, c, epi.ldy, 0, 1);
+    if (st != PAM_SUCCESS || m == 0 || n == 0)
+        return st;
+    const Workspace ws{workspace, workspace_bytes};
+    return run_gemm(PAM_OP_N, PAM_OP_T, m, n, k, a, ldx, 0, b, ldw, 0, c, epi.ldy, 0, 1,
+                    choose_plan(m, n, k, 1, k > 0 ? kAnyWorkspace : 0), PlanOf::kLibrary, stream, round_drop, &ws, bf16,
+                    &epi);
+}
 
 }  // namespace pamk
 

@@ -77,6 +77,7 @@
 #include <type_traits>
 
 #include "pam_dma_tile.h"
+#include "pam_epilogue.h"
 #include "pam_internal.h"
 #include "pam_scalar.h"
 
@@ -225,7 +226,7 @@ constexpr int dma_min_lds_words(int bm, int bn, int kw, int wps) {
 // own: compiled in one, the edges' scalar values spilled into vector lanes
 // across the K loop and cost the other launches 3%, the clamp and blanks of
 // whole pieces past the last column (1) alone 1-3%.
-template <int BM, int BN, int KW, bool TA, bool TB, int WPS, int EDGE, typename T>
+template <int BM, int BN, int KW, bool TA, bool TB, int WPS, int EDGE, bool EPI, typename T>
 __global__ void __launch_bounds__(BM * BN / 64 * KW) __attribute__((amdgpu_waves_per_eu(WPS)))
 pam_gemm_dma_kernel(GemmParams p) {
     constexpr bool kKeepAddresses = WPS <= 2 || (WPS == 3 && !TA);
@@ -541,8 +542,55 @@ pam_gemm_dma_kernel(GemmParams p) {
                 }
             }
         }
-        if (grp > 0)
+        if (grp > 0 && !(EPI && whole))
             return;
+    }
+    // A linear layer's outputs.  The sums go through LDS, two rows of each
+    // thread's micro-tile at a time, so that the activation's code works on four
+    // values in a loop (beside the 64 sums of a thread it spilled 98 registers),
+    // with all threads of the workgroup, those of the other k-groups too.
+    if constexpr (EPI) {
+        if (whole) {
+            constexpr int kPart = 2;                // rows of a micro-tile at once
+            constexpr int kRows = BM / 8 * kPart;   // rows of the tile at once
+            constexpr int kLd = BN + 16;            // lanes 16 bytes apart, rows half the banks
+            static_assert(kRows * kLd <= kWords0 && NT % (BN / 4) == 0, "the epilogue's parts");
+            float *sums = reinterpret_cast<float *>(smem);
+            const int col = n0 + tid % (BN / 4) * 4, have = p.n - col;
+            float bias[4];
+            load_bias4(p.epi, col, have, bias);
+#pragma unroll 1
+            for (int part = 0; part < 8 / kPart; ++part) {
+                __syncthreads();   // the LDS is free
+                if (KW == 1 || grp == 0) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (i / kPart != part)
+                            continue;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            *reinterpret_cast<float4 *>(&sums[(ty * kPart + i % kPart) * kLd + h * HN + tx * 4]) =
+                                make_float4(acc[i][4 * h], acc[i][4 * h + 1], acc[i][4 * h + 2], acc[i][4 * h + 3]);
+                    }
+                }
+                __syncthreads();
+                with_activation(p.epi.activation, [&](auto act) {
+#pragma unroll 1
+                    for (int r = tid / (BN / 4); r < kRows; r += NT / (BN / 4)) {
+                        const int i = part * kPart + r % kPart;
+                        const int64_t row = m0 + r / kPart * 4 + (i < 4 ? i : HM + i - 4);
+                        if (row >= p.m)
+                            continue;
+                        float res[4];
+                        load_residual4(p.epi, row, col, have, res);
+                        const float4 x = *reinterpret_cast<const float4 *>(&sums[r * kLd + tid % (BN / 4) * 4]);
+                        const float v[4] = {x.x, x.y, x.z, x.w};
+                        finish4<decltype(act)::value>(p.epi, row, col, have, v, bias, res);
+                    }
+                });
+            }
+            return;
+        }
     }
     // Four outputs a store, at any address.
     typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
@@ -576,14 +624,23 @@ pam_gemm_dma_kernel(GemmParams p) {
 template <typename T, int BM, int BN, int KW, int WPS, int EDGE>
 static hipError_t launch_dma_kernel(bool ta, bool tb, const GemmParams &p, dim3 grid, hipStream_t stream) {
     const dim3 block(BM * BN / 64 * KW);
+    if (p.epi.y != nullptr) {   // linear layers: op N, op T, where no tile reads past its rows (EDGE 1)
+        if constexpr (EDGE != 1)
+            if (!ta && tb) {
+                hipLaunchKernelGGL((pam_gemm_dma_kernel<BM, BN, KW, false, true, WPS, EDGE, true, T>), grid, block, 0,
+                                   stream, p);
+                return hipGetLastError();
+            }
+        return hipErrorInvalidValue;
+    }
     if (!ta && !tb)
-        hipLaunchKernelGGL((pam_gemm_dma_kernel<BM, BN, KW, false, false, WPS, EDGE, T>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((pam_gemm_dma_kernel<BM, BN, KW, false, false, WPS, EDGE, false, T>), grid, block, 0, stream, p);
     else if (!ta && tb)
-        hipLaunchKernelGGL((pam_gemm_dma_kernel<BM, BN, KW, false, true, WPS, EDGE, T>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((pam_gemm_dma_kernel<BM, BN, KW, false, true, WPS, EDGE, false, T>), grid, block, 0, stream, p);
     else if (ta && !tb)
-        hipLaunchKernelGGL((pam_gemm_dma_kernel<BM, BN, KW, true, false, WPS, EDGE, T>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((pam_gemm_dma_kernel<BM, BN, KW, true, false, WPS, EDGE, false, T>), grid, block, 0, stream, p);
     else
-        hipLaunchKernelGGL((pam_gemm_dma_kernel<BM, BN, KW, true, true, WPS, EDGE, T>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((pam_gemm_dma_kernel<BM, BN, KW, true, true, WPS, EDGE, false, T>), grid, block, 0, stream, p);
     return hipGetLastError();
 }
 

@@ -1,7 +1,8 @@
 // Internal interface between the C-ABI layer (pam_api.cpp) and the HIP
 // kernels (pam_gemm_dma.hip, pam_skinny.hip, pam_small.hip, pam_kernels.hip,
 // pa_ops.hip, pam_exact_grad.hip).  The attention-side operators have theirs
-// in pam_attention_internal.h.  Not installed; not part of the public ABI.
+// in pam_attention_internal.h, the optimizer's and the activations' gradient
+// in pam_training_internal.h.  Not installed; not part of the public ABI.
 #pragma once
 
 #include <stdint.h>
@@ -13,6 +14,19 @@ namespace pamk {
 
 // K extent of one LDS chunk.
 constexpr int kChunkK = 16;
+
+// What a linear layer adds to its product (pam_linear of pam_training.h): with z
+// the product plus bias[column], y = activation(z) + residual.  Outputs and
+// residual are m x n, float32 or bfloat16 (out_bf16).
+struct Epilogue {
+    const float *bias;      // n values, or nullptr
+    const void *residual;   // or nullptr
+    void *y;                // nullptr: a product alone, into C
+    void *z;                // or nullptr
+    int64_t ldr, ldy, ldz;
+    int32_t activation;     // pam_activation_t
+    int32_t out_bf16;
+};
 
 // Arguments of one (batched, possibly split-K) PAM matrix product launch.
 //
@@ -41,6 +55,8 @@ struct GemmParams {
     // mantissas set each term's carry (row-major, leading dimension ldm).
     const float *Mod;
     int64_t ldm;
+    // Linear layers only (op N, op T, one matrix): epi.y in place of C.
+    Epilogue epi;
 };
 
 // Error text and device check of the C entry points (pam_api.cpp), shared by
@@ -48,6 +64,13 @@ struct GemmParams {
 pam_status_t api_fail(pam_status_t status, const char *message);
 pam_status_t api_fail_hip(hipError_t error, const char *what);
 pam_status_t api_check_device();
+
+// A linear layer's product (op N, op T) under the library's plan, its outputs
+// by epi; the workspace is pam_gemm_workspace_size's.  Sizes and leading
+// dimensions of x, w and y are validated here (pam_api.cpp).
+pam_status_t api_linear(int64_t m, int64_t n, int64_t k, const void *x, int64_t ldx, const void *w, int64_t ldw,
+                        const Epilogue &epi, bool bf16, int round_drop, void *workspace, size_t workspace_bytes,
+                        hipStream_t stream);
 
 hipError_t launch_pam_mul(const float *a, const float *b, float *out, int64_t n, hipStream_t stream);
 

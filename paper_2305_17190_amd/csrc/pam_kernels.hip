@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <mutex>
 
+#include "pam_epilogue.h"
 #include "pam_internal.h"
 
 namespace pamk {
@@ -26,7 +27,7 @@ __device__ __forceinline__ void store_out4(float *p, float a, float b, float c, 
 
 // Each workgroup adds the K slices of a 256 x 4-output part of one split
 // tile (grid-stride over the parts); each thread four consecutive outputs.
-__global__ void __launch_bounds__(256) split_tile_reduce_kernel(GemmParams p, int bm, int bn) {
+template <bool EPI> __global__ void __launch_bounds__(256) split_tile_reduce_kernel(GemmParams p, int bm, int bn) {
     const int gpr = bn / 4;                      // four-output groups per tile row
     const int parts = bm * bn / 4 / 256;         // parts per tile
     const int64_t tile_elems = (int64_t)bm * bn;
@@ -69,6 +70,11 @@ __global__ void __launch_bounds__(256) split_tile_reduce_kernel(GemmParams p, in
             sum.z += x.z;
             sum.w += x.w;
         }
+        if constexpr (EPI) {
+            const float sv[4] = {sum.x, sum.y, sum.z, sum.w};
+            finish4(p.epi, m0 + r, n0 + c, p.n - n0 - c, sv);
+            continue;
+        }
         float *crow = p.C + bz * p.strideC + (int64_t)(m0 + r) * p.ldc + n0;
         if (n0 + c + 3 < p.n) {
             store_out4(crow + c, sum.x, sum.y, sum.z, sum.w);
@@ -86,7 +92,10 @@ hipError_t launch_split_tile_reduce(int tile_m, int tile_n, const GemmParams &p,
         return hipSuccess;
     const int64_t parts = (int64_t)p.split_tiles * (tile_m * tile_n / 4 / 256);
     const int64_t blocks = std::min<int64_t>(parts, 256 * 32);
-    hipLaunchKernelGGL(split_tile_reduce_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, p, tile_m, tile_n);
+    if (p.epi.y != nullptr)
+        hipLaunchKernelGGL(split_tile_reduce_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, stream, p, tile_m, tile_n);
+    else
+        hipLaunchKernelGGL(split_tile_reduce_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, stream, p, tile_m, tile_n);
     return hipGetLastError();
 }
 

@@ -35,6 +35,7 @@
 
 #include <type_traits>
 
+#include "pam_epilogue.h"
 #include "pam_internal.h"
 #include "pam_scalar.h"
 
@@ -58,6 +59,7 @@ struct SkinnyParams {
     int32_t kwaves;   // waves of a workgroup that share one set of wide rows (1, 2, 4 or 8)
     int32_t d_tiles, s_tiles;
     int32_t round_drop;
+    Epilogue epi;   // linear layers: the outputs in place of C
 };
 
 __device__ __forceinline__ uint32_t round_bits(uint32_t u, int drop) {
@@ -118,7 +120,7 @@ struct Range {
     __device__ __forceinline__ bool wild() const { return most >= 0x7F000000u; }
 };
 
-template <int S, typename T>
+template <int S, bool EPI, typename T>
 __global__ void __launch_bounds__(64 * kWaves) pam_skinny_kernel(SkinnyParams p) {
     // A wave's skinny chunk: 1 + M_x and +-2^E_x, [plane][row][k].  After the
     // K loop the same bytes hold the waves' partial sums [wave][row][wide row].
@@ -316,6 +318,17 @@ __global__ void __launch_bounds__(64 * kWaves) pam_skinny_kernel(SkinnyParams p)
         }
     }
     if (kq < S && s0 + kq < p.s) {
+        if constexpr (EPI) {
+            if (p.cd == 1) {   // the few rows are x's
+                finish4(p.epi, s0 + kq, d0, p.d - d0, mineacc);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kJ; ++j)
+                    if (d0 + j < p.d)
+                        finish1(p.epi, d0 + j, s0 + kq, mineacc[j]);
+            }
+            return;
+        }
         float *out = p.C + bz * p.strideC + (int64_t)(s0 + kq) * p.cs + (int64_t)d0 * p.cd;
 #pragma unroll
         for (int j = 0; j < kJ; ++j)
@@ -352,21 +365,27 @@ hipError_t launch_pam_skinny(bool rows, bool bf16, const GemmParams &g, int64_t 
     if (items <= 0 || items > kMaxSkinnyItems)
         return hipErrorInvalidValue;
     const dim3 grid((unsigned)items), block(64 * kWaves);
-    if (bf16) {
-        if (cut.rows == 4)
-            hipLaunchKernelGGL((pam_skinny_kernel<4, uint16_t>), grid, block, 0, stream, p);
-        else if (cut.rows == 8)
-            hipLaunchKernelGGL((pam_skinny_kernel<8, uint16_t>), grid, block, 0, stream, p);
+    p.epi = g.epi;
+    auto launch = [&](auto rows_of, auto epi) {
+        constexpr int S = decltype(rows_of)::value;
+        constexpr bool E = decltype(epi)::value;
+        if (bf16)
+            hipLaunchKernelGGL((pam_skinny_kernel<S, E, uint16_t>), grid, block, 0, stream, p);
         else
-            hipLaunchKernelGGL((pam_skinny_kernel<16, uint16_t>), grid, block, 0, stream, p);
-    } else {
+            hipLaunchKernelGGL((pam_skinny_kernel<S, E, float>), grid, block, 0, stream, p);
+    };
+    auto choose = [&](auto epi) {
         if (cut.rows == 4)
-            hipLaunchKernelGGL((pam_skinny_kernel<4, float>), grid, block, 0, stream, p);
+            launch(std::integral_constant<int, 4>{}, epi);
         else if (cut.rows == 8)
-            hipLaunchKernelGGL((pam_skinny_kernel<8, float>), grid, block, 0, stream, p);
+            launch(std::integral_constant<int, 8>{}, epi);
         else
-            hipLaunchKernelGGL((pam_skinny_kernel<16, float>), grid, block, 0, stream, p);
-    }
+            launch(std::integral_constant<int, 16>{}, epi);
+    };
+    if (g.epi.y != nullptr)
+        choose(std::true_type{});
+    else
+        choose(std::false_type{});
     return hipGetLastError();
 }
 

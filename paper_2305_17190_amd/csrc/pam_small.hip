@@ -30,6 +30,7 @@
 #include <type_traits>
 
 #include "pam_dma_tile.h"
+#include "pam_epilogue.h"
 #include "pam_internal.h"
 #include "pam_scalar.h"
 
@@ -43,7 +44,7 @@ __device__ __forceinline__ void quad(const uint32_t *p, uint32_t (&e)[4]) {
     e[0] = x.x; e[1] = x.y; e[2] = x.z; e[3] = x.w;
 }
 
-template <int KW, bool TA, bool TB, typename T>
+template <int KW, bool TA, bool TB, bool EPI, typename T>
 __global__ void __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(4))) pam_small_kernel(GemmParams p) {
     constexpr int D = kTile, KPG = kChunkK, BK = KPG * KW, NT = 64 * KW;
     using TileA = DmaTile<D, BK, NT, !TA, T>;
@@ -227,7 +228,10 @@ __global__ void __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(4)
         for (int g = 1; g < KW; ++g)
             s += red[g * D * D + o];
         const int row = o / D, col = o % D;
-        if (m0 + row < p.m && n0 + col < p.n)
+        if constexpr (EPI) {
+            if (m0 + row < p.m && n0 + col < p.n)
+                finish1(p.epi, m0 + row, n0 + col, s);
+        } else if (m0 + row < p.m && n0 + col < p.n)
             out[(int64_t)row * p.ldc + col] = s;
     }
 }
@@ -235,14 +239,20 @@ __global__ void __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(4)
 template <int KW, typename T>
 hipError_t launch(bool ta, bool tb, const GemmParams &p, dim3 grid, hipStream_t stream) {
     const dim3 block(64 * KW);
+    if (p.epi.y != nullptr) {   // linear layers: op N, op T
+        if (ta || !tb)
+            return hipErrorInvalidValue;
+        hipLaunchKernelGGL((pam_small_kernel<KW, false, true, true, T>), grid, block, 0, stream, p);
+        return hipGetLastError();
+    }
     if (!ta && !tb)
-        hipLaunchKernelGGL((pam_small_kernel<KW, false, false, T>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((pam_small_kernel<KW, false, false, false, T>), grid, block, 0, stream, p);
     else if (!ta && tb)
-        hipLaunchKernelGGL((pam_small_kernel<KW, false, true, T>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((pam_small_kernel<KW, false, true, false, T>), grid, block, 0, stream, p);
     else if (ta && !tb)
-        hipLaunchKernelGGL((pam_small_kernel<KW, true, false, T>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((pam_small_kernel<KW, true, false, false, T>), grid, block, 0, stream, p);
     else
-        hipLaunchKernelGGL((pam_small_kernel<KW, true, true, T>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((pam_small_kernel<KW, true, true, false, T>), grid, block, 0, stream, p);
     return hipGetLastError();
 }
 

@@ -1,0 +1,422 @@
+// The layer-and-step side's streams over memory on gfx950: the activations'
+// gradient with the bias's, the norm of all gradients, and the AdamW step over
+// many tensors.  All are bound by reading and writing each value once.
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "pam_epilogue.h"
+#include "pam_training_internal.h"
+
+namespace pamk {
+namespace {
+
+// V neighbouring elements, at any address, widened; `have` of them exist.
+template <int V, typename T> __device__ __forceinline__ void load_wide(const T *p, int have, float (&x)[V]) {
+    typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+    if (have >= V) {
+        const vec v = *reinterpret_cast<const vec *>(p);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if constexpr (sizeof(T) == 2)
+                x[i] = bf16_value(v[i]);
+            else
+                x[i] = v[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if constexpr (sizeof(T) == 2)
+                x[i] = i < have ? bf16_value(p[i]) : 0.0f;
+            else
+                x[i] = i < have ? p[i] : 0.0f;
+        }
+    }
+}
+template <int V, typename T> __device__ __forceinline__ void store_wide(T *p, int have, const float (&x)[V]) {
+    typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+    vec v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        if constexpr (sizeof(T) == 2)
+            v[i] = bf16_bits(x[i]);
+        else
+            v[i] = x[i];
+    }
+    if (have >= V) {
+        *reinterpret_cast<vec *>(p) = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < have)
+                p[i] = v[i];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The activations' gradient
+// ---------------------------------------------------------------------------
+
+// dz = dy f'(z) and the sums of its columns.  A thread keeps the sums of its V
+// columns over the rows it takes; the workgroup's rows are added in a tree, in
+// LDS, and the bands' sums by sum_bands_kernel: an order fixed by the sizes.
+template <typename T, typename Z> __global__ void __launch_bounds__(kGradThreads) activation_grad_kernel(GradParams p) {
+    constexpr int V = 16 / sizeof(T);
+    __shared__ float red[kGradThreads * V];
+    const int lanes = p.lanes, at_once = kGradThreads / lanes;
+    const int tx = threadIdx.x % lanes, ty = threadIdx.x / lanes;
+    const int groups = (p.n + lanes * V - 1) / (lanes * V);
+    const int band = blockIdx.x / groups;
+    const int col = (blockIdx.x - band * groups) * lanes * V + tx * V;
+    const int have = min(p.n - col, V);
+    const int64_t end = min((int64_t)(band + 1) * p.band, p.m);
+    float sum[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        sum[i] = 0.0f;
+    if (have > 0) {
+        const T *dy = static_cast<const T *>(p.dy) + col;
+        const Z *z = static_cast<const Z *>(p.z) + col;
+        T *dz = static_cast<T *>(p.dz) + col;
+        with_activation(p.activation, [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
+#pragma unroll 4
+            for (int64_t r = (int64_t)band * p.band + ty; r < end; r += at_once) {
+                float d[V], x[V];
+                load_wide<V>(dy + r * p.lddy, have, d);
+                if constexpr (ACT != PAM_ACT_NONE) {
+                    load_wide<V>(z + r * p.ldz, have, x);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        if constexpr (ACT == PAM_ACT_RELU)
+                            d[i] = x[i] <= 0.0f ? 0.0f : d[i];
+                        else
+                            d[i] *= activation_slope<ACT>(x[i]);
+                    }
+                    if (p.dz != nullptr)
+                        store_wide<V>(dz + r * p.lddz, have, d);
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    sum[i] += d[i];
+            }
+        });
+    }
+    if (p.db == nullptr)
+        return;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        red[threadIdx.x * V + i] = sum[i];
+    for (int half = at_once / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (ty < half) {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                red[threadIdx.x * V + i] += red[(threadIdx.x + half * lanes) * V + i];
+        }
+    }
+    if (ty != 0)
+        return;
+    float *out = p.bands == 1 ? p.db : p.partial + (int64_t)band * p.n;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (i < have)
+            out[col + i] = red[threadIdx.x * V + i];
+}
+
+// db = the sum of the bands' sums: 64 columns a workgroup, a quarter of the bands
+// a wave.
+__global__ void __launch_bounds__(256) sum_bands_kernel(const float *__restrict__ partial, float *__restrict__ db,
+                                                        int bands, int n) {
+    __shared__ float red[256];
+    const int col = blockIdx.x * 64 + (threadIdx.x & 63), part = threadIdx.x >> 6;
+    float sum = 0.0f;
+    if (col < n) {
+#pragma unroll 8
+        for (int b = part; b < bands; b += 4)
+            sum += partial[(int64_t)b * n + col];
+    }
+    red[threadIdx.x] = sum;
+    __syncthreads();
+    if (part == 0 && col < n)
+        db[col] = (sum + red[threadIdx.x + 64]) + (red[threadIdx.x + 128] + red[threadIdx.x + 192]);
+}
+
+// ---------------------------------------------------------------------------
+// Many tensors at once
+// ---------------------------------------------------------------------------
+
+// The tensor that workgroup b works on: the last whose first workgroup is not
+// after it.  Each lane compares one.
+__device__ __forceinline__ int tensor_of(const uint32_t *first, int count, uint32_t b) {
+    const int lane = threadIdx.x & 63;
+    const bool before = lane < count && first[min(lane, count - 1)] <= b;
+    return __builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) - 1;
+}
+
+template <typename T> __global__ void __launch_bounds__(kStepThreads) grad_squares_kernel(NormParams p) {
+    constexpr int V = 16 / sizeof(T);
+    __shared__ double red[kStepThreads / 64];
+    const int j = tensor_of(p.first, p.count, blockIdx.x);
+    const int64_t begin = (int64_t)(blockIdx.x - p.first[j]) * p.chunk;
+    const int64_t end = min(begin + p.chunk, p.n[j]);
+    const T *g = static_cast<const T *>(p.g[j]);
+    // In float64: a sum of 2^26 squares keeps its last bit, none overflows.
+    double sum = 0.0;
+#pragma unroll 4
+    for (int64_t i = begin + threadIdx.x * V; i < end; i += kStepThreads * V) {
+        float x[V];
+        load_wide<V>(g + i, (int)min(end - i, (int64_t)V), x);
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            sum = __builtin_fma((double)x[e], (double)x[e], sum);
+    }
+    for (int d = 32; d > 0; d /= 2)
+        sum += __shfl_xor(sum, d);
+    if ((threadIdx.x & 63) == 0)
+        red[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        p.partial[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+__global__ void __launch_bounds__(1024) grad_norm_kernel(const double *__restrict__ partial, int64_t count, float *norm) {
+    __shared__ double red[16];
+    double sum = 0.0;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < count; i += 1024)
+        sum += partial[i];
+    for (int d = 32; d > 0; d /= 2)
+        sum += __shfl_xor(sum, d);
+    if ((threadIdx.x & 63) == 0)
+        red[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 16; ++w)
+            sum += red[w];
+        *norm = (float)sqrt(sum);
+    }
+}
+
+// What the whole step has in common.
+struct Rates {
+    float step_size, sq_factor, clip;
+    uint32_t key;     // of the tensor's random bits
+};
+
+__device__ __forceinline__ uint32_t mix(uint32_t x) {
+    x = (x ^ (x >> 16)) * 0x7FEB352Du;
+    x = (x ^ (x >> 15)) * 0x846CA68Bu;
+    return x ^ (x >> 16);
+}
+
+__device__ __forceinline__ Rates rates_of(const StepParams &p, int tensor) {
+    Rates r{p.step_size, p.sq_factor, 1.0f, 0u};
+    int64_t step = p.step;
+    if (p.step_device != nullptr) {
+        step = *p.step_device;
+        r.step_size = (float)(p.step_size / -expm1((double)step * p.log_beta1));
+        r.sq_factor = (float)(1.0 / sqrt(-expm1((double)step * p.log_beta2)));
+    }
+    if (p.norm != nullptr) {
+        const float c = p.max_norm / (*p.norm + 1e-6f);
+        r.clip = c >= 1.0f ? 1.0f : c;   // NaN stays
+    }
+    r.key = mix(mix(p.seed + (uint32_t)step * 0x9E3779B9u) + (uint32_t)(p.tensor0 + tensor));
+    return r;
+}
+
+__device__ __forceinline__ float moved(const StepParams &p, const Rates &r, float x, float avg, float sq) {
+    // Within 2 units of 2^-23 of the step; the step is small beside p.
+    const float by = __builtin_fmaf(__builtin_amdgcn_sqrtf(sq), r.sq_factor, p.eps);
+    return __builtin_fmaf(-r.step_size, avg * __builtin_amdgcn_rcpf(by), x * p.keep);
+}
+
+template <typename G> __global__ void __launch_bounds__(kStepThreads) adamw_kernel(StepParams p) {
+    const int j = tensor_of(p.first, p.count, blockIdx.x);
+    const pam_step_tensor_t &t = p.tensor[j];
+    const Rates rates = rates_of(p, j);
+    const int64_t begin = (int64_t)(blockIdx.x - p.first[j]) * p.chunk;
+    const int64_t end = min(begin + p.chunk, t.n);
+    const G *g = static_cast<const G *>(t.g);
+    float *avg = static_cast<float *>(t.avg), *sq = static_cast<float *>(t.sq);
+#pragma unroll 2
+    for (int64_t i = begin + threadIdx.x * 4; i < end; i += kStepThreads * 4) {
+        const int have = (int)min(end - i, (int64_t)4);
+        float x[4], d[4], m[4], v[4];
+        load_wide<4>(g + i, have, d);
+        load_wide<4>(t.p + i, have, x);
+        load_wide<4>(avg + i, have, m);
+        load_wide<4>(sq + i, have, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            d[e] *= rates.clip;
+            m[e] = __builtin_fmaf(m[e], p.beta1, d[e] * p.rest1);
+            v[e] = __builtin_fmaf(v[e], p.beta2, d[e] * p.rest2 * d[e]);
+            x[e] = moved(p, rates, x[e], m[e], v[e]);
+        }
+        store_wide<4>(avg + i, have, m);
+        store_wide<4>(sq + i, have, v);
+        store_wide<4>(t.p + i, have, x);
+        if (t.copy != nullptr)
+            store_wide<4>(t.copy + i, have, x);
+    }
+}
+
+// 8-bit states --------------------------------------------------------------
+
+constexpr uint32_t kAvgLow = 889, kAvgMost = 127, kSqLow = 761, kSqMost = 255;
+
+__device__ __forceinline__ float held(uint32_t code, uint32_t low, float scale) {
+    return (code != 0u ? __uint_as_float((code + low) << 20) : 0.0f) * scale;
+}
+
+// The code of a magnitude as a part of its block's scale (NaN: the largest).
+__device__ __forceinline__ uint32_t coded(float x, float scale, uint32_t random, uint32_t low, uint32_t most) {
+    const float part = x / (scale > 0.0f ? scale : 1.0f);
+    const uint32_t c = (__float_as_uint(part) + random) >> 20;
+    return c <= low ? 0u : min(c - low, most);
+}
+
+// The largest of the wave's values, by their encodings (no sign): NaN above all.
+__device__ __forceinline__ float largest(const float (&x)[4]) {
+    uint32_t u = max(max(__float_as_uint(x[0]), __float_as_uint(x[1])), max(__float_as_uint(x[2]), __float_as_uint(x[3])));
+    for (int d = 32; d > 0; d /= 2)
+        u = max(u, (uint32_t)__shfl_xor((int)u, d));
+    return __uint_as_float(u);
+}
+
+// Four codes from c, at any address; `have` of them exist.
+__device__ __forceinline__ uint32_t load_codes(const uint8_t *c, int have) {
+    typedef uint32_t word __attribute__((aligned(1)));
+    if (have >= 4)
+        return *reinterpret_cast<const word *>(c);
+    uint32_t w = 0u;
+    for (int i = 0; i < have; ++i)
+        w |= (uint32_t)c[i] << (8 * i);
+    return w;
+}
+__device__ __forceinline__ void store_codes(uint8_t *c, int have, uint32_t w) {
+    typedef uint32_t word __attribute__((aligned(1)));
+    if (have >= 4) {
+        *reinterpret_cast<word *>(c) = w;
+    } else {
+        for (int i = 0; i < have; ++i)
+            c[i] = (uint8_t)(w >> (8 * i));
+    }
+}
+
+// A wave holds a block of 256 values, four a lane: its scales are maxima over
+// the wave, so that the states are read and written once.
+template <typename G> __global__ void __launch_bounds__(kStepThreads) adamw8_kernel(StepParams p) {
+    const int j = tensor_of(p.first, p.count, blockIdx.x);
+    const pam_step_tensor_t &t = p.tensor[j];
+    const Rates rates = rates_of(p, j);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t begin = (int64_t)(blockIdx.x - p.first[j]) * p.chunk;
+    const int64_t end = min(begin + p.chunk, t.n);
+    const G *g = static_cast<const G *>(t.g);
+    uint8_t *avg = static_cast<uint8_t *>(t.avg), *sq = static_cast<uint8_t *>(t.sq);
+#pragma unroll 1
+    for (int64_t b = begin + wave * PAM_STATE_BLOCK; b < end; b += kStepThreads / 64 * PAM_STATE_BLOCK) {
+        const int64_t i = b + lane * 4, block = b / PAM_STATE_BLOCK;
+        const int have = (int)max(min(end - i, (int64_t)4), (int64_t)0);
+        float x[4], d[4], m[4], v[4], size[4];
+        load_wide<4>(g + i, have, d);
+        load_wide<4>(t.p + i, have, x);
+        const uint32_t mc = load_codes(avg + i, have), vc = load_codes(sq + i, have);
+        const float ms = t.avg_scale[block], vs = t.sq_scale[block];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            // Each operation rounded by itself, as the codes' definition has it.
+#pragma clang fp contract(off)
+            const uint32_t c = (mc >> (8 * e)) & 0xFFu;
+            const float old = held(c & kAvgMost, kAvgLow, ms);
+            d[e] = d[e] * rates.clip;
+            const float m0 = (c > kAvgMost ? -old : old) * p.beta1, m1 = d[e] * p.rest1;
+            const float v0 = held((vc >> (8 * e)) & 0xFFu, kSqLow, vs) * p.beta2, v1 = d[e] * p.rest2 * d[e];
+            m[e] = m0 + m1;
+            v[e] = v0 + v1;
+            if (e >= have)
+                m[e] = v[e] = 0.0f;
+            size[e] = __builtin_fabsf(m[e]);
+        }
+        const float ms1 = largest(size), vs1 = largest(v);
+        uint32_t mw = 0u, vw = 0u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t h = mix((uint32_t)(i + e) + rates.key);
+            const uint32_t cm = coded(size[e], ms1, ((h & 0xFFFFu) << 4) + 8u, kAvgLow, kAvgMost);
+            const uint32_t cv = coded(v[e], vs1, ((h >> 16) << 4) + 8u, kSqLow, kSqMost);
+            mw |= (cm | (cm != 0u && m[e] < 0.0f ? 128u : 0u)) << (8 * e);
+            vw |= (v[e] != 0.0f ? max(cv, 1u) : 0u) << (8 * e);
+            x[e] = moved(p, rates, x[e], m[e], v[e]);
+        }
+        store_codes(avg + i, have, mw);
+        store_codes(sq + i, have, vw);
+        store_wide<4>(t.p + i, have, x);
+        if (t.copy != nullptr)
+            store_wide<4>(t.copy + i, have, x);
+        if (lane == 0) {
+            t.avg_scale[block] = ms1;
+            t.sq_scale[block] = vs1;
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_activation_grad(bool bf16, bool z_bf16, const GradParams &p, hipStream_t stream) {
+    const int wide = p.lanes * grad_values(bf16);
+    const int64_t groups = ((int64_t)p.n + wide - 1) / wide * p.bands;
+    if (groups <= 0 || groups > kMostStepGroups)
+        return hipErrorInvalidValue;
+    const dim3 grid((unsigned)groups), block(kGradThreads);
+    if (bf16 && z_bf16)
+        hipLaunchKernelGGL((activation_grad_kernel<uint16_t, uint16_t>), grid, block, 0, stream, p);
+    else if (bf16)
+        hipLaunchKernelGGL((activation_grad_kernel<uint16_t, float>), grid, block, 0, stream, p);
+    else if (z_bf16)
+        hipLaunchKernelGGL((activation_grad_kernel<float, uint16_t>), grid, block, 0, stream, p);
+    else
+        hipLaunchKernelGGL((activation_grad_kernel<float, float>), grid, block, 0, stream, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.db == nullptr || p.bands == 1)
+        return e;
+    hipLaunchKernelGGL(sum_bands_kernel, dim3((unsigned)((p.n + 63) / 64)), dim3(256), 0, stream, p.partial, p.db,
+                       p.bands, p.n);
+    return hipGetLastError();
+}
+
+hipError_t launch_grad_squares(uint32_t groups, const NormParams &p, hipStream_t stream) {
+    if (p.grad_bf16)
+        hipLaunchKernelGGL(grad_squares_kernel<uint16_t>, dim3(groups), dim3(kStepThreads), 0, stream, p);
+    else
+        hipLaunchKernelGGL(grad_squares_kernel<float>, dim3(groups), dim3(kStepThreads), 0, stream, p);
+    return hipGetLastError();
+}
+
+hipError_t launch_grad_norm(const double *partial, int64_t count, float *norm, hipStream_t stream) {
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, stream, partial, count, norm);
+    return hipGetLastError();
+}
+
+hipError_t launch_adamw(int state_bits, uint32_t groups, const StepParams &p, hipStream_t stream) {
+    const dim3 grid(groups), block(kStepThreads);
+    if (state_bits == 32) {
+        if (p.grad_bf16)
+            hipLaunchKernelGGL(adamw_kernel<uint16_t>, grid, block, 0, stream, p);
+        else
+            hipLaunchKernelGGL(adamw_kernel<float>, grid, block, 0, stream, p);
+    } else {
+        if (p.grad_bf16)
+            hipLaunchKernelGGL(adamw8_kernel<uint16_t>, grid, block, 0, stream, p);
+        else
+            hipLaunchKernelGGL(adamw8_kernel<float>, grid, block, 0, stream, p);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace pamk

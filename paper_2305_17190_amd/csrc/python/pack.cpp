@@ -1,4 +1,4 @@
-// The tensors of a call for attention.py.  pack reads the inputs: what a call's
+// The tensors of a call for attention.py and training.py.  pack reads the inputs: what a call's
 // argument checks depend on, as one hashable key, and the addresses, as the bytes
 // its argument structure begins with.  (In Python, type, shape, strides, device
 // and address of append_kv's eleven tensors took 5 of its 10 us of host time.)
@@ -15,6 +15,7 @@
 
 #include <cstdint>
 #include <memory>
+#include <vector>
 
 namespace {
 
@@ -117,8 +118,133 @@ PyObject *make(PyObject *, PyObject *const *args, Py_ssize_t count) {
     END_HANDLE_TH_ERRORS
 }
 
+// matrices(tensor, bytes, type, rows, columns, type, rows, columns) -> (matrix or
+// None, matrix or None, workspace or None, addresses): contiguous matrices of
+// float32 (type 0) or bfloat16 (1; -1: none) on the tensor's device, vectors where
+// rows < 0, and a workspace of so many bytes.
+PyObject *matrices(PyObject *, PyObject *const *args, Py_ssize_t count) {
+    HANDLE_TH_ERRORS
+    if (count != 8 || !THPVariable_Check(args[0])) {
+        PyErr_SetString(PyExc_TypeError, "matrices takes a tensor, a number of bytes and two matrices' types and sizes");
+        return nullptr;
+    }
+    long long number[8];
+    for (int i = 1; i < 8; ++i)
+        number[i] = PyLong_AsLongLong(args[i]);
+    if (PyErr_Occurred())
+        return nullptr;
+    const at::TensorOptions options = THPVariable_Unpack(args[0]).options();
+    at::Tensor made[3];
+    {
+        pybind11::gil_scoped_release others;
+        for (int i = 0; i < 2; ++i) {
+            const long long *want = number + 2 + 3 * i;
+            if (want[0] < 0)
+                continue;
+            const at::TensorOptions typed = options.dtype(want[0] == 0 ? at::kFloat : at::kBFloat16);
+            made[i] = want[1] < 0 ? at::empty({(int64_t)want[2]}, typed)
+                                  : at::empty({(int64_t)want[1], (int64_t)want[2]}, typed);
+        }
+        if (number[1] > 0)
+            made[2] = at::empty({(int64_t)number[1]}, options.dtype(at::kByte));
+    }
+    int64_t address[3];
+    std::unique_ptr<PyObject, void (*)(PyObject *)> results(PyTuple_New(4), Py_DecRef);
+    if (!results)
+        return nullptr;
+    for (int i = 0; i < 3; ++i) {
+        address[i] = made[i].defined() ? (int64_t)made[i].data_ptr() : 0;
+        PyObject *item = THPVariable_Wrap(made[i]);
+        if (item == nullptr)
+            return nullptr;
+        PyTuple_SET_ITEM(results.get(), i, item);
+    }
+    PyObject *addresses = PyBytes_FromStringAndSize((const char *)address, (Py_ssize_t)sizeof address);
+    if (addresses == nullptr)
+        return nullptr;
+    PyTuple_SET_ITEM(results.get(), 3, addresses);
+    return results.release();
+    END_HANDLE_TH_ERRORS
+}
+
+// step(params, grads, avgs, sqs, avg_scales, sq_scales, copies) -> (count, the
+// array of pam_step_tensor_t, whether the gradients are bfloat16, whether the
+// states are bytes, the first gradient or None), or None where the lists are not
+// what the call takes: the caller's checks then say why.  Each is a list or tuple
+// of tensors or, but for the gradients, None.  What the call writes counts as
+// changed in place.
+PyObject *step(PyObject *, PyObject *const *args, Py_ssize_t count) {
+    HANDLE_TH_ERRORS
+    constexpr int kLists = 7, kGrads = 1;
+    constexpr int64_t kBlock = 256;
+    if (count != kLists)
+        Py_RETURN_NONE;
+    PyObject *const *items[kLists] = {};
+    Py_ssize_t n = -1;
+    for (int l = 0; l < kLists; ++l) {
+        if (args[l] == Py_None)
+            continue;
+        if (!PyList_Check(args[l]) && !PyTuple_Check(args[l]))
+            Py_RETURN_NONE;
+        const Py_ssize_t have = PySequence_Fast_GET_SIZE(args[l]);
+        if (n >= 0 && have != n)
+            Py_RETURN_NONE;
+        n = have;
+        items[l] = PySequence_Fast_ITEMS(args[l]);
+    }
+    const bool whole = args[0] != Py_None;   // a step, not the norm alone
+    if (args[kGrads] == Py_None || (whole && (args[2] == Py_None || args[3] == Py_None)) ||
+        (args[4] == Py_None) != (args[5] == Py_None))
+        Py_RETURN_NONE;
+    const bool scales = args[4] != Py_None;
+    const at::ScalarType held = scales ? at::kByte : at::kFloat;
+    at::ScalarType grad = at::kFloat;
+    c10::Device device(c10::kCPU);
+    std::vector<int64_t> array((size_t)n * 8);
+    for (Py_ssize_t j = 0; j < n; ++j) {
+        int64_t *one = array.data() + j * 8;
+        if (!THPVariable_Check(items[kGrads][j]))
+            Py_RETURN_NONE;
+        const at::Tensor &g = THPVariable_Unpack(items[kGrads][j]);
+        if (j == 0) {
+            grad = g.scalar_type();
+            device = g.device();
+            if ((grad != at::kFloat && grad != at::kBFloat16) || !device.is_cuda())
+                Py_RETURN_NONE;
+        }
+        const int64_t values = g.numel();
+        const at::ScalarType types[kLists] = {at::kFloat, grad, held, held, at::kFloat, at::kFloat, at::kBFloat16};
+        for (int l = 0; l < kLists; ++l) {
+            if (args[l] == Py_None)
+                continue;
+            if (!THPVariable_Check(items[l][j]))
+                Py_RETURN_NONE;
+            const at::Tensor &t = THPVariable_Unpack(items[l][j]);
+            const bool scale = l == 4 || l == 5;
+            if (t.layout() != at::kStrided || t.scalar_type() != types[l] || t.device() != device ||
+                !t.is_contiguous() || t.numel() != (scale ? (values + kBlock - 1) / kBlock : values))
+                Py_RETURN_NONE;
+            one[l] = (int64_t)t.data_ptr();
+        }
+        one[7] = values;
+    }
+    for (int l = 0; l < kLists; ++l)
+        for (Py_ssize_t j = 0; j < n && l != kGrads && args[l] != Py_None; ++j) {
+            const at::Tensor &t = THPVariable_Unpack(items[l][j]);
+            if (!t.is_inference())
+                t.unsafeGetTensorImpl()->bump_version();
+        }
+    return Py_BuildValue("(ny#iiO)", n, (const char *)array.data(), (Py_ssize_t)(array.size() * sizeof(int64_t)),
+                         (int)(grad == at::kBFloat16), (int)scales, n > 0 ? items[kGrads][0] : Py_None);
+    END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {{"make", (PyCFunction)(void *)make, METH_FASTCALL,
                           "make(type, bytes, tensor or None, ...) -> (result, ..., workspace, addresses)"},
+                         {"matrices", (PyCFunction)(void *)matrices, METH_FASTCALL,
+                          "matrices(tensor, bytes, type, rows, columns, type, rows, columns)"},
+                         {"step", (PyCFunction)(void *)step, METH_FASTCALL,
+                          "step(params, grads, avgs, sqs, avg_scales, sq_scales, copies)"},
                          {"pack", (PyCFunction)(void *)pack, METH_FASTCALL, "pack(tensor or None, ...) -> (key, addresses)"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pack", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

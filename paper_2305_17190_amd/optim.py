@@ -1,0 +1,95 @@
+"""The optimizer of PAM models: AdamW over all parameters in a few launches, the
+gradients' common norm limited and the states held in 8 or in 32 bits
+(``pam.grad_norm``, ``pam.adamw_step``)."""
+from __future__ import annotations
+
+import torch
+
+from . import adamw_step as _adamw_step
+from . import grad_norm as _grad_norm
+from .training import STATE_BLOCK
+
+__all__ = ["AdamW"]
+
+
+class AdamW(torch.optim.Optimizer):
+    """AdamW with decoupled weight decay over float32 HIP parameters.
+
+    ``max_norm`` limits the common norm of all gradients of a step (its value:
+    ``last_norm``, a tensor).  ``state_bits=8`` keeps the two averages of the
+    gradients in a byte a value, and 8 bytes a block of 256, in place of 8
+    bytes a value; their rounding is stochastic, by ``seed``.  A parameter
+    without a gradient is passed over.  ``step`` counts on the host: inside a
+    captured graph use ``pam.adamw_step`` with a step on the device."""
+
+    def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
+                 max_norm: float = None, state_bits: int = 32, seed: int = 0):
+        if state_bits not in (8, 32):
+            raise ValueError(f"state_bits must be 8 or 32, got {state_bits}")
+        if max_norm is not None and not max_norm > 0:
+            raise ValueError(f"max_norm must be > 0, got {max_norm}")
+        self.max_norm, self.state_bits, self.seed = max_norm, state_bits, seed
+        self.last_norm = None
+        super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
+
+    def _state_of(self, p):
+        state = self.state[p]
+        if not state:
+            state["step"] = 0
+            if self.state_bits == 32:
+                state["avg"], state["sq"] = (torch.zeros_like(p, memory_format=torch.contiguous_format) for _ in range(2))
+            else:
+                state["avg"], state["sq"] = (torch.zeros(p.shape, dtype=torch.uint8, device=p.device) for _ in range(2))
+                state["avg_scale"], state["sq_scale"] = (
+                    torch.zeros(-(-p.numel() // STATE_BLOCK), device=p.device) for _ in range(2))
+        return state
+
+    def load_state_dict(self, state_dict) -> None:
+        """As torch's, but the loaded tensors are copied, and codes stay bytes (torch
+        makes every state the parameter's type)."""
+        for state in state_dict["state"].values():
+            if state and ("avg_scale" in state) != (self.state_bits == 8):
+                raise ValueError(f"the loaded states are not held in {self.state_bits} bits")
+        super().load_state_dict(state_dict)
+        for state in self.state.values():
+            for key in ("avg", "sq", "avg_scale", "sq_scale"):
+                if key in state:
+                    codes = self.state_bits == 8 and not key.endswith("_scale")
+                    state[key] = state[key].to(torch.uint8 if codes else torch.float32, copy=True).contiguous()
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("a captured step would not count on: use pam.adamw_step with a step on the device")
+        # Parameters of one group that have made as many steps go together.
+        together = {}
+        for index, group in enumerate(self.param_groups):
+            for p in group["params"]:
+                if p.grad is None:
+                    continue
+                if p.grad.is_sparse:
+                    raise RuntimeError("AdamW takes dense gradients")
+                state = self._state_of(p)
+                together.setdefault((index, state["step"]), []).append((p, p.grad.contiguous(), state))
+        if not together:
+            return loss
+        norm = None
+        if self.max_norm is not None:
+            norm = self.last_norm = _grad_norm([g for some in together.values() for _, g, _ in some])
+        for (index, step), some in together.items():
+            group = self.param_groups[index]
+            params, grads, states = zip(*some)
+            scales = {}
+            if self.state_bits == 8:
+                scales = dict(avg_scales=[s["avg_scale"] for s in states], sq_scales=[s["sq_scale"] for s in states])
+            # A seed of its own for each group: tensors are numbered within a call.
+            _adamw_step(params, grads, [s["avg"] for s in states], [s["sq"] for s in states], step + 1, lr=group["lr"],
+                        betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"], norm=norm,
+                        max_norm=self.max_norm, seed=self.seed + 0x51ED27 * index, **scales)
+            for s in states:
+                s["step"] = step + 1
+        return loss
