@@ -57,10 +57,11 @@ typedef enum {
  *   residual: m x n of out_type, or NULL; y itself (with ldr == ldy) is allowed
  *   y, z: m x n of out_type; z may be NULL (not written).  float32 arithmetic,
  *       rounded once
- *   workspace: pam_gemm_workspace_size(m, n, k, 1) bytes, 16-byte aligned (NULL
- *       if those are 0)
- * The product is pam_gemm_batched_ws's, sum for sum.  k == 0 counts as a
- * product of zeros.
+ *   workspace: pam_linear_workspace_size bytes, 16-byte aligned (NULL if those
+ *       are 0)
+ * The product's plan is pam_gemm_plan's; its tiles take long sums in parts of
+ * 1024 terms (up to k = 1024 the sums are pam_gemm_batched_ws's, bit for bit).
+ * k == 0 counts as a product of zeros.
  */
 typedef struct {
     const void *x, *w;
@@ -75,6 +76,7 @@ typedef struct {
     pam_activation_t activation;
     int32_t mantissa_bits;
 } pam_linear_t;
+pam_status_t pam_linear_workspace_size(int64_t m, int64_t n, int64_t k, size_t *bytes);
 pam_status_t pam_linear(const pam_linear_t *args, hipStream_t stream);
 
 /*

@@ -501,6 +501,27 @@ bool small_product(const Plan &plan, PlanOf whose, int64_t m, int64_t n, int64_t
     return whose == PlanOf::kLibrary || same_plan(plan, choose_plan(m, n, k, batch, kAnyWorkspace));
 }
 
+// A linear layer's workspace: the plan's partial sums, then the tiles' running
+// sums where a chain would be longer than kFoldChunks chunks.
+struct LinearSpace {
+    size_t partial, folds;
+};
+
+pam_status_t linear_space(const Plan &plan, int64_t m, int64_t n, int64_t k, LinearSpace *out) {
+    Layout L{};
+    const pam_status_t st = layout_of(plan, m, n, 1, &L);
+    if (st != PAM_SUCCESS)
+        return st;
+    *out = {(L.ws_bytes + 255) / 256 * 256, 0};
+    const bool other = k > 0 && (skinny_product(PAM_OP_N, PAM_OP_T, plan, m, n, k, 1) ||
+                                 small_product(plan, PlanOf::kLibrary, m, n, k, 1));
+    const int64_t whole = L.splits > 1 ? L.whole_tiles : L.total;
+    const int64_t longest = whole > 0 ? k : plan.k_per_split;
+    if (!other && longest > (int64_t)pamk::kFoldChunks * pamk::kChunkK * plan.kgroups)
+        out->folds = (size_t)(whole + (L.total - whole) * L.splits) * plan.kgroups * plan.tile_m * plan.tile_n * sizeof(float);
+    return PAM_SUCCESS;
+}
+
 // The product under `plan` (unless it is the caller's, skinny and small products
 // take their own kernels); a split plan keeps its partial sums in `ext`,
 // which must hold the plan's workspace bytes.  Allocates nothing.
@@ -748,13 +769,37 @@ pam_status_t api_linear(int64_t m, int64_t n, int64_t k, const void *x, int64_t 
                         hipStream_t stream) {
     const float *a = static_cast<const float *>(x), *b = static_cast<const float *>(w);
     float *c = static_cast<float *>(epi.y);   // never written as such: outputs go by epi
-    const pam_status_t st = validate(PAM_OP_N, PAM_OP_T, m, n, k, a, ldx, 0, b, ldw, 0, c, epi.ldy, 0, 1);
+    pam_status_t st = validate(PAM_OP_N, PAM_OP_T, m, n, k, a, ldx, 0, b, ldw, 0, c, epi.ldy, 0, 1);
     if (st != PAM_SUCCESS || m == 0 || n == 0)
         return st;
+    const Plan plan = choose_plan(m, n, k, 1, k > 0 ? kAnyWorkspace : 0);
+    LinearSpace space;
+    st = linear_space(plan, m, n, k, &space);
+    if (st != PAM_SUCCESS)
+        return st;
     const Workspace ws{workspace, workspace_bytes};
-    return run_gemm(PAM_OP_N, PAM_OP_T, m, n, k, a, ldx, 0, b, ldw, 0, c, epi.ldy, 0, 1,
-                    choose_plan(m, n, k, 1, k > 0 ? kAnyWorkspace : 0), PlanOf::kLibrary, stream, round_drop, &ws, bf16,
-                    &epi);
+    st = check_workspace(&ws, space.partial + space.folds);
+    if (st != PAM_SUCCESS)
+        return st;
+    Epilogue e = epi;
+    e.folds = space.folds > 0 ? reinterpret_cast<float *>(static_cast<char *>(workspace) + space.partial) : nullptr;
+    return run_gemm(PAM_OP_N, PAM_OP_T, m, n, k, a, ldx, 0, b, ldw, 0, c, epi.ldy, 0, 1, plan, PlanOf::kLibrary, stream,
+                    round_drop, &ws, bf16, &e);
+}
+
+pam_status_t api_linear_workspace_size(int64_t m, int64_t n, int64_t k, size_t *bytes) {
+    *bytes = 0;
+    if (m < 0 || n < 0 || k < 0 || m > kMaxDim || n > kMaxDim || k > kMaxDim)
+        return fail(PAM_ERROR_INVALID_VALUE, "m, n and k must be in [0, 2^31)");
+    if (check_output_size(m, n, 1) != PAM_SUCCESS)
+        return PAM_ERROR_INVALID_VALUE;
+    if (m == 0 || n == 0 || k == 0)
+        return PAM_SUCCESS;
+    LinearSpace space;
+    const pam_status_t st = linear_space(choose_plan(m, n, k, 1, kAnyWorkspace), m, n, k, &space);
+    if (st == PAM_SUCCESS)
+        *bytes = space.partial + space.folds;
+    return st;
 }
 
 }  // namespace pamk

@@ -217,6 +217,20 @@ constexpr int dma_min_lds_words(int bm, int bn, int kw, int wps) {
                                                            : 0;
 }
 
+// The launch's parameters, read anew: what only the kernel's end needs would
+// otherwise be loaded at its start and spill across the K loop (67 scalar values
+// into vector lanes, 5% of a large layer's time).
+typedef const GemmParams __attribute__((address_space(4))) ParamsAgain;   // read by scalar loads
+__device__ __forceinline__ ParamsAgain *params_again() {
+    ParamsAgain *at = (ParamsAgain *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return at;
+}
+__device__ __forceinline__ Epilogue epilogue_of(ParamsAgain *p) {
+    return {p->epi.bias, p->epi.residual, p->epi.y, p->epi.z, p->epi.ldr, p->epi.ldy, p->epi.ldz, p->epi.activation,
+            p->epi.out_bf16, nullptr};
+}
+
 // WPS: waves per SIMD the kernel is compiled for.  At two (256 registers a
 // wave), and at three for a row-major A (168 registers, measured to fit), the
 // per-thread staging addresses are computed once, before the K loop;
@@ -473,11 +487,68 @@ pam_gemm_dma_kernel(GemmParams p) {
     constexpr int kInner = EDGE < 2 ? EDGE : 1;
     const int inner = EDGE < 2 || (ke - kb) % BK == 0 ? nchunks : max(nchunks - 2, 0);
     const int first = kinds != 0u ? 0 : inner;
+    if constexpr (EPI) {
+        // A linear layer's sums: the chain so far to the running sums in memory
+        // (of this thread, 16 bytes apart by thread) and from zero again, every
+        // kFoldChunks chunks but after the last ones.  The registers are the sums':
+        // no branch on what is kept already, four loads in flight, addresses not held
+        // across the loop (the empty asm).
+        const int every = p.epi.folds != nullptr ? kFoldChunks : nchunks;
+        auto kept = [&](int q) {   // four of 16 columns from q on
+            uint32_t place = (uint32_t)t * 16u;
+            asm volatile("" : "+v"(place)::"memory");
+            char *at = reinterpret_cast<char *>(params_again()->epi.folds) +
+                       ((int64_t)item * KW + __builtin_amdgcn_readfirstlane(grp)) * (256 * NTG);
+            return reinterpret_cast<float4 *>(at + q * 16 * NTG + place);
+        };
+        int c = 0;
+        while (true) {
+            const int stop = min(c + every, nchunks);
+            for (; c < (EDGE == 2 ? min(stop, first) : stop); ++c)
+                chunk(std::integral_constant<int, kInner>{}, c);
+            if constexpr (EDGE == 2) {
+                for (; c < stop; ++c)
+                    chunk(std::integral_constant<int, 2>{}, c);
+            }
+            if (c >= nchunks)
+                break;
+            const bool again = c > every;
+#pragma unroll
+            for (int q = 0; q < 16; q += 4) {
+                float4 *at = kept(q), x[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    x[u] = at[u * NTG];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    float *a = acc[(q + u) / 2] + u % 2 * 4;
+                    at[u * NTG] = make_float4(a[0] + (again ? x[u].x : 0.0f), a[1] + (again ? x[u].y : 0.0f),
+                                              a[2] + (again ? x[u].z : 0.0f), a[3] + (again ? x[u].w : 0.0f));
+                    a[0] = a[1] = a[2] = a[3] = 0.0f;
+                }
+            }
+        }
+        if (nchunks > every) {
+#pragma unroll
+            for (int q = 0; q < 16; q += 4) {
+                float4 *at = kept(q), x[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    x[u] = at[u * NTG];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    float *a = acc[(q + u) / 2] + u % 2 * 4;
+                    a[0] += x[u].x; a[1] += x[u].y; a[2] += x[u].z; a[3] += x[u].w;
+                }
+            }
+        }
+    } else {
     for (int c = 0; c < first; ++c)
         chunk(std::integral_constant<int, kInner>{}, c);
     if constexpr (EDGE == 2) {
         for (int c = first; c < nchunks; ++c)
             chunk(std::integral_constant<int, 2>{}, c);
+    }
     }
 
     // Epilogue: the output tile in C, or this K slice's partial tile (packed,
@@ -555,10 +626,13 @@ pam_gemm_dma_kernel(GemmParams p) {
             constexpr int kRows = BM / 8 * kPart;   // rows of the tile at once
             constexpr int kLd = BN + 16;            // lanes 16 bytes apart, rows half the banks
             static_assert(kRows * kLd <= kWords0 && NT % (BN / 4) == 0, "the epilogue's parts");
+            ParamsAgain *again = params_again();
+            const Epilogue e = epilogue_of(again);
+            const int rows = again->m, columns = again->n;
             float *sums = reinterpret_cast<float *>(smem);
-            const int col = n0 + tid % (BN / 4) * 4, have = p.n - col;
+            const int col = n0 + tid % (BN / 4) * 4, have = columns - col;
             float bias[4];
-            load_bias4(p.epi, col, have, bias);
+            load_bias4(e, col, have, bias);
 #pragma unroll 1
             for (int part = 0; part < 8 / kPart; ++part) {
                 __syncthreads();   // the LDS is free
@@ -574,18 +648,18 @@ pam_gemm_dma_kernel(GemmParams p) {
                     }
                 }
                 __syncthreads();
-                with_activation(p.epi.activation, [&](auto act) {
+                with_activation(e.activation, [&](auto act) {
 #pragma unroll 1
                     for (int r = tid / (BN / 4); r < kRows; r += NT / (BN / 4)) {
                         const int i = part * kPart + r % kPart;
                         const int64_t row = m0 + r / kPart * 4 + (i < 4 ? i : HM + i - 4);
-                        if (row >= p.m)
+                        if (row >= rows)
                             continue;
                         float res[4];
-                        load_residual4(p.epi, row, col, have, res);
+                        load_residual4(e, row, col, have, res);
                         const float4 x = *reinterpret_cast<const float4 *>(&sums[r * kLd + tid % (BN / 4) * 4]);
                         const float v[4] = {x.x, x.y, x.z, x.w};
-                        finish4<decltype(act)::value>(p.epi, row, col, have, v, bias, res);
+                        finish4<decltype(act)::value>(e, row, col, have, v, bias, res);
                     }
                 });
             }

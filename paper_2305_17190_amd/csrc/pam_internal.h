@@ -26,7 +26,14 @@ struct Epilogue {
     int64_t ldr, ldy, ldz;
     int32_t activation;     // pam_activation_t
     int32_t out_bf16;
+    // Running sums of the tiled kernel, kept here every kFoldChunks chunks: [work
+    // item][k-group][16-byte column][thread], or nullptr where no chain is longer.
+    float *folds;
 };
+// A sum's longest chain of roundings in a linear layer's tiles: so many chunks
+// of kChunkK terms.  A chain of L terms of either sign is off by about sqrt(L) / 3
+// units of 2^-24: 1.2e-6 of the result over K = 4096, 5.7e-7 in parts of 1024.
+constexpr int kFoldChunks = 64;
 
 // Arguments of one (batched, possibly split-K) PAM matrix product launch.
 //
@@ -66,11 +73,12 @@ pam_status_t api_fail_hip(hipError_t error, const char *what);
 pam_status_t api_check_device();
 
 // A linear layer's product (op N, op T) under the library's plan, its outputs
-// by epi; the workspace is pam_gemm_workspace_size's.  Sizes and leading
-// dimensions of x, w and y are validated here (pam_api.cpp).
+// by epi (whose folds are set here).  Sizes and leading dimensions of x, w and
+// y are validated here (pam_api.cpp).
 pam_status_t api_linear(int64_t m, int64_t n, int64_t k, const void *x, int64_t ldx, const void *w, int64_t ldw,
                         const Epilogue &epi, bool bf16, int round_drop, void *workspace, size_t workspace_bytes,
                         hipStream_t stream);
+pam_status_t api_linear_workspace_size(int64_t m, int64_t n, int64_t k, size_t *bytes);
 
 hipError_t launch_pam_mul(const float *a, const float *b, float *out, int64_t n, hipStream_t stream);
 

@@ -157,6 +157,12 @@ int64_t step_chunk(int64_t total) {
 
 extern "C" {
 
+pam_status_t pam_linear_workspace_size(int64_t m, int64_t n, int64_t k, size_t *bytes) {
+    if (bytes == nullptr)
+        return invalid("bytes is NULL");
+    return pamk::api_linear_workspace_size(m, n, k, bytes);
+}
+
 pam_status_t pam_linear(const pam_linear_t *args, hipStream_t stream) {
     if (args == nullptr)
         return invalid("args is NULL");

@@ -25,8 +25,8 @@ from . import PamError, _check, _launch, _require, _same_device, _torch, load
 __all__ = ["linear", "activation_grad", "grad_norm", "adamw_step", "STATE_BLOCK"]
 
 # Every symbol include/pam_training.h declares.
-EXPORTS = ("pam_linear", "pam_activation_grad_workspace_size", "pam_activation_grad", "pam_grad_norm_workspace_size",
-           "pam_grad_norm", "pam_adamw_step")
+EXPORTS = ("pam_linear_workspace_size", "pam_linear", "pam_activation_grad_workspace_size", "pam_activation_grad",
+           "pam_grad_norm_workspace_size", "pam_grad_norm", "pam_adamw_step")
 
 # pam_activation_t.
 ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
@@ -42,6 +42,7 @@ def _library() -> ctypes.CDLL:
     if _bound is None:
         lib = load()
         i32, i64, vp, psz = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.POINTER(ctypes.c_size_t)
+        lib.pam_linear_workspace_size.argtypes = [i64, i64, i64, psz]
         lib.pam_linear.argtypes = [ctypes.c_char_p, vp]
         lib.pam_activation_grad.argtypes = [ctypes.c_char_p, vp]
         lib.pam_activation_grad_workspace_size.argtypes = [i64, i64, psz]
@@ -138,7 +139,7 @@ def _linear_plan(x, w, bias, residual, activation, out_dtype, mantissa_bits):
             raise TypeError(f"residual must have the output's type {out_dtype}, got {residual.dtype}")
     _same_device(x, ("w", w), ("bias", bias), ("residual", residual))
     need = ctypes.c_size_t()
-    _check(load().pam_gemm_workspace_size(m, n, k, 1, ctypes.byref(need)))
+    _check(_library().pam_linear_workspace_size(m, n, k, ctypes.byref(need)))
     nbytes = int(need.value)
     tail = struct.pack("=qqqqqqqqqiiii", m, n, k, _ld(x), _ld(w), _ld(residual), max(n, 1), max(n, 1), nbytes,
                        int(x.dtype == torch.bfloat16), out, act, bits)

@@ -1,5 +1,5 @@
 """Linear layers with bias, activation and residual: the product is gemm's, sum
-for sum, and what is added follows the definition."""
+for sum where no sum is long, and what is added follows the definition."""
 import ctypes
 import struct
 
@@ -10,6 +10,7 @@ import paper_2305_17190_amd as pam
 import training_util as tu
 from attention_util import check
 from gpu_util import device, note, to_dev
+from oracle import pam_ref
 from oracle import training_ref as ref
 
 pytestmark = pytest.mark.gpu
@@ -85,6 +86,36 @@ def test_against_the_definition(m, k, n):
     check(y.cpu().numpy(), want, 1.13 * dz + tu.activation_error(zr, "gelu") + tu.U * np.abs(want), "y")
 
 
+# Whole tiles of every shape and slices whose K is taken in parts, K inside a part,
+# at its end and one past it.
+@pytest.mark.parametrize("m,k,n", [(1100, 3000, 1300), (4096, 1025, 1024), (2048, 2048, 2048), (2048, 8192, 2048),
+                                   (5000, 4097, 260), (700, 8191, 3000), (520, 40000, 140)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_long_sums(m, k, n, bf16):
+    import torch
+    plan, need = pam.plan(m, n, k), [ctypes.c_size_t() for _ in "ab"]
+    lib = pam.training._library()
+    assert lib.pam_linear_workspace_size(m, n, k, ctypes.byref(need[0])) == 0
+    assert lib.pam_gemm_workspace_size(m, n, k, 1, ctypes.byref(need[1])) == 0
+    folds = need[0].value > need[1].value + 255
+    note(f"linear {m}x{k}x{n} bf16 {bf16}, plan {plan}, in parts {folds}")
+    x, w, bias, res = inputs(m, k, n, bf16)
+    y, z = pam.linear(x, w, bias, "relu", res, save_z=True)
+    rows, cols = (np.unique(np.linspace(0, s - 1, 40).astype(int)) for s in (m, n))
+    want, size = pam_ref.pam_gemm_ref(x[rows].float().cpu().numpy(), w[cols].float().cpu().numpy(), False, True)
+    z0 = z[rows][:, cols].cpu().numpy()
+    whole = want + bias[cols].cpu().numpy().astype(np.float64)
+    part = 1024 if folds else k
+    check(z0, whole, (part + k / 1024 + 80) * tu.U * size + tu.U * np.abs(whole), "z")
+    assert bool((y == torch.relu(z) + res).all())
+    if folds:     # shorter chains, smaller errors
+        alone = pam.gemm(x, w, trans_b=True)[rows][:, cols].cpu().numpy()
+        off = [np.linalg.norm(t.astype(np.float64) - want) for t in (alone, pam.linear(x, w)[rows][:, cols].cpu().numpy())]
+        assert off[1] < off[0] or not k > 4000
+    again = pam.linear(x, w, bias, "relu", res)
+    assert same(again, y)
+
+
 def test_narrow_mantissas():
     import torch
     note("linear, 7 mantissa bits")
@@ -124,7 +155,7 @@ def test_c_call_in_place_with_wide_rows(m, k, n, out_bf16):
     y[:, :n] = res
     lib = pam.training._library()
     need = ctypes.c_size_t()
-    assert lib.pam_gemm_workspace_size(m, n, k, 1, ctypes.byref(need)) == 0
+    assert lib.pam_linear_workspace_size(m, n, k, ctypes.byref(need)) == 0
     ws = torch.empty(max(need.value, 1), dtype=torch.uint8, device=device())
     args = struct.pack("=7q9q4i", x.data_ptr(), w.data_ptr(), bias.data_ptr(), y.data_ptr(), y.data_ptr(), z.data_ptr(),
                        ws.data_ptr(), m, n, k, k, k, n + 5, n + 5, n + 3, need.value, 0, int(out_bf16), 3, 23)

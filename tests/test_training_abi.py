@@ -70,6 +70,24 @@ def test_linear_accepts(lib, change):
     assert linear(lib, **{**change, "m": 0}) == 0 and linear(lib, **{**change, "n": 0}) == 0
 
 
+def test_linear_workspace(lib):
+    """The plan's partial sums, and the tiles' running sums where K is taken in parts."""
+    need, plan = ctypes.c_size_t(), ctypes.c_size_t()
+    for m, k, n in ((1, 512, 2048), (8, 8192, 4096), (197, 64, 197), (2048, 512, 2048), (0, 4096, 4096), (4096, 0, 4096)):
+        assert lib.pam_linear_workspace_size(m, n, k, ctypes.byref(need)) == 0
+        assert lib.pam_gemm_workspace_size(m, n, k, 1, ctypes.byref(plan)) == 0
+        assert plan.value <= need.value <= plan.value + 255
+    assert lib.pam_linear_workspace_size(16384, 4096, 4096, ctypes.byref(need)) == 0
+    assert need.value >= 16384 * 4096 * 4
+    args = dict(m=16384, k=4096, n=4096, x=at(0), w=at(8), bias=0, residual=0, y=at(16), z=0, workspace=at(32), ldx=4096,
+                ldw=4096, ldy=4096)
+    assert linear(lib, workspace_bytes=need.value - 1, **args) == INVALID
+    assert linear(lib, workspace_bytes=need.value, **args) == LAUNCH
+    for bad in ((-1, 1, 1), (1, -1, 1), (1, 1, -1), (1 << 31, 1, 1), (1 << 30, 1 << 30, 1)):
+        assert lib.pam_linear_workspace_size(*bad, ctypes.byref(need)) == INVALID
+    assert lib.pam_linear_workspace_size(1, 1, 1, None) == INVALID
+
+
 def grad(lib, **change):
     f = dict(dy=at(0), z=at(1), dz=at(2), db=at(3), workspace=at(4), m=3000, n=200, lddy=200, ldz=200, lddz=200,
              workspace_bytes=64 * MB, type=0, z_type=0, activation=4, reserved=0)
