@@ -138,7 +138,8 @@ typedef struct {
  * norm = the square root of the sum of the squares of all gradients (the n
  * and g of `count` tensors; nothing else of them is looked at), one float32.
  * Summed in float64, in an order fixed by the sizes.
- *   workspace: pam_grad_norm_workspace_size bytes, 16-byte aligned; a call's own
+ *   workspace: pam_grad_norm_workspace_size bytes (at most 8 (2048 + count)),
+ *       16-byte aligned; a call's own
  */
 pam_status_t pam_grad_norm_workspace_size(const pam_step_tensor_t *tensors, int64_t count, size_t *bytes);
 pam_status_t pam_grad_norm(const pam_step_tensor_t *tensors, int64_t count, pam_type_t grad_type, float *norm,

@@ -240,7 +240,7 @@ constexpr size_t kAnyWorkspace = ~(size_t)0;
 // on short workgroups (measured: fewer, longer slices end later than the
 // model's imbalance term predicts).  A plan with split-K must beat the best
 // unsplit one by kSplitMargin.
-Plan choose_plan(int64_t m, int64_t n, int64_t k, int64_t batch, size_t max_ws_bytes) {
+Plan search_plan(int64_t m, int64_t n, int64_t k, int64_t batch, size_t max_ws_bytes) {
     double best_t[2] = {0.0, 0.0};
     Plan best[2] = {};
     bool have[2] = {false, false};
@@ -337,6 +337,25 @@ Plan choose_plan(int64_t m, int64_t n, int64_t k, int64_t batch, size_t max_ws_b
             return h;
     }
     return best[0];
+}
+
+// search_plan's plan: the search takes 0.3 to 3.5 us of host time, as long as a
+// small product's kernel, so each thread keeps the plans of its last sizes.
+Plan choose_plan(int64_t m, int64_t n, int64_t k, int64_t batch, size_t max_ws_bytes) {
+    struct Kept {
+        int64_t m = -1, n, k, batch;
+        size_t max_ws_bytes;
+        Plan plan;
+    };
+    constexpr uint64_t kPlaces = 64;
+    static thread_local Kept kept[kPlaces];
+    uint64_t h = 0;
+    for (const uint64_t x : {(uint64_t)m, (uint64_t)n, (uint64_t)k, (uint64_t)batch, (uint64_t)max_ws_bytes})
+        h = (h ^ x) * 0x9E3779B97F4A7C15u;
+    Kept &place = kept[h >> 58];
+    if (place.m != m || place.n != n || place.k != k || place.batch != batch || place.max_ws_bytes != max_ws_bytes)
+        place = {m, n, k, batch, max_ws_bytes, search_plan(m, n, k, batch, max_ws_bytes)};
+    return place.plan;
 }
 
 // Output tiles of the smallest tile shape over the whole batch, at most

@@ -18,6 +18,7 @@ bias, activation, residual and the optimizer are ordinary float32 arithmetic.
 from __future__ import annotations
 
 import ctypes
+import functools
 import struct
 
 from . import PamError, _check, _launch, _require, _same_device, _torch, load
@@ -33,6 +34,8 @@ ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 # Values of a tensor that share a scale in 8-bit states.
 STATE_BLOCK = 256
+# Partial sums of a norm, beside one a tensor.
+NORM_PARTIALS = 2048
 
 _bound = None
 
@@ -69,6 +72,12 @@ def _packer():
             raise PamError(f"_pack.so is missing: build it with `python -m paper_2305_17190_amd.build` ({e})") from e
         _pack_module = module
     return _pack_module
+
+
+@functools.lru_cache(maxsize=None)
+def _entry(name: str):
+    """The entry point `name`, for ``_launch``: takes integers and bytes."""
+    return functools.partial(_packer().call, ctypes.cast(getattr(_library(), name), ctypes.c_void_p).value)
 
 
 # Calls whose arguments' types, shapes, strides and devices have been checked
@@ -166,7 +175,7 @@ def linear(x, w, bias=None, activation=None, residual=None, save_z: bool = False
         raise TypeError("linear takes dense tensors")
     tail, nbytes, out, m, n = _known((0, packed[0], activation, out_dtype, mantissa_bits), _linear_plan, *args)
     y, z, keep, outs = module.matrices(x, nbytes, out, m, n, out if save_z else -1, m, n)
-    _launch(x, (_bound or _library()).pam_linear, packed[1] + outs + tail)
+    _launch(x, _entry("pam_linear"), packed[1] + outs + tail)
     del keep
     return (y, z) if save_z else y
 
@@ -214,7 +223,7 @@ def activation_grad(dy, z, activation, bias: bool = True, input_grad: bool = Tru
                                                   *args)
     dz, db, keep, outs = module.matrices(dy, nbytes, dz_type, m, n, db_type, -1, n)
     if bias or dz is not None:
-        _launch(dy, (_bound or _library()).pam_activation_grad, packed[1] + outs + tail)
+        _launch(dy, _entry("pam_activation_grad"), packed[1] + outs + tail)
     del keep
     return dy if activation is None and input_grad else dz, db
 
@@ -282,21 +291,17 @@ def grad_norm(grads):
     contiguous float32 or bfloat16 tensors), as a float32 tensor of no
     dimensions: ``adamw_step``'s ``norm``.  Summed in float64, in an order fixed
     by the sizes."""
-    torch = _torch()
     count, tensors, bf16, _, first = _step_tensors(None, grads, None, None, None, None, None)
     if count == 0:
         raise ValueError("grad_norm takes at least one gradient")
-    lib = _bound or _library()
-    need = ctypes.c_size_t()
-    _check(lib.pam_grad_norm_workspace_size(tensors, count, ctypes.byref(need)))
-    # The norm behind the partial sums.
-    keep = torch.empty(need.value // 4 + 1, dtype=torch.float32, device=first.device)
-    norm = torch.empty((), dtype=torch.float32, device=first.device)
-    _launch(first, lib.pam_grad_norm, tensors, count, bf16, norm.data_ptr(), keep.data_ptr(), need.value)
+    nbytes = 8 * (NORM_PARTIALS + count)             # at least what pam_grad_norm_workspace_size says
+    norm, _, keep, outs = _packer().matrices(first, nbytes, 0, -2, 1, -1, 0, 0)
+    _launch(first, _entry("pam_grad_norm"), tensors, count, bf16, *_norm_outs(outs), nbytes)
     del keep
     return norm
 
 
+_norm_outs = struct.Struct("=q8xq").unpack
 _step_args = struct.Struct("=qqddddddqIiii").pack
 
 
@@ -342,4 +347,4 @@ def adamw_step(params, grads, avgs, sqs, step, lr: float = 1e-3, betas=(0.9, 0.9
     if first is None:
         _check((_bound or _library()).pam_adamw_step(tensors, count, args, None))   # its refusals; launches nothing
         return
-    _launch(first, (_bound or _library()).pam_adamw_step, tensors, count, args)
+    _launch(first, _entry("pam_adamw_step"), tensors, count, args)
