@@ -5,12 +5,13 @@
 // What bounds it: reading the wide operand once.  The tiled kernel pads the
 // few rows to 64 and gives each workgroup a few chunks between barriers.
 // Measured against it (one call after the other, other weights each time): 8
-// x 4096 x 4096 20.6 us (52.5; its 67 MB take 14 us at a copy's rate), 1 x 4096
-// x 4096 18.8 us (53.0), 16 x 4096 x 4096 25.9 us (53.9), 32 x 4096 x 4096
-// 47.9 us (54.1; two passes of 16 rows), 8 x 2048 x 512 4.9 us (27.7), 32 x 768 x
-// 192 6.0 us (20.7); bfloat16, 4096 x 4096 weights: 1 row 11.0 us (61.4), 8 rows
-// 14.9 us (61.7), 16 rows 22.5 us (62.1), 32 rows 43.6 us (62.1).  Where it is
-// taken: skinny_product in pam_api.cpp.
+// x 4096 x 4096 20.3 us (52.5; its 67 MB take 14 us at a copy's rate), 1 x 4096
+// x 4096 18.6 us (53.0), 16 x 4096 x 4096 24.2 us (53.9), 32 x 4096 x 4096
+// 44.4 us (54.1; two passes of 16 rows), 8 x 2048 x 512 4.9 us (27.7), 32 x 768 x
+// 192 6.0 us (20.7); bfloat16, 4096 x 4096 weights: 1 row 11.4 us (61.4), 8 rows
+// 13.7 us (61.7), 16 rows 20.8 us (62.1), 32 rows 39.7 us (62.1).  Where it is
+// taken: skinny_product in pam_api.cpp.  Two and four chunks in flight in place
+// of one are no faster (8 rows 21.7 and, bfloat16, 16.6 us).
 //
 // No wave waits for another until the end: a lane holds four consecutive k of
 // kJ rows of the wide operand, loaded straight into registers one chunk ahead
@@ -19,14 +20,14 @@
 // chunks; the skinny operand's chunk comes from LDS, written by the wave
 // itself.  The waves of a workgroup take parts of K (long K) or further wide rows.
 //
-// Arithmetic: the SCALED form with the product and sum in one fma (S2 of
-// pam_gemm_dma.hip): t = (1 + M_x) + w' is the encoding of PAM(1 + M_x, w),
-// acc = fma(t, +-2^E_x, acc); a zero x gives the factor 0, a zero w a t that
-// reads as 0.  It is exact while every nonzero operand has exponent field in
-// [64, 190].  A wave's chunk holding a tiny normal (field below 64) rounds each
-// product on its own (S3 there); one holding |x| >= 2^64, inf or NaN takes the
-// complete definition (as tiny normals did: with 0.1% of them among the weights
-// 32 x 4096 x 4096 took 491 us, now 58 us; on clean operands 47 us).  bfloat16
+// Arithmetic, by a wave's chunk, as in pam_gemm_dma.hip.  S1, acc += x + w - bias
+// on the encodings, where all exponent fields are in [64, 190].  S2 where there are
+// zeros: t = M_x + w is the encoding of PAM(1 + M_x, w), acc = fma(t, +-2^E_x, acc);
+// a zero x gives the factor 0, a zero w a t that reads as 0.  (S2 alone, with a
+// range of both operands' elements: 8 rows in bfloat16 15.2 us.)  A chunk holding
+// a tiny normal (field below 64) rounds each product on its own (S3); one holding
+// |x| >= 2^64, inf or NaN takes the complete definition (as tiny normals did: with
+// 0.1% of them among the weights 32 x 4096 x 4096 took 491 us, now 58 us).  bfloat16
 // operands widen to the same encodings, so their product equals the float32 one
 // bit for bit.
 
@@ -108,23 +109,27 @@ __device__ __forceinline__ void widen4(const uint32_t (&w)[2], uint32_t (&e)[4])
 // the largest, both times 2^63.
 struct Range {
     uint32_t least = 0xFFFFFFFFu, most = 0u;
+    uint32_t none = 0xFFFFFFFFu;   // 0 where a magnitude is zero or denormal
     __device__ __forceinline__ void add(uint32_t u) {
         uint32_t f;
         asm("v_mul_f32 %0, |%1|, %2" : "=v"(f) : "v"(u), "v"(0x5F000000u));   // 2^63
         least = min(least, f - 1u);
+        none = min(none, f);
         most = max(most, f & kMag);
     }
     // Some nonzero magnitude is below 2^-63; some is at or above 2^64 or not
     // finite (times 2^63 one of 2^65 or more is inf).
     __device__ __forceinline__ bool tiny() const { return least < kBias - 1u; }
+    __device__ __forceinline__ bool far() const { return most >= 0x7E800000u; }   // at or above 2^63
     __device__ __forceinline__ bool wild() const { return most >= 0x7F000000u; }
 };
 
 template <int S, bool EPI, typename T>
 __global__ void __launch_bounds__(64 * kWaves) pam_skinny_kernel(SkinnyParams p) {
-    // A wave's skinny chunk: 1 + M_x and +-2^E_x, [plane][row][k].  After the
-    // K loop the same bytes hold the waves' partial sums [wave][row][wide row].
-    constexpr int kChunkWords = 2 * S * kStep;
+    // A wave's skinny chunk: x's encoding less one bias, M_x and +-2^E_x,
+    // [plane][row][k].  After the K loop the same bytes hold the waves' partial
+    // sums [wave][row][wide row].
+    constexpr int kChunkWords = 3 * S * kStep;
     static_assert(kChunkWords >= S * kWaveRows, "the partial sums fit the chunk buffers");
     __shared__ __attribute__((aligned(16))) uint32_t smem[kWaves * kChunkWords];
 
@@ -155,6 +160,16 @@ __global__ void __launch_bounds__(64 * kWaves) pam_skinny_kernel(SkinnyParams p)
 #pragma unroll
     for (int i = 0; i < XQ; ++i)
         xrow[i] = x + (int64_t)min(s0 + dr + 4 * i, p.s - 1) * p.ldx;
+
+    // A linear layer's bias and residual ahead of the K loop: their latency would
+    // come after it.
+    float bias[kJ], res[kJ];
+    if constexpr (EPI) {
+        if (p.cd == 1 && kw == 0 && kq < S && s0 + kq < p.s) {
+            load_bias4(p.epi, d0, p.d - d0, bias);
+            load_residual4(p.epi, s0 + kq, d0, p.d - d0, res);
+        }
+    }
 
     float acc[S][kJ];
 #pragma unroll
@@ -203,14 +218,13 @@ __global__ void __launch_bounds__(64 * kWaves) pam_skinny_kernel(SkinnyParams p)
         const int kend = n - kf > kFoldChunks * step ? kf + kFoldChunks * step : n;
 #pragma unroll 1
         for (int k0 = kf; k0 < kend; k0 += step) {
-            uint32_t wn[kJ][4], xn[XQ][4], wc[kJ][4];
+            uint32_t wn[kJ][4], xn[XQ][4];
 #pragma unroll
             for (int j = 0; j < kJ; ++j)
                 widen4(wr[j], wn[j]);
 #pragma unroll
             for (int i = 0; i < XQ; ++i)
                 widen4(xr[i], xn[i]);
-            Range range;
             if (p.round_drop != 0) {
 #pragma unroll
                 for (int j = 0; j < kJ; ++j)
@@ -223,74 +237,103 @@ __global__ void __launch_bounds__(64 * kWaves) pam_skinny_kernel(SkinnyParams p)
                     for (int c = 0; c < 4; ++c)
                         xn[i][c] = round_bits(xn[i][c], p.round_drop);
             }
+            // The wide operand's elements have exponent fields in [64, 191] where bit 30
+            // is set after 2^29 is added, two operations instead of the seven of a range
+            // and a flush; with the skinny one's in [64, 189] no sum leaves the normal
+            // range.  (8 x 4096 x 4096, bfloat16: 15.2 us with ranges of both.)
+            uint32_t all = 0xFFFFFFFFu;
 #pragma unroll
             for (int j = 0; j < kJ; ++j)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    range.add(wn[j][c]);
-                    // A denormal to its signed zero, then less one bias.
-                    asm("v_mul_f32 %0, 1.0, %1" : "=v"(wc[j][c]) : "v"(wn[j][c]));
-                    wc[j][c] -= kBias;
-                }
+                for (int c = 0; c < 4; ++c)
+                    all &= wn[j][c] + 0x20000000u;
+            Range range;
 #pragma unroll
             for (int i = 0; i < XQ; ++i) {
-                uint4 am, m;
-                am.x = (xn[i][0] & kMant) | kBias; m.x = xn[i][0] & kSignExp;
-                am.y = (xn[i][1] & kMant) | kBias; m.y = xn[i][1] & kSignExp;
-                am.z = (xn[i][2] & kMant) | kBias; m.z = xn[i][2] & kSignExp;
-                am.w = (xn[i][3] & kMant) | kBias; m.w = xn[i][3] & kSignExp;
+                uint4 whole, mant, power;
+                whole.x = xn[i][0] - kBias; mant.x = xn[i][0] & kMant; power.x = xn[i][0] & kSignExp;
+                whole.y = xn[i][1] - kBias; mant.y = xn[i][1] & kMant; power.y = xn[i][1] & kSignExp;
+                whole.z = xn[i][2] - kBias; mant.z = xn[i][2] & kMant; power.z = xn[i][2] & kSignExp;
+                whole.w = xn[i][3] - kBias; mant.w = xn[i][3] & kMant; power.w = xn[i][3] & kSignExp;
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
                     range.add(xn[i][c]);
                 const int row = dr + 4 * i;
                 if (S % 4 == 0 || row < S) {
-                    *reinterpret_cast<uint4 *>(mine + row * kStep + kq * 4) = am;
-                    *reinterpret_cast<uint4 *>(mine + (S + row) * kStep + kq * 4) = m;
+                    *reinterpret_cast<uint4 *>(mine + row * kStep + kq * 4) = whole;
+                    *reinterpret_cast<uint4 *>(mine + (S + row) * kStep + kq * 4) = mant;
+                    *reinterpret_cast<uint4 *>(mine + (2 * S + row) * kStep + kq * 4) = power;
                 }
             }
             if (k0 + step < n)
                 fetch(k0 + step);
-            const bool wild = __builtin_amdgcn_ballot_w64(range.wild()) != 0u;
-            const bool tiny = __builtin_amdgcn_ballot_w64(range.tiny()) != 0u;
+            const bool plain = __builtin_amdgcn_ballot_w64((all & 0x40000000u) == 0u || range.tiny() || range.far()) == 0u;
+            const bool zero = __builtin_amdgcn_ballot_w64(range.none == 0u) != 0u;
             // The wave's own writes, read by its other lanes: LDS operations of a
             // wave complete in order, and the compiler keeps them in order here.
             asm volatile("" ::: "memory");
-            auto terms = [&](auto own) {
-                constexpr bool kOwn = decltype(own)::value;   // each product rounded on its own
+            auto plane = [&](int at, int i, uint32_t (&v)[4]) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(mine + (at * S + i) * kStep + kq * 4);
+                v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+            };
+            // Form 1: the sum of the encodings.  2: product and sum in one.  3: the
+            // product rounded on its own.
+            auto terms = [&](auto form) {
+                constexpr int F = decltype(form)::value;
 #pragma unroll
                 for (int i = 0; i < S; ++i) {
-                    const uint4 am = *reinterpret_cast<const uint4 *>(mine + i * kStep + kq * 4);
-                    const uint4 m = *reinterpret_cast<const uint4 *>(mine + (S + i) * kStep + kq * 4);
-                    const uint32_t a4[4] = {am.x, am.y, am.z, am.w}, m4[4] = {m.x, m.y, m.z, m.w};
+                    uint32_t a4[4], m4[4];
+                    plane(F == 1 ? 0 : 1, i, a4);
+                    if constexpr (F != 1)
+                        plane(2, i, m4);
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
                         for (int j = 0; j < kJ; ++j) {
-                            if constexpr (kOwn) {
-                                float t;   // in asm: the compiler would fuse the product and the sum
-                                asm("v_mul_f32 %0, %1, %2" : "=v"(t) : "v"(a4[c] + wc[j][c]), "v"(m4[c]));
-                                acc[i][j] += t;
-                            } else {
-                                acc[i][j] = __builtin_fmaf(__uint_as_float(a4[c] + wc[j][c]), __uint_as_float(m4[c]),
+                            if constexpr (F == 1) {
+                                acc[i][j] += __uint_as_float(a4[c] + wn[j][c]);
+                            } else if constexpr (F == 2) {
+                                acc[i][j] = __builtin_fmaf(__uint_as_float(a4[c] + wn[j][c]), __uint_as_float(m4[c]),
                                                            acc[i][j]);
+                            } else {
+                                float t;   // in asm: the compiler would fuse the product and the sum
+                                asm("v_mul_f32 %0, %1, %2" : "=v"(t) : "v"(a4[c] + wn[j][c]), "v"(m4[c]));
+                                acc[i][j] += t;
                             }
                         }
                 }
             };
-            if (!wild && !tiny) {
-                terms(std::false_type{});
-            } else if (!wild) {
-                terms(std::true_type{});
+            if (plain && !zero) {
+                terms(std::integral_constant<int, 1>{});
+            } else if (plain) {
+                terms(std::integral_constant<int, 2>{});
             } else {
+                // Zeros, tiny normals or wild values among the wide operand's, or
+                // those of the skinny one's: denormals to signed zeros, then by range.
 #pragma unroll
-                for (int i = 0; i < S; ++i) {
-#pragma unroll 1
+                for (int j = 0; j < kJ; ++j)
+#pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const uint32_t xe = (mine[i * kStep + kq * 4 + c] & kMant) | mine[(S + i) * kStep + kq * 4 + c];
+                        range.add(wn[j][c]);
+                        asm("v_mul_f32 %0, 1.0, %0" : "+v"(wn[j][c]));
+                    }
+                const bool wild = __builtin_amdgcn_ballot_w64(range.wild()) != 0u;
+                const bool tiny = __builtin_amdgcn_ballot_w64(range.tiny()) != 0u;
+                if (!wild && !tiny) {
+                    terms(std::integral_constant<int, 2>{});
+                } else if (!wild) {
+                    terms(std::integral_constant<int, 3>{});
+                } else {
 #pragma unroll
-                        for (int j = 0; j < kJ; ++j) {
-                            const uint32_t we = c == 0 ? wc[j][0] : c == 1 ? wc[j][1] : c == 2 ? wc[j][2] : wc[j][3];
-                            acc[i][j] += __uint_as_float(pam_full(xe, we + kBias));
+                    for (int i = 0; i < S; ++i) {
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            const uint32_t xe = mine[(S + i) * kStep + kq * 4 + c] | mine[(2 * S + i) * kStep + kq * 4 + c];
+#pragma unroll
+                            for (int j = 0; j < kJ; ++j) {
+                                const uint32_t we = c == 0 ? wn[j][0] : c == 1 ? wn[j][1] : c == 2 ? wn[j][2] : wn[j][3];
+                                acc[i][j] += __uint_as_float(pam_full(xe, we));
+                            }
                         }
                     }
                 }
@@ -320,7 +363,9 @@ __global__ void __launch_bounds__(64 * kWaves) pam_skinny_kernel(SkinnyParams p)
     if (kq < S && s0 + kq < p.s) {
         if constexpr (EPI) {
             if (p.cd == 1) {   // the few rows are x's
-                finish4(p.epi, s0 + kq, d0, p.d - d0, mineacc);
+                with_activation(p.epi.activation, [&](auto act) {
+                    finish4<decltype(act)::value>(p.epi, s0 + kq, d0, p.d - d0, mineacc, bias, res);
+                });
             } else {
 #pragma unroll
                 for (int j = 0; j < kJ; ++j)

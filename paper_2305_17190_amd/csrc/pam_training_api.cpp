@@ -84,10 +84,14 @@ pam_status_t check_workspace(const void *workspace, int64_t bytes, size_t need) 
 // The activations' gradient
 // ---------------------------------------------------------------------------
 
-// How the rows are cut: column groups of lanes * V columns, and bands of rows
-// for about kGradGroups workgroups with at least kGradRows rows a thread.
+// How the rows are cut.  Few rows: one band, whose sums need no second launch (2.5
+// us), with as few lanes a row, from kGradLanes on, that a thread has at most
+// kGradFew rows.  Otherwise 64 lanes a row (or the row's) and bands for about
+// kGradGroups workgroups with at least kGradRows rows a thread.
 constexpr int64_t kGradGroups = 1024;
 constexpr int64_t kGradRows = 4;
+constexpr int64_t kGradFew = 16;
+constexpr int kGradLanes = 8;
 
 struct GradCut {
     int lanes;
@@ -95,17 +99,19 @@ struct GradCut {
 };
 
 GradCut grad_cut(int64_t m, int64_t n, int values) {
-    GradCut c{};
-    c.lanes = 1;
-    while (c.lanes < 64 && (int64_t)c.lanes * values < n)
-        c.lanes *= 2;
-    const int64_t at_once = pamk::kGradThreads / c.lanes;
-    const int64_t groups = ceil_div(n, (int64_t)c.lanes * values);
-    const int64_t most = std::max<int64_t>(1, ceil_div(kGradGroups, groups));
-    const int64_t bands = std::max<int64_t>(1, std::min(most, m / (at_once * kGradRows)));
-    c.band = ceil_div(ceil_div(m, bands), at_once) * at_once;
-    c.bands = ceil_div(m, c.band);
-    return c;
+    int most = 1;
+    while (most < 64 && (int64_t)most * values < n)
+        most *= 2;
+    for (int lanes = most; lanes >= std::min(most, kGradLanes); lanes /= 2) {
+        const int64_t at_once = pamk::kGradThreads / lanes;
+        if (m <= at_once * kGradFew)
+            return {lanes, ceil_div(m, at_once) * at_once, 1};
+    }
+    const int64_t at_once = pamk::kGradThreads / most;
+    const int64_t groups = ceil_div(n, (int64_t)most * values);
+    const int64_t bands = std::max<int64_t>(1, std::min(ceil_div(kGradGroups, groups), m / (at_once * kGradRows)));
+    const int64_t band = ceil_div(ceil_div(m, bands), at_once) * at_once;
+    return {most, band, ceil_div(m, band)};
 }
 
 // ---------------------------------------------------------------------------
