@@ -13,11 +13,13 @@
 namespace pamk {
 namespace {
 
-// V neighbouring elements, at any address, widened; `have` of them exist.
-template <int V, typename T> __device__ __forceinline__ void load_wide(const T *p, int have, float (&x)[V]) {
+// V neighbouring elements, at any address, widened; `have` of them exist.  NT:
+// with the non-temporal hint.
+template <int V, bool NT = false, typename T> __device__ __forceinline__ void load_wide(const T *p, int have, float (&x)[V]) {
     typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
     if (have >= V) {
-        const vec v = *reinterpret_cast<const vec *>(p);
+        const vec *at = reinterpret_cast<const vec *>(p);
+        const vec v = NT ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             if constexpr (sizeof(T) == 2)
@@ -35,7 +37,7 @@ template <int V, typename T> __device__ __forceinline__ void load_wide(const T *
         }
     }
 }
-template <int V, typename T> __device__ __forceinline__ void store_wide(T *p, int have, const float (&x)[V]) {
+template <int V, bool NT = false, typename T> __device__ __forceinline__ void store_wide(T *p, int have, const float (&x)[V]) {
     typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
     vec v;
 #pragma unroll
@@ -46,7 +48,11 @@ template <int V, typename T> __device__ __forceinline__ void store_wide(T *p, in
             v[i] = x[i];
     }
     if (have >= V) {
-        *reinterpret_cast<vec *>(p) = v;
+        vec *at = reinterpret_cast<vec *>(p);
+        if constexpr (NT)
+            __builtin_nontemporal_store(v, at);
+        else
+            *at = v;
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
@@ -62,7 +68,7 @@ template <int V, typename T> __device__ __forceinline__ void store_wide(T *p, in
 // dz = dy f'(z) and the sums of its columns.  A thread keeps the sums of its V
 // columns over the rows it takes; the workgroup's rows are added in a tree, in
 // LDS, and the bands' sums by sum_bands_kernel: an order fixed by the sizes.
-template <typename T, typename Z> __global__ void __launch_bounds__(kGradThreads) activation_grad_kernel(GradParams p) {
+template <typename T, typename Z, bool NT> __global__ void __launch_bounds__(kGradThreads) activation_grad_kernel(GradParams p) {
     constexpr int V = 16 / sizeof(T);
     __shared__ float red[kGradThreads * V];
     const int lanes = p.lanes, at_once = kGradThreads / lanes;
@@ -85,9 +91,9 @@ template <typename T, typename Z> __global__ void __launch_bounds__(kGradThreads
 #pragma unroll 4
             for (int64_t r = (int64_t)band * p.band + ty; r < end; r += at_once) {
                 float d[V], x[V];
-                load_wide<V>(dy + r * p.lddy, have, d);
+                load_wide<V, NT>(dy + r * p.lddy, have, d);
                 if constexpr (ACT != PAM_ACT_NONE) {
-                    load_wide<V>(z + r * p.ldz, have, x);
+                    load_wide<V, NT>(z + r * p.ldz, have, x);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         if constexpr (ACT == PAM_ACT_RELU)
@@ -156,7 +162,7 @@ __device__ __forceinline__ int tensor_of(const uint32_t *first, int count, uint3
     return __builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) - 1;
 }
 
-template <typename T> __global__ void __launch_bounds__(kStepThreads) grad_squares_kernel(NormParams p) {
+template <typename T, bool NT> __global__ void __launch_bounds__(kStepThreads) grad_squares_kernel(NormParams p) {
     constexpr int V = 16 / sizeof(T);
     __shared__ double red[kStepThreads / 64];
     const int j = tensor_of(p.first, p.count, blockIdx.x);
@@ -168,7 +174,7 @@ template <typename T> __global__ void __launch_bounds__(kStepThreads) grad_squar
 #pragma unroll 4
     for (int64_t i = begin + threadIdx.x * V; i < end; i += kStepThreads * V) {
         float x[V];
-        load_wide<V>(g + i, (int)min(end - i, (int64_t)V), x);
+        load_wide<V, NT>(g + i, (int)min(end - i, (int64_t)V), x);
 #pragma unroll
         for (int e = 0; e < V; ++e)
             sum = __builtin_fma((double)x[e], (double)x[e], sum);
@@ -234,7 +240,7 @@ __device__ __forceinline__ float moved(const StepParams &p, const Rates &r, floa
     return __builtin_fmaf(-r.step_size, avg * __builtin_amdgcn_rcpf(by), x * p.keep);
 }
 
-template <typename G> __global__ void __launch_bounds__(kStepThreads) adamw_kernel(StepParams p) {
+template <typename G, bool NT> __global__ void __launch_bounds__(kStepThreads) adamw_kernel(StepParams p) {
     const int j = tensor_of(p.first, p.count, blockIdx.x);
     const pam_step_tensor_t &t = p.tensor[j];
     const Rates rates = rates_of(p, j);
@@ -246,10 +252,10 @@ template <typename G> __global__ void __launch_bounds__(kStepThreads) adamw_kern
     for (int64_t i = begin + threadIdx.x * 4; i < end; i += kStepThreads * 4) {
         const int have = (int)min(end - i, (int64_t)4);
         float x[4], d[4], m[4], v[4];
-        load_wide<4>(g + i, have, d);
-        load_wide<4>(t.p + i, have, x);
-        load_wide<4>(avg + i, have, m);
-        load_wide<4>(sq + i, have, v);
+        load_wide<4, NT>(g + i, have, d);
+        load_wide<4, NT>(t.p + i, have, x);
+        load_wide<4, NT>(avg + i, have, m);
+        load_wide<4, NT>(sq + i, have, v);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             d[e] *= rates.clip;
@@ -257,11 +263,11 @@ template <typename G> __global__ void __launch_bounds__(kStepThreads) adamw_kern
             v[e] = __builtin_fmaf(v[e], p.beta2, d[e] * p.rest2 * d[e]);
             x[e] = moved(p, rates, x[e], m[e], v[e]);
         }
-        store_wide<4>(avg + i, have, m);
-        store_wide<4>(sq + i, have, v);
-        store_wide<4>(t.p + i, have, x);
+        store_wide<4, NT>(avg + i, have, m);
+        store_wide<4, NT>(sq + i, have, v);
+        store_wide<4, NT>(t.p + i, have, x);
         if (t.copy != nullptr)
-            store_wide<4>(t.copy + i, have, x);
+            store_wide<4, NT>(t.copy + i, have, x);
     }
 }
 
@@ -273,35 +279,67 @@ __device__ __forceinline__ float held(uint32_t code, uint32_t low, float scale) 
     return (code != 0u ? __uint_as_float((code + low) << 20) : 0.0f) * scale;
 }
 
-// The code of a magnitude as a part of its block's scale (NaN: the largest).
-__device__ __forceinline__ uint32_t coded(float x, float scale, uint32_t random, uint32_t low, uint32_t most) {
-    const float part = x / (scale > 0.0f ? scale : 1.0f);
+// Division by a block's scale, correctly rounded: with s = scale / 2^e in [1, 4), x'
+// = x / 2^e and r the rounded 1 / s, q = x' r is within a unit in the last place of
+// x' / s, and q + (x' - q s) r, the residual exact in an fma, is x' / s rounded
+// (Markstein).  Three operations a value in place of a division's twelve or so.
+// What 2^-e flushes is below 2^-126 of the scale, and coded as 0 anyway.
+struct Divisor {
+    float shift, s, r;
+    __device__ __forceinline__ explicit Divisor(float scale) {
+        // The shift's own field is 254 less the scale's, at least 1; without a scale
+        // there is nothing to divide, and by inf every finite value gives 0.
+        const int e = (int)(__float_as_uint(scale) >> 23);   // no sign
+        shift = e == 255 ? 0.0f : e == 0 ? 1.0f : __uint_as_float((uint32_t)max(254 - e, 1) << 23);
+        s = e == 255 || e == 0 ? 1.0f : scale * shift;
+        r = 1.0f / s;
+    }
+    __device__ __forceinline__ float operator()(float x) const {
+        const float a = x * shift, q = a * r;
+        return __builtin_fmaf(__builtin_fmaf(-q, s, a), r, q);
+    }
+};
+
+// The code of a part of its block's scale (NaN: the largest).
+__device__ __forceinline__ uint32_t coded(float part, uint32_t random, uint32_t low, uint32_t most) {
     const uint32_t c = (__float_as_uint(part) + random) >> 20;
     return c <= low ? 0u : min(c - low, most);
 }
 
-// The largest of the wave's values, by their encodings (no sign): NaN above all.
+// The largest of the wave's magnitudes, by their encodings: NaN above all.
 __device__ __forceinline__ float largest(const float (&x)[4]) {
-    uint32_t u = max(max(__float_as_uint(x[0]), __float_as_uint(x[1])), max(__float_as_uint(x[2]), __float_as_uint(x[3])));
-    for (int d = 32; d > 0; d /= 2)
-        u = max(u, (uint32_t)__shfl_xor((int)u, d));
-    return __uint_as_float(u);
+    int m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        m[i] = __float_as_int(__builtin_fabsf(x[i]));
+    int u = max(max(m[0], m[1]), max(m[2], m[3]));
+    // Along the rows of 16 lanes, then from row to row: lane 63 has all.
+    u = max(u, __builtin_amdgcn_update_dpp(0, u, 0x111, 0xF, 0xF, true));
+    u = max(u, __builtin_amdgcn_update_dpp(0, u, 0x112, 0xF, 0xF, true));
+    u = max(u, __builtin_amdgcn_update_dpp(0, u, 0x114, 0xF, 0xF, true));
+    u = max(u, __builtin_amdgcn_update_dpp(0, u, 0x118, 0xF, 0xF, true));
+    u = max(u, __builtin_amdgcn_update_dpp(0, u, 0x142, 0xA, 0xF, true));
+    u = max(u, __builtin_amdgcn_update_dpp(0, u, 0x143, 0xC, 0xF, true));
+    return __int_as_float(__builtin_amdgcn_readlane(u, 63));
 }
 
 // Four codes from c, at any address; `have` of them exist.
-__device__ __forceinline__ uint32_t load_codes(const uint8_t *c, int have) {
+template <bool NT> __device__ __forceinline__ uint32_t load_codes(const uint8_t *c, int have) {
     typedef uint32_t word __attribute__((aligned(1)));
     if (have >= 4)
-        return *reinterpret_cast<const word *>(c);
+        return NT ? __builtin_nontemporal_load(reinterpret_cast<const word *>(c)) : *reinterpret_cast<const word *>(c);
     uint32_t w = 0u;
     for (int i = 0; i < have; ++i)
         w |= (uint32_t)c[i] << (8 * i);
     return w;
 }
-__device__ __forceinline__ void store_codes(uint8_t *c, int have, uint32_t w) {
+template <bool NT> __device__ __forceinline__ void store_codes(uint8_t *c, int have, uint32_t w) {
     typedef uint32_t word __attribute__((aligned(1)));
     if (have >= 4) {
-        *reinterpret_cast<word *>(c) = w;
+        if constexpr (NT)
+            __builtin_nontemporal_store(w, reinterpret_cast<word *>(c));
+        else
+            *reinterpret_cast<word *>(c) = w;
     } else {
         for (int i = 0; i < have; ++i)
             c[i] = (uint8_t)(w >> (8 * i));
@@ -310,7 +348,7 @@ __device__ __forceinline__ void store_codes(uint8_t *c, int have, uint32_t w) {
 
 // A wave holds a block of 256 values, four a lane: its scales are maxima over
 // the wave, so that the states are read and written once.
-template <typename G> __global__ void __launch_bounds__(kStepThreads) adamw8_kernel(StepParams p) {
+template <typename G, bool NT> __global__ void __launch_bounds__(kStepThreads) adamw8_kernel(StepParams p) {
     const int j = tensor_of(p.first, p.count, blockIdx.x);
     const pam_step_tensor_t &t = p.tensor[j];
     const Rates rates = rates_of(p, j);
@@ -324,9 +362,9 @@ template <typename G> __global__ void __launch_bounds__(kStepThreads) adamw8_ker
         const int64_t i = b + lane * 4, block = b / PAM_STATE_BLOCK;
         const int have = (int)max(min(end - i, (int64_t)4), (int64_t)0);
         float x[4], d[4], m[4], v[4], size[4];
-        load_wide<4>(g + i, have, d);
-        load_wide<4>(t.p + i, have, x);
-        const uint32_t mc = load_codes(avg + i, have), vc = load_codes(sq + i, have);
+        load_wide<4, NT>(g + i, have, d);
+        load_wide<4, NT>(t.p + i, have, x);
+        const uint32_t mc = load_codes<NT>(avg + i, have), vc = load_codes<NT>(sq + i, have);
         const float ms = t.avg_scale[block], vs = t.sq_scale[block];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -344,21 +382,22 @@ template <typename G> __global__ void __launch_bounds__(kStepThreads) adamw8_ker
             size[e] = __builtin_fabsf(m[e]);
         }
         const float ms1 = largest(size), vs1 = largest(v);
+        const Divisor by_m(ms1), by_v(vs1);
         uint32_t mw = 0u, vw = 0u;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const uint32_t h = mix((uint32_t)(i + e) + rates.key);
-            const uint32_t cm = coded(size[e], ms1, ((h & 0xFFFFu) << 4) + 8u, kAvgLow, kAvgMost);
-            const uint32_t cv = coded(v[e], vs1, ((h >> 16) << 4) + 8u, kSqLow, kSqMost);
+            const uint32_t cm = coded(by_m(size[e]), ((h & 0xFFFFu) << 4) + 8u, kAvgLow, kAvgMost);
+            const uint32_t cv = coded(by_v(v[e]), ((h >> 16) << 4) + 8u, kSqLow, kSqMost);
             mw |= (cm | (cm != 0u && m[e] < 0.0f ? 128u : 0u)) << (8 * e);
             vw |= (v[e] != 0.0f ? max(cv, 1u) : 0u) << (8 * e);
             x[e] = moved(p, rates, x[e], m[e], v[e]);
         }
-        store_codes(avg + i, have, mw);
-        store_codes(sq + i, have, vw);
-        store_wide<4>(t.p + i, have, x);
+        store_codes<NT>(avg + i, have, mw);
+        store_codes<NT>(sq + i, have, vw);
+        store_wide<4, NT>(t.p + i, have, x);
         if (t.copy != nullptr)
-            store_wide<4>(t.copy + i, have, x);
+            store_wide<4, NT>(t.copy + i, have, x);
         if (lane == 0) {
             t.avg_scale[block] = ms1;
             t.sq_scale[block] = vs1;
@@ -374,14 +413,23 @@ hipError_t launch_activation_grad(bool bf16, bool z_bf16, const GradParams &p, h
     if (groups <= 0 || groups > kMostStepGroups)
         return hipErrorInvalidValue;
     const dim3 grid((unsigned)groups), block(kGradThreads);
-    if (bf16 && z_bf16)
-        hipLaunchKernelGGL((activation_grad_kernel<uint16_t, uint16_t>), grid, block, 0, stream, p);
-    else if (bf16)
-        hipLaunchKernelGGL((activation_grad_kernel<uint16_t, float>), grid, block, 0, stream, p);
-    else if (z_bf16)
-        hipLaunchKernelGGL((activation_grad_kernel<float, uint16_t>), grid, block, 0, stream, p);
+    auto launch = [&](auto t, auto z, auto nt) {
+        hipLaunchKernelGGL((activation_grad_kernel<decltype(t), decltype(z), decltype(nt)::value>), grid, block, 0, stream, p);
+    };
+    auto choose = [&](auto nt) {
+        if (bf16 && z_bf16)
+            launch(uint16_t{}, uint16_t{}, nt);
+        else if (bf16)
+            launch(uint16_t{}, float{}, nt);
+        else if (z_bf16)
+            launch(float{}, uint16_t{}, nt);
+        else
+            launch(float{}, float{}, nt);
+    };
+    if (p.streaming)
+        choose(std::true_type{});
     else
-        hipLaunchKernelGGL((activation_grad_kernel<float, float>), grid, block, 0, stream, p);
+        choose(std::false_type{});
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.db == nullptr || p.bands == 1)
         return e;
@@ -391,10 +439,15 @@ hipError_t launch_activation_grad(bool bf16, bool z_bf16, const GradParams &p, h
 }
 
 hipError_t launch_grad_squares(uint32_t groups, const NormParams &p, hipStream_t stream) {
-    if (p.grad_bf16)
-        hipLaunchKernelGGL(grad_squares_kernel<uint16_t>, dim3(groups), dim3(kStepThreads), 0, stream, p);
+    const dim3 grid(groups), block(kStepThreads);
+    if (p.grad_bf16 && p.streaming)
+        hipLaunchKernelGGL((grad_squares_kernel<uint16_t, true>), grid, block, 0, stream, p);
+    else if (p.grad_bf16)
+        hipLaunchKernelGGL((grad_squares_kernel<uint16_t, false>), grid, block, 0, stream, p);
+    else if (p.streaming)
+        hipLaunchKernelGGL((grad_squares_kernel<float, true>), grid, block, 0, stream, p);
     else
-        hipLaunchKernelGGL(grad_squares_kernel<float>, dim3(groups), dim3(kStepThreads), 0, stream, p);
+        hipLaunchKernelGGL((grad_squares_kernel<float, false>), grid, block, 0, stream, p);
     return hipGetLastError();
 }
 
@@ -405,17 +458,22 @@ hipError_t launch_grad_norm(const double *partial, int64_t count, float *norm, h
 
 hipError_t launch_adamw(int state_bits, uint32_t groups, const StepParams &p, hipStream_t stream) {
     const dim3 grid(groups), block(kStepThreads);
-    if (state_bits == 32) {
-        if (p.grad_bf16)
-            hipLaunchKernelGGL(adamw_kernel<uint16_t>, grid, block, 0, stream, p);
+    auto launch = [&](auto g, auto nt) {
+        using G = decltype(g);
+        constexpr bool NT = decltype(nt)::value;
+        if (state_bits == 32)
+            hipLaunchKernelGGL((adamw_kernel<G, NT>), grid, block, 0, stream, p);
         else
-            hipLaunchKernelGGL(adamw_kernel<float>, grid, block, 0, stream, p);
-    } else {
-        if (p.grad_bf16)
-            hipLaunchKernelGGL(adamw8_kernel<uint16_t>, grid, block, 0, stream, p);
-        else
-            hipLaunchKernelGGL(adamw8_kernel<float>, grid, block, 0, stream, p);
-    }
+            hipLaunchKernelGGL((adamw8_kernel<G, NT>), grid, block, 0, stream, p);
+    };
+    if (p.grad_bf16 && p.streaming)
+        launch(uint16_t{}, std::true_type{});
+    else if (p.grad_bf16)
+        launch(uint16_t{}, std::false_type{});
+    else if (p.streaming)
+        launch(float{}, std::true_type{});
+    else
+        launch(float{}, std::false_type{});
     return hipGetLastError();
 }
 

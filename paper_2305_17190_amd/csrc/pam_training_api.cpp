@@ -275,6 +275,7 @@ pam_status_t pam_activation_grad(const pam_activation_grad_t *args, hipStream_t 
     p.m = a.m;
     p.n = (int32_t)a.n;
     p.activation = a.activation;
+    p.streaming = a.m * a.n * (each * (a.dz != nullptr ? 2 : 1) + (none ? 0 : size_of(a.z_type))) > pamk::kCacheBytes;
     const GradCut cut = grad_cut(std::max<int64_t>(a.m, 1), a.n, pamk::grad_values(bf16));
     p.lanes = cut.lanes;
     p.band = (int32_t)std::min<int64_t>(cut.band, kMaxDim);
@@ -323,6 +324,7 @@ pam_status_t pam_grad_norm(const pam_step_tensor_t *tensors, int64_t count, pam_
         pamk::NormParams p{};
         p.chunk = chunk;
         p.grad_bf16 = grad_type == PAM_TYPE_BF16;
+        p.streaming = total * size_of(grad_type) > pamk::kCacheBytes;
         p.partial = partial + done;
         uint32_t here = 0;
         for (; j < count && p.count < pamk::kNormTensors; ++j) {
@@ -429,6 +431,7 @@ pam_status_t pam_adamw_step(const pam_step_tensor_t *tensors, int64_t count, con
     p.eps = (float)a.eps;
     p.seed = a.seed;
     p.grad_bf16 = a.grad_type == PAM_TYPE_BF16;
+    p.streaming = total * (4 + size_of(a.grad_type) + (bytes ? 2 : 8)) > pamk::kCacheBytes;
     for (int64_t j = 0; j < count;) {
         p.count = 0;
         p.tensor0 = (int32_t)j;

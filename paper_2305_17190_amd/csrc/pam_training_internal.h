@@ -10,6 +10,10 @@
 
 namespace pamk {
 
+// Calls on more memory than the last-level cache holds take the hint: what they
+// read first would have left the cache by the time it is read again.
+constexpr int64_t kCacheBytes = (int64_t)256 << 20;
+
 // ---------------------------------------------------------------------------
 // The activations' gradient
 // ---------------------------------------------------------------------------
@@ -29,6 +33,7 @@ struct GradParams {
     int32_t n;
     int32_t bands, band, lanes;
     int32_t activation;
+    int32_t streaming;   // loads with the non-temporal hint
 };
 inline int grad_values(bool bf16) { return bf16 ? 8 : 4; }
 hipError_t launch_activation_grad(bool bf16, bool z_bf16, const GradParams &p, hipStream_t stream);
@@ -63,6 +68,7 @@ struct StepParams {
     float beta1, rest1, beta2, rest2, eps, max_norm;
     uint32_t seed;
     int32_t grad_bf16;
+    int32_t streaming;     // with the non-temporal hint
 };
 static_assert(sizeof(StepParams) <= 4096, "a kernel's arguments");
 hipError_t launch_adamw(int state_bits, uint32_t groups, const StepParams &p, hipStream_t stream);
@@ -73,6 +79,7 @@ struct NormParams {
     uint32_t first[kNormTensors];
     int32_t count;
     int32_t grad_bf16;
+    int32_t streaming;     // loads with the non-temporal hint
     int64_t chunk;
     double *partial;       // one a workgroup
 };
