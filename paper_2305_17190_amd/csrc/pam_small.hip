@@ -80,6 +80,16 @@ __global__ void __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(4)
     TileB::template copy<kRawA * 4, 2>(b_base, lds_w, tid, p.ldb, n0, p.n, p.k, kind_b);
     if (tid < 2)
         sVote[tid] = 0u;
+    // A linear layer's bias and residual, ahead of the chunks.
+    const bool own = tid < D * D / 4;
+    const int orow = tid / (D / 4), ocol = tid % (D / 4) * 4;
+    float bias[4], res[4];
+    if constexpr (EPI) {
+        if (own && m0 + orow < p.m) {
+            load_bias4(p.epi, n0 + ocol, p.n - n0 - ocol, bias);
+            load_residual4(p.epi, m0 + orow, n0 + ocol, p.n - n0 - ocol, res);
+        }
+    }
 
     // A chunk's sums start at zero and are added to the running ones: chains
     // of 16 roundings, so that eight waves' parts of K round no more than the
@@ -220,6 +230,24 @@ __global__ void __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(4)
         *reinterpret_cast<float4 *>(&red[(wave * D + r0 + i) * D + c0]) =
             make_float4(total[i][0], total[i][1], total[i][2], total[i][3]);
     __syncthreads();
+    if constexpr (EPI) {
+        // A linear layer's outputs, four neighbours a thread.
+        if (own && m0 + orow < p.m) {
+            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int g = 0; g < KW; ++g) {
+                const float4 x = *reinterpret_cast<const float4 *>(&red[(g * D + orow) * D + ocol]);
+                v[0] = g == 0 ? x.x : v[0] + x.x;
+                v[1] = g == 0 ? x.y : v[1] + x.y;
+                v[2] = g == 0 ? x.z : v[2] + x.z;
+                v[3] = g == 0 ? x.w : v[3] + x.w;
+            }
+            with_activation(p.epi.activation, [&](auto act) {
+                finish4<decltype(act)::value>(p.epi, m0 + orow, n0 + ocol, p.n - n0 - ocol, v, bias, res);
+            });
+        }
+        return;
+    }
     float *out = p.C + bz * p.strideC + (int64_t)m0 * p.ldc + n0;
 #pragma unroll
     for (int o = tid; o < D * D; o += NT) {
@@ -228,10 +256,7 @@ __global__ void __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(4)
         for (int g = 1; g < KW; ++g)
             s += red[g * D * D + o];
         const int row = o / D, col = o % D;
-        if constexpr (EPI) {
-            if (m0 + row < p.m && n0 + col < p.n)
-                finish1(p.epi, m0 + row, n0 + col, s);
-        } else if (m0 + row < p.m && n0 + col < p.n)
+        if (m0 + row < p.m && n0 + col < p.n)
             out[(int64_t)row * p.ldc + col] = s;
     }
 }
