@@ -1,11 +1,12 @@
 """A small decoder whose products are PAM: trained with whole sequences, answering
 from a paged key/value cache.
 
-    python examples/decoder.py [--steps N] [--new TOKENS]
+    python examples/decoder.py [--steps N] [--new TOKENS] [--state-bits 8]
 
-Training runs the linear layers through ``PAMLinear``, queries and keys through
+Training runs the linear layers through ``PAMLinear``, the activation and the
+residual stream in their products' launches, queries and keys through
 ``pam_norm_rope`` and the attention through ``pam_matmul`` with a softmax between,
-under autograd.  Answering runs the same weights over ``append_kv`` and
+under autograd; ``AdamW`` steps over all parameters at once.  Answering runs the same weights over ``append_kv`` and
 ``paged_attention``: the prompts in chunks of different lengths at once, then one
 token a sequence.  The two are the same function, so the logits agree to
 float32 rounding; the example checks that and says how far they are apart.
@@ -24,6 +25,7 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 import paper_2305_17190_amd as pam  # noqa: E402
 from paper_2305_17190_amd.autograd import PAMLinear, pam_matmul, pam_norm_rope  # noqa: E402
+from paper_2305_17190_amd.optim import AdamW  # noqa: E402
 
 
 class Cache:
@@ -60,7 +62,8 @@ class Layer(nn.Module):
         self.norm1, self.norm2 = (nn.RMSNorm(width, device=device) for _ in range(2))
         self.qkv = PAMLinear(width, (heads + 2 * kv_heads) * d, bias=False, device=device)
         self.out = PAMLinear(heads * d, width, bias=False, device=device)
-        self.up, self.down = PAMLinear(width, hidden, device=device), PAMLinear(hidden, width, device=device)
+        self.up = PAMLinear(width, hidden, device=device, activation="relu")
+        self.down = PAMLinear(hidden, width, device=device)
         self.q_weight, self.k_weight = (nn.Parameter(torch.ones(d, device=device)) for _ in range(2))
 
     def heads_of(self, x):
@@ -69,8 +72,8 @@ class Layer(nn.Module):
         return qkv.split((self.heads, self.kv_heads, self.kv_heads), 1)
 
     def rest(self, x, attended):
-        x = x + self.out(attended.reshape(x.shape[0], -1))
-        return x + self.down(torch.relu(self.up(self.norm2(x))))
+        x = self.out(attended.reshape(x.shape[0], -1), residual=x)
+        return self.down(self.up(self.norm2(x)), residual=x)
 
     def whole(self, x, batch, positions, cos, sin):
         """All tokens of `batch` sequences of one length, differentiable."""
@@ -133,9 +136,9 @@ def batch_of(rng, size, half, vocabulary):
     return torch.cat((first, first), 1).cuda()
 
 
-def train(model, steps, half=12, size=32):
+def train(model, steps, half=12, size=32, state_bits=32):
     rng = torch.Generator().manual_seed(0)
-    optimizer = torch.optim.AdamW(model.parameters(), lr=2e-3, weight_decay=0.01)
+    optimizer = AdamW(model.parameters(), lr=2e-3, weight_decay=0.01, state_bits=state_bits)
     losses = []
     for _ in range(steps):
         tokens = batch_of(rng, size, half, model.embed.num_embeddings)
@@ -180,10 +183,11 @@ def main(argv=None):
     parser = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     parser.add_argument("--steps", type=int, default=300)
     parser.add_argument("--new", type=int, default=12)
+    parser.add_argument("--state-bits", type=int, default=32, choices=(8, 32))
     args = parser.parse_args(argv)
     torch.manual_seed(0)
     model = Decoder()
-    losses = train(model, args.steps)
+    losses = train(model, args.steps, state_bits=args.state_bits)
     if losses:
         print(f"loss {losses[0]:.3f} -> {losses[-1]:.3f} in {len(losses)} steps")
     tokens = batch_of(torch.Generator().manual_seed(1), 4, 12, 64)
