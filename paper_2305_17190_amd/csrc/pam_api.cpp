@@ -525,6 +525,8 @@ bool small_product(const Plan &plan, PlanOf whose, int64_t m, int64_t n, int64_t
 struct LinearSpace {
     size_t partial, folds;
 };
+int64_t fold_bytes(const Plan &plan) { return (int64_t)plan.kgroups * plan.tile_m * plan.tile_n * (int64_t)sizeof(float); }
+int64_t fold_items(const Plan &plan) { return pamk::kFoldBytes / fold_bytes(plan); }   // of a launch, at most
 
 pam_status_t linear_space(const Plan &plan, int64_t m, int64_t n, int64_t k, LinearSpace *out) {
     Layout L{};
@@ -537,7 +539,7 @@ pam_status_t linear_space(const Plan &plan, int64_t m, int64_t n, int64_t k, Lin
     const int64_t whole = L.splits > 1 ? L.whole_tiles : L.total;
     const int64_t longest = whole > 0 ? k : plan.k_per_split;
     if (!other && longest > (int64_t)pamk::kFoldChunks * pamk::kChunkK * plan.kgroups)
-        out->folds = (size_t)(whole + (L.total - whole) * L.splits) * plan.kgroups * plan.tile_m * plan.tile_n * sizeof(float);
+        out->folds = (size_t)(std::min(whole + (L.total - whole) * L.splits, fold_items(plan)) * fold_bytes(plan));
     return PAM_SUCCESS;
 }
 
@@ -617,8 +619,17 @@ pam_status_t run_gemm(pam_op_t ta, pam_op_t tb, int64_t m, int64_t n, int64_t k,
             p.whole = (int32_t)(nb * L.tiles);
             p.split_tiles = 0;
         }
-        hipError_t e = pamk::launch_pam_gemm(plan.tile_m, plan.tile_n, plan.kgroups, ta == PAM_OP_T, tb == PAM_OP_T,
-                                             bf16, p, stream);
+        const int64_t items = p.whole + (int64_t)p.split_tiles * p.splits;
+        const int64_t most = p.epi.folds != nullptr ? fold_items(plan) : items;
+        hipError_t e = hipSuccess;
+        for (int64_t i = 0; i < items && e == hipSuccess; i += most) {
+            if (most < items) {
+                p.epi.first_item = (int32_t)i;
+                p.epi.items = (int32_t)std::min(most, items - i);
+            }
+            e = pamk::launch_pam_gemm(plan.tile_m, plan.tile_n, plan.kgroups, ta == PAM_OP_T, tb == PAM_OP_T, bf16, p,
+                                      stream);
+        }
         if (e != hipSuccess)
             return fail_hip(e, "gemm kernel launch");
         if (p.split_tiles > 0) {

@@ -228,7 +228,7 @@ __device__ __forceinline__ ParamsAgain *params_again() {
 }
 __device__ __forceinline__ Epilogue epilogue_of(ParamsAgain *p) {
     return {p->epi.bias, p->epi.residual, p->epi.y, p->epi.z, p->epi.ldr, p->epi.ldy, p->epi.ldz, p->epi.activation,
-            p->epi.out_bf16, nullptr};
+            p->epi.out_bf16, nullptr, 0, 0};
 }
 
 // WPS: waves per SIMD the kernel is compiled for.  At two (256 registers a
@@ -292,7 +292,7 @@ pam_gemm_dma_kernel(GemmParams p) {
     const int lane = tid & 63;
     const int tx = wc * 8 + (lane & 7);
     const int ty = wr * 8 + (lane >> 3);
-    const uint32_t item = blockIdx.x;
+    const uint32_t item = EPI ? blockIdx.x + (uint32_t)p.epi.first_item : blockIdx.x;
     const bool whole = item < (uint32_t)p.whole;
     const uint32_t rel = item - (uint32_t)p.whole;
     const uint32_t nsplit = (uint32_t)max(p.split_tiles, 1);
@@ -498,7 +498,7 @@ pam_gemm_dma_kernel(GemmParams p) {
             uint32_t place = (uint32_t)t * 16u;
             asm volatile("" : "+v"(place)::"memory");
             char *at = reinterpret_cast<char *>(params_again()->epi.folds) +
-                       ((int64_t)item * KW + __builtin_amdgcn_readfirstlane(grp)) * (256 * NTG);
+                       ((int64_t)blockIdx.x * KW + __builtin_amdgcn_readfirstlane(grp)) * (256 * NTG);
             return reinterpret_cast<float4 *>(at + q * 16 * NTG + place);
         };
         int c = 0;
@@ -755,7 +755,7 @@ extern PAM_DMA_SHAPE(uint16_t, 2);
 
 hipError_t launch_pam_gemm(int tile_m, int tile_n, int kgroups, bool trans_a, bool trans_b, bool bf16,
                                const GemmParams &p, hipStream_t stream) {
-    const int64_t items = (int64_t)p.whole + (int64_t)p.split_tiles * p.splits;
+    const int64_t items = p.epi.items > 0 ? p.epi.items : (int64_t)p.whole + (int64_t)p.split_tiles * p.splits;
     if (items <= 0 || items > kMaxLaunchItems)
         return hipErrorInvalidValue;
     const int bk = kChunkK * kgroups;

@@ -27,13 +27,18 @@ struct Epilogue {
     int32_t activation;     // pam_activation_t
     int32_t out_bf16;
     // Running sums of the tiled kernel, kept here every kFoldChunks chunks: [work
-    // item][k-group][16-byte column][thread], or nullptr where no chain is longer.
+    // item of the launch][k-group][16-byte column][thread], or nullptr where no
+    // chain is longer.
     float *folds;
+    int32_t first_item;     // of the launch, and how many (0: all of the plan's)
+    int32_t items;
 };
 // A sum's longest chain of roundings in a linear layer's tiles: so many chunks
 // of kChunkK terms.  A chain of L terms of either sign is off by about sqrt(L) / 3
 // units of 2^-24: 1.2e-6 of the result over K = 4096, 5.7e-7 in parts of 1024.
 constexpr int kFoldChunks = 64;
+// Work items beyond what this memory holds running sums of take launches of their own.
+constexpr int64_t kFoldBytes = (int64_t)512 << 20;
 
 // Arguments of one (batched, possibly split-K) PAM matrix product launch.
 //

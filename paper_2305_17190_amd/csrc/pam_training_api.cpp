@@ -53,8 +53,11 @@ Range range_of(const void *data, int64_t bytes, bool written) {
     const uintptr_t at = reinterpret_cast<uintptr_t>(data);
     return {at, at + (uintptr_t)(data == nullptr ? 0 : bytes), written};
 }
+// rows, cols below 2^31, ld at most 2^31: the last element's place is below 2^62 + 2^31,
+// its byte may not be; no memory is that large.
 Range rows_of(const void *data, int64_t rows, int64_t cols, int64_t ld, int64_t size, bool written) {
-    return range_of(data, rows > 0 && cols > 0 ? ((rows - 1) * ld + cols) * size : 0, written);
+    const int64_t elements = rows > 0 && cols > 0 ? (rows - 1) * ld + cols : 0;
+    return range_of(data, std::min(elements, (int64_t)1 << 56) * size, written);
 }
 
 bool overlap(const Range &a, const Range &b) { return a.begin < b.end && b.begin < a.end; }
@@ -118,6 +121,26 @@ GradCut grad_cut(int64_t m, int64_t n, int values) {
 // Many tensors at once
 // ---------------------------------------------------------------------------
 
+// By beginning: ascending runs merged, one with the next, until one is left (lists
+// of tensors in ascending order are a few runs; spare is as long as ranges).
+void sort_runs(std::vector<Range> &ranges, std::vector<Range> &spare) {
+    auto before = [](const Range &a, const Range &b) { return a.begin < b.begin; };
+    spare.resize(ranges.size());
+    for (size_t runs = 2; runs > 1;) {
+        runs = 0;
+        auto from = ranges.begin();
+        auto to = spare.begin();
+        while (from != ranges.end()) {
+            const auto middle = std::is_sorted_until(from, ranges.end(), before);
+            const auto end = std::is_sorted_until(middle, ranges.end(), before);
+            to = std::merge(from, middle, middle, end, to, before);
+            from = end;
+            ++runs;
+        }
+        ranges.swap(spare);
+    }
+}
+
 constexpr int64_t kMaxTensors = 1 << 20;
 constexpr int64_t kMaxValues = (int64_t)1 << 38;   // 1 TB of float32
 
@@ -136,9 +159,9 @@ pam_status_t check_tensors(const pam_step_tensor_t *tensors, int64_t count, int6
 }
 
 // Values a workgroup of the norm takes: at most kNormPartials of them in all
-// (but one a tensor at least), in steps of 4096.
+// (but one a tensor at least), in steps of 1024.
 constexpr int64_t kNormPartials = 2048;
-int64_t norm_chunk(int64_t total) { return 4096 * std::max<int64_t>(1, ceil_div(total, 4096 * kNormPartials)); }
+int64_t norm_chunk(int64_t total) { return 1024 * std::max<int64_t>(1, ceil_div(total, 1024 * kNormPartials)); }
 
 int64_t norm_groups(const pam_step_tensor_t *tensors, int64_t count, int64_t chunk) {
     int64_t groups = 0;
@@ -367,16 +390,6 @@ pam_status_t pam_adamw_step(const pam_step_tensor_t *tensors, int64_t count, con
     PAM_TRY(check_tensors(tensors, count, &total));
     const int64_t chunk = step_chunk(total);
     const bool bytes = a.state_bits == 8;
-    std::vector<Range> ranges;
-    try {
-        ranges.reserve((size_t)count * 7 + 2);   // what is pushed below
-    } catch (const std::bad_alloc &) {
-        return invalid("no host memory to compare the tensors' addresses");
-    }
-    if (a.norm != nullptr)
-        ranges.push_back(range_of(a.norm, 4, false));
-    if (a.step_device != nullptr)
-        ranges.push_back(range_of(a.step_device, 8, false));
     int64_t groups = 0;
     for (int64_t j = 0; j < count; ++j) {
         const pam_step_tensor_t &t = tensors[j];
@@ -387,21 +400,36 @@ pam_status_t pam_adamw_step(const pam_step_tensor_t *tensors, int64_t count, con
         if (bytes != (t.avg_scale != nullptr) || bytes != (t.sq_scale != nullptr))
             return invalid("8-bit states have scales, 32-bit ones none");
         groups += ceil_div(t.n, chunk);
-        const int64_t state = bytes ? 1 : 4, scales = ceil_div(t.n, PAM_STATE_BLOCK) * 4;
-        ranges.push_back(range_of(t.p, t.n * 4, true));
-        ranges.push_back(range_of(t.g, t.n * size_of(a.grad_type), false));
-        ranges.push_back(range_of(t.avg, t.n * state, true));
-        ranges.push_back(range_of(t.sq, t.n * state, true));
-        if (bytes) {
-            ranges.push_back(range_of(t.avg_scale, scales, true));
-            ranges.push_back(range_of(t.sq_scale, scales, true));
-        }
-        if (t.copy != nullptr)
-            ranges.push_back(range_of(t.copy, t.n * 2, true));
     }
     if (groups > pamk::kMostStepGroups)
         return invalid("too many values");
-    std::sort(ranges.begin(), ranges.end(), [](const Range &x, const Range &y) { return x.begin < y.begin; });
+    std::vector<Range> ranges, spare;
+    try {
+        ranges.reserve((size_t)count * 7 + 2);   // what is pushed below
+        spare.resize((size_t)count * 7 + 2);
+    } catch (const std::bad_alloc &) {
+        return invalid("no host memory to compare the tensors' addresses");
+    }
+    if (a.norm != nullptr)
+        ranges.push_back(range_of(a.norm, 4, false));
+    if (a.step_device != nullptr)
+        ranges.push_back(range_of(a.step_device, 8, false));
+    // List by list: tensors made one after the other lie in ascending order.
+    auto list = [&](auto data, auto size, bool written) {
+        for (int64_t j = 0; j < count; ++j)
+            if (tensors[j].n > 0 && data(tensors[j]) != nullptr)
+                ranges.push_back(range_of(data(tensors[j]), size(tensors[j].n), written));
+    };
+    const int64_t grad = size_of(a.grad_type), state = bytes ? 1 : 4;
+    auto scales = [](int64_t n) { return ceil_div(n, PAM_STATE_BLOCK) * 4; };
+    list([](auto &t) -> const void * { return t.p; }, [](int64_t n) { return n * 4; }, true);
+    list([](auto &t) -> const void * { return t.g; }, [&](int64_t n) { return n * grad; }, false);
+    list([](auto &t) -> const void * { return t.avg; }, [&](int64_t n) { return n * state; }, true);
+    list([](auto &t) -> const void * { return t.sq; }, [&](int64_t n) { return n * state; }, true);
+    list([](auto &t) -> const void * { return t.avg_scale; }, scales, true);
+    list([](auto &t) -> const void * { return t.sq_scale; }, scales, true);
+    list([](auto &t) -> const void * { return t.copy; }, [](int64_t n) { return n * 2; }, true);
+    sort_runs(ranges, spare);
     uintptr_t written = 0, read = 0;   // ends of the ranges so far
     for (const Range &r : ranges) {
         if (r.begin < written || (r.written && r.begin < read))

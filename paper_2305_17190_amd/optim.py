@@ -32,6 +32,10 @@ class AdamW(torch.optim.Optimizer):
         self.last_norm = None
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
 
+    def __getstate__(self):
+        return {**super().__getstate__(), "max_norm": self.max_norm, "state_bits": self.state_bits, "seed": self.seed,
+                "last_norm": self.last_norm}
+
     def _state_of(self, p):
         state = self.state[p]
         if not state:
@@ -48,8 +52,8 @@ class AdamW(torch.optim.Optimizer):
         """As torch's, but the loaded tensors are copied, and codes stay bytes (torch
         makes every state the parameter's type)."""
         for state in state_dict["state"].values():
-            if state and ("avg_scale" in state) != (self.state_bits == 8):
-                raise ValueError(f"the loaded states are not held in {self.state_bits} bits")
+            if state and ("avg" not in state or ("avg_scale" in state) != (self.state_bits == 8)):
+                raise ValueError(f"the loaded states are not this optimizer's in {self.state_bits} bits")
         super().load_state_dict(state_dict)
         for state in self.state.values():
             for key in ("avg", "sq", "avg_scale", "sq_scale"):

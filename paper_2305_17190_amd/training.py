@@ -249,6 +249,8 @@ def _check_lists(*lists) -> None:
             if t.layout != torch.strided or not t.is_contiguous():
                 raise ValueError(f"{name}[{j}] must be contiguous")
         named[name] = tensors
+    if "grads" not in named:
+        raise TypeError("grads must be a list or tuple of tensors")
     grads = named["grads"]
     for name, tensors in named.items():
         if len(tensors) != len(grads):
@@ -327,6 +329,9 @@ def adamw_step(params, grads, avgs, sqs, step, lr: float = 1e-3, betas=(0.9, 0.9
     to it).  ``norm`` is ``grad_norm``'s result (or any float32 tensor of one
     element)."""
     torch = _torch()
+    for name, tensors in (("params", params), ("grads", grads), ("avgs", avgs), ("sqs", sqs)):
+        if tensors is None:
+            raise TypeError(f"{name} must be a list or tuple of tensors")
     count, tensors, bf16, eight, first = _step_tensors(params, grads, avgs, sqs, avg_scales, sq_scales, copies)
     for name, t in (("norm", norm), ("step", step if isinstance(step, torch.Tensor) else None)):
         if t is None:

@@ -116,6 +116,45 @@ def test_long_sums(m, k, n, bf16):
     assert same(again, y)
 
 
+def test_long_sums_of_many_tiles():
+    """More work items than their running sums' memory holds: several launches."""
+    import torch
+    m, k, n = 16640, 1040, 8192
+    assert -(-m // 128) * (n // 128) * 65536 > 512 << 20
+    note(f"linear {m}x{k}x{n}, running sums in rounds")
+    x, w, bias, _ = inputs(m, k, n, True)
+    y = pam.linear(x, w, bias, out_dtype=torch.bfloat16)
+    rows, cols = (np.unique(np.linspace(0, s - 1, 50).astype(int)) for s in (m, n))
+    want, size = pam_ref.pam_gemm_ref(x[rows].float().cpu().numpy(), w[cols].float().cpu().numpy(), False, True)
+    want = want + bias[cols].cpu().numpy().astype(np.float64)
+    check(y[rows][:, cols].float().cpu().numpy(), want, 1100 * tu.U * size + 2.0 ** -8 * np.abs(want), "y")
+    whole = pam.gemm(x, w, trans_b=True) + bias
+    off = (y.float() - whole).abs() - 2.0 ** -8 * whole.abs()
+    assert float(off.max()) <= 1e-4          # every output, against the other order of sums
+
+
+def test_few_rows_at_the_top_of_the_range():
+    """Magnitudes about 2^63 and 2^64, whose products reach the largest float32: the
+    forms without a range check may not take them."""
+    import torch
+    note("linear, few rows, magnitudes about 2^64")
+    rng = np.random.default_rng(8)
+    for bf16 in (False, True):
+        for m, n in ((5, 40), (40, 5)):
+            x, w = ((2.0 ** rng.integers(61, 66, (r, 64)) * (1 + rng.random((r, 64))) *
+                     rng.choice([-1, 1], (r, 64))).astype(np.float32) for r in (m, n))
+            x[:, 1:], w[:, 2:] = x[:, 1:] * np.float32(2.0 ** -70), w[:, 2:] * np.float32(2.0 ** -70)
+            xd, wd = to_dev(x), to_dev(w)
+            if bf16:
+                xd, wd = xd.bfloat16(), wd.bfloat16()
+                x, w = xd.float().cpu().numpy(), wd.float().cpu().numpy()
+            # One term at the top, the others far below: float32 sums are the terms'.
+            want, size = pam_ref.pam_gemm_ref(x, w, False, True)
+            got = pam.linear(xd, wd).cpu().numpy()
+            assert np.isfinite(got).all() and np.abs(want).max() > 1e38
+            check(got, want, 70 * tu.U * size, "product")
+
+
 def test_narrow_mantissas():
     import torch
     note("linear, 7 mantissa bits")

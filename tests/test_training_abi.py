@@ -54,7 +54,7 @@ def linear(lib, **change):
     dict(type=-1), dict(out_type=2), dict(activation=5), dict(activation=-1), dict(mantissa_bits=24),
     dict(mantissa_bits=-1), dict(type=1, mantissa_bits=7), dict(y=at(0)), dict(y=at(1) + 4), dict(z=at(4)), dict(z=at(3)),
     dict(z=at(4) + 4 * 300 * 200 - 4), dict(y=at(2)), dict(residual=at(4), ldr=201), dict(residual=at(4) + 4),
-    dict(workspace=at(4)), dict(workspace=at(0)), dict(k=8192, ldx=8192, ldw=8192, workspace=0),
+    dict(workspace=at(4)), dict(workspace=at(0)), dict(m=(1 << 31) - 1, ldr=1 << 31, ldy=1 << 31, ldz=1 << 31), dict(k=8192, ldx=8192, ldw=8192, workspace=0),
     dict(k=8192, ldx=8192, ldw=8192, workspace_bytes=4), dict(k=8192, ldx=8192, ldw=8192, workspace=at(6) + 4)])
 def test_linear_refuses(lib, change):
     assert linear(lib, **change) == INVALID, lib.pam_last_error()
@@ -212,6 +212,13 @@ def test_binding_refuses_what_is_not_on_the_gpu(lib):
         pam.grad_norm([None])
     with pytest.raises(ValueError, match="at least one"):
         pam.grad_norm([])
+    with pytest.raises(TypeError, match="grads"):
+        pam.grad_norm(None)
+    for missing in range(4):
+        lists = [[x]] * 4
+        lists[missing] = None
+        with pytest.raises(TypeError, match="list or tuple"):
+            pam.adamw_step(*lists, 1)
 
 
 def test_checks_of_the_binding(monkeypatch):
@@ -271,3 +278,14 @@ def test_optimizer_refusals():
         AdamW(p, state_bits=16)
     with pytest.raises(ValueError, match="max_norm"):
         AdamW(p, max_norm=0.0)
+    import copy
+    import pickle
+    made = AdamW(p, lr=0.5, max_norm=2.0, state_bits=8, seed=3)
+    for other in (copy.deepcopy(made), pickle.loads(pickle.dumps(made))):
+        assert (other.max_norm, other.state_bits, other.seed) == (2.0, 8, 3) and other.param_groups[0]["lr"] == 0.5
+    state = torch.optim.AdamW(p).state_dict()
+    made.load_state_dict(state)
+    state["state"] = {0: dict(step=1, exp_avg=torch.zeros(3))}
+    for bits in (8, 32):
+        with pytest.raises(ValueError, match="8 bits" if bits == 8 else "32 bits"):
+            AdamW(p, state_bits=bits).load_state_dict(state)
