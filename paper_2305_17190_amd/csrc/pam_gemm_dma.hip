@@ -616,7 +616,9 @@ pam_gemm_dma_kernel(GemmParams p) {
         if (grp > 0 && !(EPI && whole))
             return;
     }
-    // A linear layer's outputs.  The sums go through LDS, two rows of each
+    // A linear layer's outputs, at 1-4% of the product's time (8192 x 512 -> 2048
+    // 294 us, with bias and gelu 302, with z as well 307; 4096^3 2193 us, with silu, z
+    // and long sums in parts 2230).  The sums go through LDS, two rows of each
     // thread's micro-tile at a time, so that the activation's code works on four
     // values in a loop (beside the 64 sums of a thread it spilled 98 registers),
     // with all threads of the workgroup, those of the other k-groups too.

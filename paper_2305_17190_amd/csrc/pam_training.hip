@@ -1,6 +1,12 @@
 // The layer-and-step side's streams over memory on gfx950: the activations'
 // gradient with the bias's, the norm of all gradients, and the AdamW step over
-// many tensors.  All are bound by reading and writing each value once.
+// many tensors.  All are bound by reading and writing each value once; a large
+// copy runs at 4.9 TB/s on these cards, reading and writing streams at up to 6.2.
+// Measured (passes in a row): the gradient of 16384 x 4096 float32 values 129 us (6.2
+// TB/s), bfloat16 71 us (5.7), 8192 x 2048 float32 39.5 us (5.1, the sums' launch 4
+// of it); the norm of 188 M float32 values 114 us (6.6 TB/s); the step over them 910
+// us (5.8 TB/s), with 8-bit states 530 us (5.7); the norm and the step of a decoder's
+// 25.7 M parameters, gradients and copies bfloat16, 140 us (5.5).
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -13,33 +19,31 @@
 namespace pamk {
 namespace {
 
-// V neighbouring elements, at any address, widened; `have` of them exist.  NT:
-// with the non-temporal hint.
-template <int V, bool NT = false, typename T> __device__ __forceinline__ void load_wide(const T *p, int have, float (&x)[V]) {
-    typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-    if (have >= V) {
-        const vec *at = reinterpret_cast<const vec *>(p);
-        const vec v = NT ? __builtin_nontemporal_load(at) : *at;
+// V neighbouring elements at any address.  NT: with the non-temporal hint.
+template <int V, typename T> using Wide = T __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+template <int V, bool NT, typename T> __device__ __forceinline__ Wide<V, T> load_raw(const T *p) {
+    const Wide<V, T> *at = reinterpret_cast<const Wide<V, T> *>(p);
+    return NT ? __builtin_nontemporal_load(at) : *at;
+}
+// Elements one by one, the `have` that exist.
+template <int V, typename T> __device__ __forceinline__ Wide<V, T> load_some(const T *p, int have) {
+    Wide<V, T> v;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if constexpr (sizeof(T) == 2)
-                x[i] = bf16_value(v[i]);
-            else
-                x[i] = v[i];
-        }
-    } else {
+    for (int i = 0; i < V; ++i)
+        v[i] = i < have ? p[i] : T(0);
+    return v;
+}
+template <int V, typename T> __device__ __forceinline__ void widened(const Wide<V, T> &v, float (&x)[V]) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if constexpr (sizeof(T) == 2)
-                x[i] = i < have ? bf16_value(p[i]) : 0.0f;
-            else
-                x[i] = i < have ? p[i] : 0.0f;
-        }
+    for (int i = 0; i < V; ++i) {
+        if constexpr (sizeof(T) == 2)
+            x[i] = bf16_value(v[i]);
+        else
+            x[i] = v[i];
     }
 }
-template <int V, bool NT = false, typename T> __device__ __forceinline__ void store_wide(T *p, int have, const float (&x)[V]) {
-    typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-    vec v;
+template <int V, typename T> __device__ __forceinline__ Wide<V, T> rounded(const float (&x)[V]) {
+    Wide<V, T> v;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         if constexpr (sizeof(T) == 2)
@@ -47,25 +51,29 @@ template <int V, bool NT = false, typename T> __device__ __forceinline__ void st
         else
             v[i] = x[i];
     }
-    if (have >= V) {
-        vec *at = reinterpret_cast<vec *>(p);
-        if constexpr (NT)
-            __builtin_nontemporal_store(v, at);
-        else
-            *at = v;
-    } else {
+    return v;
+}
+template <int V, bool NT, typename T> __device__ __forceinline__ void store_wide(T *p, const float (&x)[V]) {
+    Wide<V, T> *at = reinterpret_cast<Wide<V, T> *>(p);
+    if constexpr (NT)
+        __builtin_nontemporal_store(rounded<V, T>(x), at);
+    else
+        *at = rounded<V, T>(x);
+}
+template <int V, typename T> __device__ __forceinline__ void store_some(T *p, int have, const float (&x)[V]) {
+    const Wide<V, T> v = rounded<V, T>(x);
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < have)
-                p[i] = v[i];
-    }
+    for (int i = 0; i < V; ++i)
+        if (i < have)
+            p[i] = v[i];
 }
 
 // ---------------------------------------------------------------------------
 // The activations' gradient
 // ---------------------------------------------------------------------------
 
-// dz = dy f'(z) and the sums of its columns.  A thread keeps the sums of its V
+// dz = dy f'(z) and the sums of its columns, each value read once and written once:
+// the sums ride along.  A thread keeps the sums of its V
 // columns over the rows it takes; the workgroup's rows are added in a tree, in
 // LDS, and the bands' sums by sum_bands_kernel: an order fixed by the sizes.
 template <typename T, typename Z, bool NT> __global__ void __launch_bounds__(kGradThreads) activation_grad_kernel(GradParams p) {
@@ -77,23 +85,26 @@ template <typename T, typename Z, bool NT> __global__ void __launch_bounds__(kGr
     const int band = blockIdx.x / groups;
     const int col = (blockIdx.x - band * groups) * lanes * V + tx * V;
     const int have = min(p.n - col, V);
+    // A row's last columns, fewer than V: the V that end there, some of them the
+    // neighbour's too, whose dz is then written twice with the same value.  (Single
+    // elements made their whole wave wait: 197 x 771 in bfloat16 14.7 us, now 11.8.)
+    // Not where dz lies on an input, which the neighbour may have overwritten.
+    const int start = p.apart && p.n >= V ? min(col, p.n - V) : col;
     const int64_t end = min((int64_t)(band + 1) * p.band, p.m);
     float sum[V];
 #pragma unroll
     for (int i = 0; i < V; ++i)
         sum[i] = 0.0f;
-    if (have > 0) {
-        const T *dy = static_cast<const T *>(p.dy) + col;
-        const Z *z = static_cast<const Z *>(p.z) + col;
-        T *dz = static_cast<T *>(p.dz) + col;
+    const T *dy = static_cast<const T *>(p.dy) + start;
+    const Z *z = static_cast<const Z *>(p.z) + start;
+    T *dz = static_cast<T *>(p.dz) + start;
+    if (have > 0)
         with_activation(p.activation, [&](auto act) {
             constexpr int ACT = decltype(act)::value;
-#pragma unroll 4
-            for (int64_t r = (int64_t)band * p.band + ty; r < end; r += at_once) {
-                float d[V], x[V];
-                load_wide<V, NT>(dy + r * p.lddy, have, d);
+            auto slopes = [&](float (&d)[V], const Wide<V, Z> &zs) {
                 if constexpr (ACT != PAM_ACT_NONE) {
-                    load_wide<V, NT>(z + r * p.ldz, have, x);
+                    float x[V];
+                    widened<V, Z>(zs, x);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         if constexpr (ACT == PAM_ACT_RELU)
@@ -101,15 +112,55 @@ template <typename T, typename Z, bool NT> __global__ void __launch_bounds__(kGr
                         else
                             d[i] *= activation_slope<ACT>(x[i]);
                     }
-                    if (p.dz != nullptr)
-                        store_wide<V>(dz + r * p.lddz, have, d);
                 }
 #pragma unroll
                 for (int i = 0; i < V; ++i)
                     sum[i] += d[i];
+            };
+            int64_t r = (int64_t)band * p.band + ty;
+            if (have == V || start != col) {
+                // U rows' loads, then their work.
+                auto rows = [&](auto count) {
+                    constexpr int U = decltype(count)::value;
+                    Wide<V, T> d[U];
+                    Wide<V, Z> x[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        d[u] = load_raw<V, NT>(dy + (r + u * at_once) * p.lddy);
+                        if constexpr (ACT != PAM_ACT_NONE)
+                            x[u] = load_raw<V, NT>(z + (r + u * at_once) * p.ldz);
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        float g[V];
+                        widened<V, T>(d[u], g);
+                        slopes(g, x[u]);
+                        if (ACT != PAM_ACT_NONE && p.dz != nullptr)
+                            store_wide<V, false>(dz + (r + u * at_once) * p.lddz, g);
+                    }
+                };
+                // Several rows at once where the few there are make up a thread's time
+                // (64 x 512 6.5 -> 5.2 us); where memory does, one by one (8192 x 2048
+                // 39.5 us, by two 41.2, by four 46.8).
+                constexpr int kRows = 4;
+                if (p.bands == 1)
+                    for (; r + (kRows - 1) * at_once < end; r += kRows * at_once)
+                        rows(std::integral_constant<int, kRows>{});
+                for (; r < end; r += at_once)
+                    rows(std::integral_constant<int, 1>{});
+            } else {
+                for (; r < end; r += at_once) {
+                    Wide<V, Z> x{};
+                    if constexpr (ACT != PAM_ACT_NONE)
+                        x = load_some<V>(z + r * p.ldz, have);
+                    float g[V];
+                    widened<V, T>(load_some<V>(dy + r * p.lddy, have), g);
+                    slopes(g, x);
+                    if (ACT != PAM_ACT_NONE && p.dz != nullptr)
+                        store_some<V>(dz + r * p.lddz, have, g);
+                }
             }
         });
-    }
     if (p.db == nullptr)
         return;
 #pragma unroll
@@ -128,8 +179,8 @@ template <typename T, typename Z, bool NT> __global__ void __launch_bounds__(kGr
     float *out = p.bands == 1 ? p.db : p.partial + (int64_t)band * p.n;
 #pragma unroll
     for (int i = 0; i < V; ++i)
-        if (i < have)
-            out[col + i] = red[threadIdx.x * V + i];
+        if (start + i >= col && start + i < p.n)
+            out[start + i] = red[threadIdx.x * V + i];
 }
 
 // db = the sum of the bands' sums: 64 columns a workgroup, a quarter of the bands
@@ -171,14 +222,19 @@ template <typename T, bool NT> __global__ void __launch_bounds__(kStepThreads) g
     const T *g = static_cast<const T *>(p.g[j]);
     // In float64: a sum of 2^26 squares keeps its last bit, none overflows.
     double sum = 0.0;
-#pragma unroll 4
-    for (int64_t i = begin + threadIdx.x * V; i < end; i += kStepThreads * V) {
+    auto add = [&](const Wide<V, T> &v) {
         float x[V];
-        load_wide<V, NT>(g + i, (int)min(end - i, (int64_t)V), x);
+        widened<V, T>(v, x);
 #pragma unroll
         for (int e = 0; e < V; ++e)
             sum = __builtin_fma((double)x[e], (double)x[e], sum);
-    }
+    };
+    int64_t i = begin + threadIdx.x * V;
+#pragma unroll 4
+    for (; i + V <= end; i += kStepThreads * V)
+        add(load_raw<V, NT>(g + i));
+    if (i < end)
+        add(load_some<V>(g + i, (int)(end - i)));
     for (int d = 32; d > 0; d /= 2)
         sum += __shfl_xor(sum, d);
     if ((threadIdx.x & 63) == 0)
@@ -248,14 +304,7 @@ template <typename G, bool NT> __global__ void __launch_bounds__(kStepThreads) a
     const int64_t end = min(begin + p.chunk, t.n);
     const G *g = static_cast<const G *>(t.g);
     float *avg = static_cast<float *>(t.avg), *sq = static_cast<float *>(t.sq);
-#pragma unroll 2
-    for (int64_t i = begin + threadIdx.x * 4; i < end; i += kStepThreads * 4) {
-        const int have = (int)min(end - i, (int64_t)4);
-        float x[4], d[4], m[4], v[4];
-        load_wide<4, NT>(g + i, have, d);
-        load_wide<4, NT>(t.p + i, have, x);
-        load_wide<4, NT>(avg + i, have, m);
-        load_wide<4, NT>(sq + i, have, v);
+    auto step = [&](float (&x)[4], float (&d)[4], float (&m)[4], float (&v)[4]) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             d[e] *= rates.clip;
@@ -263,11 +312,53 @@ template <typename G, bool NT> __global__ void __launch_bounds__(kStepThreads) a
             v[e] = __builtin_fmaf(v[e], p.beta2, d[e] * p.rest2 * d[e]);
             x[e] = moved(p, rates, x[e], m[e], v[e]);
         }
-        store_wide<4, NT>(avg + i, have, m);
-        store_wide<4, NT>(sq + i, have, v);
-        store_wide<4, NT>(t.p + i, have, x);
+    };
+    int64_t i = begin + threadIdx.x * 4;
+    float x[4], d[4], m[4], v[4];
+    // U groups' loads, then their work.
+    auto some = [&](auto count) {
+        constexpr int U = decltype(count)::value, kNext = kStepThreads * 4;
+        Wide<4, G> gw[U];
+        Wide<4, float> xw[U], mw[U], vw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            gw[u] = load_raw<4, NT>(g + i + u * kNext);
+            xw[u] = load_raw<4, NT>(t.p + i + u * kNext);
+            mw[u] = load_raw<4, NT>(avg + i + u * kNext);
+            vw[u] = load_raw<4, NT>(sq + i + u * kNext);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            widened<4, G>(gw[u], d);
+            widened<4, float>(xw[u], x);
+            widened<4, float>(mw[u], m);
+            widened<4, float>(vw[u], v);
+            step(x, d, m, v);
+            store_wide<4, NT>(avg + i + u * kNext, m);
+            store_wide<4, NT>(sq + i + u * kNext, v);
+            store_wide<4, NT>(t.p + i + u * kNext, x);
+            if (t.copy != nullptr)
+                store_wide<4, NT>(t.copy + i + u * kNext, x);
+        }
+        i += U * kNext;
+    };
+#pragma unroll 1
+    while (i + kStepThreads * 4 + 4 <= end)
+        some(std::integral_constant<int, 2>{});
+    if (i + 4 <= end)
+        some(std::integral_constant<int, 1>{});
+    if (i < end) {   // a tensor's last values
+        const int have = (int)(end - i);
+        widened<4, G>(load_some<4>(g + i, have), d);
+        widened<4, float>(load_some<4>(t.p + i, have), x);
+        widened<4, float>(load_some<4>(avg + i, have), m);
+        widened<4, float>(load_some<4>(sq + i, have), v);
+        step(x, d, m, v);
+        store_some<4>(avg + i, have, m);
+        store_some<4>(sq + i, have, v);
+        store_some<4>(t.p + i, have, x);
         if (t.copy != nullptr)
-            store_wide<4, NT>(t.copy + i, have, x);
+            store_some<4>(t.copy + i, have, x);
     }
 }
 
@@ -349,7 +440,8 @@ template <bool NT> __device__ __forceinline__ void store_codes(uint8_t *c, int h
 }
 
 // A wave holds a block of 256 values, four a lane: its scales are maxima over
-// the wave, so that the states are read and written once.
+// the wave, so that the states are read and written once, 16 bytes a parameter
+// beside 28.  About 90 vector operations a value stay just below the memory's time.
 template <typename G, bool NT> __global__ void __launch_bounds__(kStepThreads) adamw8_kernel(StepParams p) {
     const int j = tensor_of(p.first, p.count, blockIdx.x);
     const pam_step_tensor_t &t = p.tensor[j];
@@ -359,13 +451,18 @@ template <typename G, bool NT> __global__ void __launch_bounds__(kStepThreads) a
     const int64_t end = min(begin + p.chunk, t.n);
     const G *g = static_cast<const G *>(t.g);
     uint8_t *avg = static_cast<uint8_t *>(t.avg), *sq = static_cast<uint8_t *>(t.sq);
-#pragma unroll 1
-    for (int64_t b = begin + wave * PAM_STATE_BLOCK; b < end; b += kStepThreads / 64 * PAM_STATE_BLOCK) {
+    auto one = [&](auto full, int64_t b) {
+        constexpr bool kFull = decltype(full)::value;   // all 256 values exist
         const int64_t i = b + lane * 4, block = b / PAM_STATE_BLOCK;
-        const int have = (int)max(min(end - i, (int64_t)4), (int64_t)0);
+        const int have = kFull ? 4 : (int)max(min(end - i, (int64_t)4), (int64_t)0);
         float x[4], d[4], m[4], v[4], size[4];
-        load_wide<4, NT>(g + i, have, d);
-        load_wide<4, NT>(t.p + i, have, x);
+        if constexpr (kFull) {
+            widened<4, G>(load_raw<4, NT>(g + i), d);
+            widened<4, float>(load_raw<4, NT>(t.p + i), x);
+        } else {
+            widened<4, G>(load_some<4>(g + i, have), d);
+            widened<4, float>(load_some<4>(t.p + i, have), x);
+        }
         const uint32_t mc = load_codes<NT>(avg + i, have), vc = load_codes<NT>(sq + i, have);
         const float ms = t.avg_scale[block], vs = t.sq_scale[block];
 #pragma unroll
@@ -397,14 +494,26 @@ template <typename G, bool NT> __global__ void __launch_bounds__(kStepThreads) a
         }
         store_codes<NT>(avg + i, have, mw);
         store_codes<NT>(sq + i, have, vw);
-        store_wide<4, NT>(t.p + i, have, x);
-        if (t.copy != nullptr)
-            store_wide<4, NT>(t.copy + i, have, x);
+        if constexpr (kFull) {
+            store_wide<4, NT>(t.p + i, x);
+            if (t.copy != nullptr)
+                store_wide<4, NT>(t.copy + i, x);
+        } else {
+            store_some<4>(t.p + i, have, x);
+            if (t.copy != nullptr)
+                store_some<4>(t.copy + i, have, x);
+        }
         if (lane == 0) {
             t.avg_scale[block] = ms1;
             t.sq_scale[block] = vs1;
         }
-    }
+    };
+    int64_t b = begin + wave * PAM_STATE_BLOCK;
+#pragma unroll 1
+    for (; b + PAM_STATE_BLOCK <= end; b += kStepThreads / 64 * PAM_STATE_BLOCK)
+        one(std::true_type{}, b);
+    if (b < end)
+        one(std::false_type{}, b);
 }
 
 }  // namespace

@@ -88,12 +88,12 @@ pam_status_t check_workspace(const void *workspace, int64_t bytes, size_t need) 
 // ---------------------------------------------------------------------------
 
 // How the rows are cut.  Few rows: one band, whose sums need no second launch (2.5
-// us), with as few lanes a row, from kGradLanes on, that a thread has at most
+// us), with as few lanes a row, down to kGradLanes, that a thread has at most
 // kGradFew rows.  Otherwise 64 lanes a row (or the row's) and bands for about
 // kGradGroups workgroups with at least kGradRows rows a thread.
 constexpr int64_t kGradGroups = 1024;
 constexpr int64_t kGradRows = 4;
-constexpr int64_t kGradFew = 16;
+constexpr int64_t kGradFew = 8;
 constexpr int kGradLanes = 8;
 
 struct GradCut {
@@ -299,6 +299,7 @@ pam_status_t pam_activation_grad(const pam_activation_grad_t *args, hipStream_t 
     p.n = (int32_t)a.n;
     p.activation = a.activation;
     p.streaming = a.m * a.n * (each * (a.dz != nullptr ? 2 : 1) + (none ? 0 : size_of(a.z_type))) > pamk::kCacheBytes;
+    p.apart = a.dz == nullptr || (a.dz != a.dy && a.dz != a.z);
     const GradCut cut = grad_cut(std::max<int64_t>(a.m, 1), a.n, pamk::grad_values(bf16));
     p.lanes = cut.lanes;
     p.band = (int32_t)std::min<int64_t>(cut.band, kMaxDim);

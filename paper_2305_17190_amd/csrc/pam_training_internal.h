@@ -34,6 +34,7 @@ struct GradParams {
     int32_t bands, band, lanes;
     int32_t activation;
     int32_t streaming;   // loads with the non-temporal hint
+    int32_t apart;       // dz lies on neither dy nor z
 };
 inline int grad_values(bool bf16) { return bf16 ? 8 : 4; }
 hipError_t launch_activation_grad(bool bf16, bool z_bf16, const GradParams &p, hipStream_t stream);

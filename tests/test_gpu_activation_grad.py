@@ -12,7 +12,7 @@ from oracle import training_ref as ref
 
 pytestmark = pytest.mark.gpu
 
-SIZES = [(1, 1), (1, 771), (197, 771), (5, 3), (1000, 1), (4097, 2), (300, 37), (64, 256), (2048, 512), (3000, 770),
+SIZES = [(1, 1), (1, 771), (197, 771), (260, 9), (5, 3), (1000, 1), (4097, 2), (300, 37), (64, 256), (2048, 512), (3000, 770),
          (16384, 5), (7, 9000)]
 
 
@@ -62,6 +62,30 @@ def test_without_an_activation(m, n):
         dz, db = pam.activation_grad(dy, None, None)
         assert dz is dy
         expect(None, db, dy, dy, None, bf16)
+
+
+@pytest.mark.parametrize("m,n", [(300, 771), (40, 13), (9, 3), (2000, 130)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_c_call_in_place(m, n, bf16):
+    """dz on dy, and on z, rows longer than n: the columns between stay."""
+    import ctypes
+    import struct
+    import torch
+    note(f"pam_activation_grad {m}x{n} in place, bf16 {bf16}")
+    dy, z = problem(m, n, bf16, bf16)
+    want, sums = pam.activation_grad(dy, z, "gelu")
+    lib, need = pam.training._library(), ctypes.c_size_t()
+    assert lib.pam_activation_grad_workspace_size(m, n, ctypes.byref(need)) == 0
+    for onto in (0, 1):
+        wide = torch.full((2, m, n + 5), 7.0, device=device(), dtype=dy.dtype)
+        wide[0, :, :n], wide[1, :, :n] = dy, z
+        db = torch.empty(n, device=device())
+        ws = torch.empty(max(need.value, 1), dtype=torch.uint8, device=device())
+        args = struct.pack("=5q6q4i", wide[0].data_ptr(), wide[1].data_ptr(), wide[onto].data_ptr(), db.data_ptr(),
+                           ws.data_ptr(), m, n, n + 5, n + 5, n + 5, need.value, int(bf16), int(bf16), 2, 0)
+        assert lib.pam_activation_grad(args, torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(wide[onto, :, :n], want) and torch.equal(db, sums)
+        assert torch.equal(wide[1 - onto, :, :n], (z, dy)[onto]) and bool((wide[:, :, n:] == 7).all())
 
 
 def test_views_and_no_rows():
