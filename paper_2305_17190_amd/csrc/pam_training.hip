@@ -4,9 +4,9 @@
 // copy runs at 4.9 TB/s on these cards, reading and writing streams at up to 6.2.
 // Measured (passes in a row): the gradient of 16384 x 4096 float32 values 129 us (6.2
 // TB/s), bfloat16 71 us (5.7), 8192 x 2048 float32 39.5 us (5.1, the sums' launch 4
-// of it); the norm of 188 M float32 values 114 us (6.6 TB/s); the step over them 910
-// us (5.8 TB/s), with 8-bit states 530 us (5.7); the norm and the step of a decoder's
-// 25.7 M parameters, gradients and copies bfloat16, 140 us (5.5).
+// of it); the norm of 188 M float32 values 113 us (6.7 TB/s); the step over them 857
+// us (6.1 TB/s), with 8-bit states 535 us (5.6); the norm and the step of a decoder's
+// 25.7 M parameters, gradients and copies bfloat16, 133 us (5.8).
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -313,41 +313,23 @@ template <typename G, bool NT> __global__ void __launch_bounds__(kStepThreads) a
             x[e] = moved(p, rates, x[e], m[e], v[e]);
         }
     };
-    int64_t i = begin + threadIdx.x * 4;
+    // A vector a thread: the chunk is kStepThreads * 4 values.
+    const int64_t i = begin + threadIdx.x * 4;
     float x[4], d[4], m[4], v[4];
-    // U groups' loads, then their work.
-    auto some = [&](auto count) {
-        constexpr int U = decltype(count)::value, kNext = kStepThreads * 4;
-        Wide<4, G> gw[U];
-        Wide<4, float> xw[U], mw[U], vw[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            gw[u] = load_raw<4, NT>(g + i + u * kNext);
-            xw[u] = load_raw<4, NT>(t.p + i + u * kNext);
-            mw[u] = load_raw<4, NT>(avg + i + u * kNext);
-            vw[u] = load_raw<4, NT>(sq + i + u * kNext);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            widened<4, G>(gw[u], d);
-            widened<4, float>(xw[u], x);
-            widened<4, float>(mw[u], m);
-            widened<4, float>(vw[u], v);
-            step(x, d, m, v);
-            store_wide<4, NT>(avg + i + u * kNext, m);
-            store_wide<4, NT>(sq + i + u * kNext, v);
-            store_wide<4, NT>(t.p + i + u * kNext, x);
-            if (t.copy != nullptr)
-                store_wide<4, NT>(t.copy + i + u * kNext, x);
-        }
-        i += U * kNext;
-    };
-#pragma unroll 1
-    while (i + kStepThreads * 4 + 4 <= end)
-        some(std::integral_constant<int, 2>{});
-    if (i + 4 <= end)
-        some(std::integral_constant<int, 1>{});
-    if (i < end) {   // a tensor's last values
+    if (i + 4 <= end) {
+        const auto gw = load_raw<4, NT>(g + i);
+        const auto xw = load_raw<4, NT>(t.p + i), mw = load_raw<4, NT>(avg + i), vw = load_raw<4, NT>(sq + i);
+        widened<4, G>(gw, d);
+        widened<4, float>(xw, x);
+        widened<4, float>(mw, m);
+        widened<4, float>(vw, v);
+        step(x, d, m, v);
+        store_wide<4, NT>(avg + i, m);
+        store_wide<4, NT>(sq + i, v);
+        store_wide<4, NT>(t.p + i, x);
+        if (t.copy != nullptr)
+            store_wide<4, NT>(t.copy + i, x);
+    } else if (i < end) {   // a tensor's last values
         const int have = (int)(end - i);
         widened<4, G>(load_some<4>(g + i, have), d);
         widened<4, float>(load_some<4>(t.p + i, have), x);

@@ -170,16 +170,14 @@ int64_t norm_groups(const pam_step_tensor_t *tensors, int64_t count, int64_t chu
     return groups;
 }
 
-// Values a workgroup of the step takes: kStepValues where that makes workgroups
-// enough, else fewer.
-constexpr int64_t kStepValues = 4096;
+// Values a workgroup of the step takes.  32-bit states: one vector a thread (188 M
+// parameters 857 us; with two and four 918 and 908).  8-bit ones: a block a wave
+// where that makes few workgroups, else four (558 and 535 us; of 0.9 M 7.0 and 8.4).
 constexpr int64_t kStepGroups = 1024;
 
-int64_t step_chunk(int64_t total) {
-    int64_t chunk = kStepValues;
-    while (chunk > 1024 && total < chunk * kStepGroups)
-        chunk /= 2;
-    return chunk;
+int64_t step_chunk(int64_t total, bool bytes) {
+    const int64_t least = pamk::kStepThreads * 4;
+    return bytes && total >= 4 * least * kStepGroups ? 4 * least : least;
 }
 
 }  // namespace
@@ -389,7 +387,7 @@ pam_status_t pam_adamw_step(const pam_step_tensor_t *tensors, int64_t count, con
         return invalid("max_norm must be > 0");
     int64_t total;
     PAM_TRY(check_tensors(tensors, count, &total));
-    const int64_t chunk = step_chunk(total);
+    const int64_t chunk = step_chunk(total, a.state_bits == 8);
     const bool bytes = a.state_bits == 8;
     int64_t groups = 0;
     for (int64_t j = 0; j < count; ++j) {
