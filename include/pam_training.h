@@ -61,7 +61,7 @@ typedef enum {
  *       are 0)
  * The product's plan is pam_gemm_plan's; its tiles take long sums in parts of
  * 1024 terms (up to k = 1024 the sums are pam_gemm_batched_ws's, bit for bit).
- * k == 0 counts as a product of zeros.
+ * k == 0 counts as a product of zeros.  m, n <= 2^31 - 1024.
  */
 typedef struct {
     const void *x, *w;
@@ -88,7 +88,7 @@ pam_status_t pam_linear(const pam_linear_t *args, hipStream_t stream);
  * no z, and writes db alone (dz is dy).  dz may be dy (with lddz == lddy) or z
  * (with lddz == ldz and the same type).
  *
- *   dy, z: m x n, each float32 or bfloat16
+ *   dy, z: m x n, each float32 or bfloat16; n <= 2^31 - 1024
  *   workspace: pam_activation_grad_workspace_size bytes, 16-byte aligned (NULL if
  *       those are 0, or without db)
  */

@@ -219,7 +219,7 @@ constexpr int dma_min_lds_words(int bm, int bn, int kw, int wps) {
 
 // The launch's parameters, read anew: what only the kernel's end needs would
 // otherwise be loaded at its start and spill across the K loop (67 scalar values
-// into vector lanes, 5% of a large layer's time).
+// into vector lanes; 16384 x 4096 -> 4096 9.39 ms, read anew 9.27).
 typedef const GemmParams __attribute__((address_space(4))) ParamsAgain;   // read by scalar loads
 __device__ __forceinline__ ParamsAgain *params_again() {
     ParamsAgain *at = (ParamsAgain *)__builtin_amdgcn_kernarg_segment_ptr();

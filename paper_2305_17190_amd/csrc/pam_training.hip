@@ -73,9 +73,9 @@ template <int V, typename T> __device__ __forceinline__ void store_some(T *p, in
 // ---------------------------------------------------------------------------
 
 // dz = dy f'(z) and the sums of its columns, each value read once and written once:
-// the sums ride along.  A thread keeps the sums of its V
-// columns over the rows it takes; the workgroup's rows are added in a tree, in
-// LDS, and the bands' sums by sum_bands_kernel: an order fixed by the sizes.
+// the sums ride along.  A thread keeps the sums of its V columns over the rows it
+// takes; the workgroup's rows are added in a tree, in LDS, and the bands' sums by
+// sum_bands_kernel: an order fixed by the sizes.
 template <typename T, typename Z, bool NT> __global__ void __launch_bounds__(kGradThreads) activation_grad_kernel(GradParams p) {
     constexpr int V = 16 / sizeof(T);
     __shared__ float red[kGradThreads * V];
@@ -279,8 +279,9 @@ __device__ __forceinline__ Rates rates_of(const StepParams &p, int tensor) {
     int64_t step = p.step;
     if (p.step_device != nullptr) {
         step = *p.step_device;
-        r.step_size = (float)(p.step_size / -expm1((double)step * p.log_beta1));
-        r.sq_factor = (float)(1.0 / sqrt(-expm1((double)step * p.log_beta2)));
+        // The exponents in float64, the rest in float32: every wave does this.
+        r.step_size = p.step_size / -expm1f((float)((double)step * p.log_beta1));
+        r.sq_factor = 1.0f / sqrtf(-expm1f((float)((double)step * p.log_beta2)));
     }
     if (p.norm != nullptr) {
         const float c = p.max_norm / (*p.norm + 1e-6f);

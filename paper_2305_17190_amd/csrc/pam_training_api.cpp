@@ -37,6 +37,7 @@ pam_status_t invalid(const char *name, const char *why) {
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 constexpr int64_t kMaxDim = 0x7FFFFFFF;
+constexpr int64_t kMaxTiled = kMaxDim - 1023;  // rows and columns, with what a last tile has beyond them
 constexpr int64_t kMaxLd = (int64_t)1 << 31;   // times a count below 2^31: offsets stay inside int64
 
 bool type_ok(pam_type_t t) { return t == PAM_TYPE_F32 || t == PAM_TYPE_BF16; }
@@ -203,8 +204,8 @@ pam_status_t pam_linear(const pam_linear_t *args, hipStream_t stream) {
     const bool bf16 = a.type == PAM_TYPE_BF16;
     if (bf16 && a.mantissa_bits != 23)
         return invalid("bfloat16 operands take mantissa_bits 23");
-    if (a.m < 0 || a.n < 0 || a.k < 0 || a.m > kMaxDim || a.n > kMaxDim || a.k > kMaxDim)
-        return invalid("m, n and k must be in [0, 2^31)");
+    if (a.m < 0 || a.n < 0 || a.k < 0 || a.m > kMaxTiled || a.n > kMaxTiled || a.k > kMaxDim)
+        return invalid("m and n must be in [0, 2^31 - 1024], k in [0, 2^31)");
     PAM_TRY(check_ld("residual", a.residual, a.ldr, a.n));
     PAM_TRY(check_ld("z", a.z, a.ldz, a.n));
     PAM_TRY(check_ld("y", a.y, a.ldy, a.n));
@@ -214,7 +215,9 @@ pam_status_t pam_linear(const pam_linear_t *args, hipStream_t stream) {
     const Range y = rows_of(a.y, a.m, a.n, a.ldy, out, true), z = rows_of(a.z, a.m, a.n, a.ldz, out, true);
     const Range read[] = {rows_of(a.x, a.m, a.k, a.ldx, in, false), rows_of(a.w, a.n, a.k, a.ldw, in, false),
                           range_of(a.bias, a.n * 4, false), rows_of(a.residual, a.m, a.n, a.ldr, out, false)};
-    const Range ws = range_of(a.workspace, std::max<int64_t>(a.workspace_bytes, 0), true);
+    size_t need = 0;
+    PAM_TRY(pamk::api_linear_workspace_size(a.m, a.n, a.k, &need));
+    const Range ws = range_of(a.workspace, (int64_t)need, true);
     if (overlap(y, z) || overlap(y, ws) || overlap(z, ws))
         return invalid("y, z and the workspace overlap");
     for (int i = 0; i < 4; ++i) {
@@ -232,8 +235,8 @@ pam_status_t pam_activation_grad_workspace_size(int64_t m, int64_t n, size_t *by
     if (bytes == nullptr)
         return invalid("bytes is NULL");
     *bytes = 0;
-    if (m < 0 || n < 0 || m > kMaxDim || n > kMaxDim)
-        return invalid("m and n must be in [0, 2^31)");
+    if (m < 0 || n < 0 || m > kMaxDim || n > kMaxTiled)
+        return invalid("m must be in [0, 2^31), n in [0, 2^31 - 1024]");
     if (m == 0 || n == 0)
         return PAM_SUCCESS;
     for (const int values : {4, 8}) {   // either type
@@ -252,8 +255,8 @@ pam_status_t pam_activation_grad(const pam_activation_grad_t *args, hipStream_t 
         return invalid("type and z_type must be PAM_TYPE_F32 or PAM_TYPE_BF16");
     if (!activation_ok(a.activation))
         return invalid("unknown activation");
-    if (a.m < 0 || a.n < 0 || a.m > kMaxDim || a.n > kMaxDim)
-        return invalid("m and n must be in [0, 2^31)");
+    if (a.m < 0 || a.n < 0 || a.m > kMaxDim || a.n > kMaxTiled)
+        return invalid("m must be in [0, 2^31), n in [0, 2^31 - 1024]");
     const bool none = a.activation == PAM_ACT_NONE;
     if (none && (a.z != nullptr || a.dz != nullptr))
         return invalid("without an activation there is no z, and dz is dy");

@@ -26,6 +26,14 @@ def lib():
     return training._library()
 
 
+def test_header_is_c():
+    """Without C++."""
+    import shutil
+    rocm = os.path.join(os.path.dirname(os.path.dirname(shutil.which("hipcc") or "/opt/rocm/bin/hipcc")), "include")
+    subprocess.run(["gcc", "-std=c99", "-fsyntax-only", "-Wall", "-Werror", "-D__HIP_PLATFORM_AMD__", "-isystem", rocm,
+                    "-I", os.path.dirname(HEADER), "-x", "c", HEADER], check=True)
+
+
 def test_every_declared_symbol_is_exported():
     with open(HEADER) as f:
         declared = set(re.findall(r"^pam_status_t (pam_\w+)\(", f.read(), re.M))
@@ -54,7 +62,8 @@ def linear(lib, **change):
     dict(type=-1), dict(out_type=2), dict(activation=5), dict(activation=-1), dict(mantissa_bits=24),
     dict(mantissa_bits=-1), dict(type=1, mantissa_bits=7), dict(y=at(0)), dict(y=at(1) + 4), dict(z=at(4)), dict(z=at(3)),
     dict(z=at(4) + 4 * 300 * 200 - 4), dict(y=at(2)), dict(residual=at(4), ldr=201), dict(residual=at(4) + 4),
-    dict(workspace=at(4)), dict(workspace=at(0)), dict(m=(1 << 31) - 1, ldr=1 << 31, ldy=1 << 31, ldz=1 << 31), dict(k=8192, ldx=8192, ldw=8192, workspace=0),
+    dict(k=8192, ldx=8192, ldw=8192, workspace=at(4)), dict(k=8192, ldx=8192, ldw=8192, workspace=at(0)),
+    dict(m=(1 << 31) - 1024, ldr=1 << 31, ldy=1 << 31, ldz=1 << 31), dict(m=(1 << 31) - 1023), dict(n=(1 << 31) - 1023), dict(k=8192, ldx=8192, ldw=8192, workspace=0),
     dict(k=8192, ldx=8192, ldw=8192, workspace_bytes=4), dict(k=8192, ldx=8192, ldw=8192, workspace=at(6) + 4)])
 def test_linear_refuses(lib, change):
     assert linear(lib, **change) == INVALID, lib.pam_last_error()
@@ -63,7 +72,7 @@ def test_linear_refuses(lib, change):
 @pytest.mark.parametrize("change", [
     {}, dict(bias=0), dict(residual=0, ldr=0), dict(z=0, ldz=0), dict(residual=at(4)), dict(workspace=0, workspace_bytes=0),
     dict(type=1, out_type=1), dict(mantissa_bits=0), dict(k=0, x=0, w=0, ldx=1, ldw=1), dict(ldy=1000, ldx=1 << 17),
-    dict(z=at(4) + 4 * 300 * 200)])
+    dict(z=at(4) + 4 * 300 * 200), dict(workspace=at(6), workspace_bytes=1 << 40)])
 def test_linear_accepts(lib, change):
     """As far as the device, which is missing here."""
     assert linear(lib, **change) == LAUNCH
@@ -97,7 +106,7 @@ def grad(lib, **change):
 
 
 @pytest.mark.parametrize("change", [
-    dict(dy=0), dict(z=0), dict(m=-1), dict(n=-1), dict(m=1 << 31), dict(n=1 << 31), dict(lddy=199), dict(ldz=199),
+    dict(dy=0), dict(z=0), dict(m=-1), dict(n=-1), dict(m=1 << 31), dict(n=(1 << 31) - 1023), dict(lddy=199), dict(ldz=199),
     dict(lddz=199), dict(type=2), dict(z_type=-1), dict(activation=5), dict(activation=0),
     dict(activation=0, z=0), dict(workspace=0), dict(workspace_bytes=4), dict(workspace=at(4) + 8), dict(dz=at(0) + 4),
     dict(dz=at(0), lddz=300), dict(dz=at(1), z_type=1), dict(db=at(0)), dict(db=at(2)), dict(db=at(4)),
