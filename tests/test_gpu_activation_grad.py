@@ -88,6 +88,19 @@ def test_c_call_in_place(m, n, bf16):
         assert torch.equal(wide[1 - onto, :, :n], (z, dy)[onto]) and bool((wide[:, :, n:] == 7).all())
 
 
+@pytest.mark.parametrize("seed", range(24))
+def test_random_sizes(seed):
+    import random
+    rng = random.Random(700 + seed)
+    m, n = (int(round(20000 ** rng.random())) for _ in "mn")
+    m = min(m, 4000000 // n)
+    bf16, z_bf16, name = rng.random() < 0.5, rng.random() < 0.5, rng.choice(ref.ACTIVATIONS[1:])
+    note(f"random activation_grad {seed}: {m}x{n} {name} bf16 {bf16} {z_bf16}")
+    dy, z = problem(m, n, bf16, z_bf16, seed)
+    dz, db = pam.activation_grad(dy, z, name)
+    expect(dz, db, dy, z, name, bf16)
+
+
 def test_views_and_no_rows():
     import torch
     note("activation_grad of views")

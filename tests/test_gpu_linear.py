@@ -277,3 +277,77 @@ def test_streams_and_graphs():
         torch.cuda.synchronize()
         assert all(same(a, b) for g, w in zip(outs, want) for a, b in zip(g, w)), rep
     del graph
+
+
+@pytest.mark.parametrize("seed", range(48))
+def test_random_layers(seed):
+    """Random sizes, types, views and parts, each against gemm and the definition."""
+    import random
+    import torch
+    rng = random.Random(900 + seed)
+
+    def log_uniform(lo, hi):
+        return int(round(lo * (hi / lo) ** rng.random()))
+
+    m, k, n = log_uniform(1, 5000), log_uniform(1, 3000), log_uniform(1, 3000)
+    while m * k * n > 3e9:
+        m, k = max(m // 2, 1), max(k // 2, 1)
+    bf16, out_bf16 = rng.random() < 0.4, rng.random() < 0.4
+    name, pad = rng.choice(ref.ACTIVATIONS), rng.choice((0, 0, 1, 3, 8))
+    x, w, bias, res = inputs(m, k, n, bf16, seed, out_bf16)
+    if rng.random() < 0.5:
+        x = torch.relu(x)
+    bias = bias if rng.random() < 0.7 else None
+    res = res if rng.random() < 0.5 else None
+    wide = [torch.nn.functional.pad(t, (pad, 1 + pad))[:, pad:pad + t.shape[1]] if pad and t is not None else t
+            for t in (x, w, res)]
+    out = torch.bfloat16 if out_bf16 else torch.float32
+    note(f"random layer {seed}: {m}x{k}x{n} {name} {x.dtype} -> {out}, pad {pad}, bias {bias is not None}, "
+         f"residual {res is not None}")
+    y, z = pam.linear(wide[0], wide[1], bias, name, wide[2], save_z=True, out_dtype=out)
+    z32 = pam.gemm(x, w, trans_b=True)
+    z32 = z32 if bias is None else z32 + bias
+    if k <= 1024:
+        assert same(z, z32.to(out))
+    else:        # other orders of the same terms, whose magnitudes' sum is at most |x| |w|^T's
+        size = x.float().abs().cpu().double() @ w.float().abs().cpu().double().t()
+        off = (z.cpu().double() - z32.cpu().double()).abs()
+        assert bool((off <= 2 * (k + 2) * tu.U * size + (2.0 ** -8 if out_bf16 else 2 * tu.U) * z32.cpu().double().abs()).all())
+        z32 = pam.linear(x, w, bias)
+    expect(y, z32, name, res, out_bf16, "y")
+
+
+def test_host_threads():
+    """Layers and their gradients from four host threads, a stream each."""
+    import threading
+    import torch
+    note("linear from 4 host threads")
+    cases = [inputs(*s, seed=5) for s in ((2048, 512, 300), (8, 2000, 500), (197, 64, 197), (300, 3000, 700))]
+
+    def run(c):
+        y, z = pam.linear(*c[:3], "silu", c[3], save_z=True)
+        return (y, z, *pam.activation_grad(y, z, "silu"), pam.grad_norm([y, z]))
+
+    want = [run(c) for c in cases]
+    torch.cuda.synchronize()
+    got, errors = [None] * len(cases), []
+
+    def work(i):
+        try:
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                for j in range(20):
+                    r = run(cases[(i + j) % len(cases)])
+                    if (i + j) % len(cases) == i:
+                        got[i] = r
+            s.synchronize()
+        except Exception as e:   # reported below, on the main thread
+            errors.append((i, repr(e)))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(cases))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(timeout=60)
+    assert not any(t.is_alive() for t in threads) and not errors, errors
+    assert all(same(a, b) for g, w in zip(got, want) for a, b in zip(g, w))

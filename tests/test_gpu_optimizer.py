@@ -154,6 +154,41 @@ def test_8_bit_states(sizes, grad_bf16):
             at += gap + length(n)
 
 
+@pytest.mark.parametrize("seed", range(12))
+def test_random_lists(seed):
+    """Lists of random lengths and sizes, four steps from fresh states: 8-bit codes bit for
+    bit, 32-bit states within their tolerance of the definition carried along."""
+    import random
+    import torch
+    rng = random.Random(500 + seed)
+    eight, grad_bf16 = seed % 2 == 0, rng.random() < 0.5
+    sizes = [int(round(30000 ** rng.random())) - (rng.random() < 0.1) for _ in range(rng.choice((1, 5, 60, 140)))]
+    note(f"random adamw {seed}: {len(sizes)} tensors, {sum(sizes)} values, 8 bits {eight}, bf16 {grad_bf16}")
+    p0 = [np.ascontiguousarray(t) for t in make(sizes, seed)["p"]]
+    state = [[np.zeros(n, np.uint8 if eight else np.float32) for n in sizes] for _ in "mv"]
+    scales = [[np.zeros(blocks(n), np.float32) for n in sizes] for _ in "mv"] if eight else [None, None]
+    p = [to_dev(t) for t in p0]
+    d = [None if x is None else [to_dev(t) for t in x] for x in (*state, *scales)]
+    for step in range(1, 5):
+        gn = make(sizes, 10 * seed + step, grad_bf16)["g"]
+        g = [to_dev(t) for t in gn]
+        g = [t.bfloat16() for t in g] if grad_bf16 else g
+        old = [[t.cpu().numpy().copy() for t in x] for x in (p, d[0], d[1])]
+        pam.adamw_step(p, g, d[0], d[1], step, **KW, avg_scales=d[2], sq_scales=d[3], seed=seed)
+        for j in range(len(sizes)):
+            if eight:
+                want = ref.adamw8(old[0][j], gn[j], state[0][j], state[1][j], scales[0][j], scales[1][j], step=step, seed=seed,
+                                  tensor=j, **KW)
+                state[0][j], state[1][j], scales[0][j], scales[1][j] = want[1:5]
+                for t, w_ in zip((d[0][j], d[1][j], d[2][j], d[3][j]), want[1:5]):
+                    assert np.array_equal(t.cpu().numpy(), w_), (step, j)
+            else:
+                args = old[0][j], gn[j], old[1][j], old[2][j]
+                for t, w_, e in zip((p[j], d[0][j], d[1][j]), ref.adamw(*args, step, **KW),
+                                    tu.step_errors(*args, 0.0, step, **KW)):
+                    check(t.cpu().numpy(), w_, e, f"tensor {j}, step {step}")
+
+
 def test_special_gradients():
     """Zero gradients, whole blocks of them, infinities and NaN stay in their block."""
     import torch
