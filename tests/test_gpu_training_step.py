@@ -148,6 +148,47 @@ def test_steps_in_a_graph(eight):
     del graph
 
 
+def test_backward_pass_in_a_graph():
+    """Forward and backward of the layers under autograd, captured with the step: the
+    gradients asked for, no eager graph of the same leaves alive; replays equal eager
+    passes bit for bit."""
+    import torch
+    from paper_2305_17190_amd.autograd import pam_linear
+    note("layers' backward pass in a graph")
+    p, x, target = block(seed=3)
+
+    def passed(leaves):
+        h = pam_linear(x, leaves[0], leaves[1], activation="silu")
+        y = pam_linear(h, leaves[2], leaves[3], residual=x)
+        return y.detach(), torch.autograd.grad(y, leaves, (y - target).detach())
+
+    leaves = [t.clone().requires_grad_() for t in p]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            passed(leaves)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, g = passed(leaves)
+    for rep in range(4):
+        x.mul_(0.9)
+        target.add_(0.1)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        again = [t.detach().clone().requires_grad_() for t in leaves]
+        want, gw = passed(again)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and all(torch.equal(a, b) for a, b in zip(g, gw)), rep
+        with torch.no_grad():
+            for t in leaves:
+                t.mul_(0.99)
+    del graph
+
+
 @pytest.mark.parametrize("bits", [8, 32])
 def test_example_runs_with_either_state(bits):
     path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decoder.py")
