@@ -287,6 +287,9 @@ def test_optimizer_refusals():
         AdamW(p, state_bits=16)
     with pytest.raises(ValueError, match="max_norm"):
         AdamW(p, max_norm=0.0)
+    for bad in (dict(lr=-1.0), dict(eps=-1.0), dict(weight_decay=-0.1), dict(betas=(1.0, 0.9)), dict(betas=(0.9, -0.1))):
+        with pytest.raises(ValueError, match=next(iter(bad))):
+            AdamW(p, **bad)
     import copy
     import pickle
     made = AdamW(p, lr=0.5, max_norm=2.0, state_bits=8, seed=3)
