@@ -56,6 +56,7 @@ struct SkinnyParams {
     float *C;
     int64_t ldx, ldd, strideX, strideD, strideC;
     int64_t cs, cd;   // C's strides along the skinny and the wide index
+    int32_t rows;     // the few rows are op(A)'s (no stride says so: both are 1 in a single column)
     int32_t s, d, k;
     int32_t kwaves;   // waves of a workgroup that share one set of wide rows (1, 2, 4 or 8)
     int32_t d_tiles, s_tiles;
@@ -165,7 +166,7 @@ __global__ void __launch_bounds__(64 * kWaves) pam_skinny_kernel(SkinnyParams p)
     // come after it.
     float bias[kJ], res[kJ];
     if constexpr (EPI) {
-        if (p.cd == 1 && kw == 0 && kq < S && s0 + kq < p.s) {
+        if (p.rows != 0 && kw == 0 && kq < S && s0 + kq < p.s) {
             load_bias4(p.epi, d0, p.d - d0, bias);
             load_residual4(p.epi, s0 + kq, d0, p.d - d0, res);
         }
@@ -362,7 +363,7 @@ __global__ void __launch_bounds__(64 * kWaves) pam_skinny_kernel(SkinnyParams p)
     }
     if (kq < S && s0 + kq < p.s) {
         if constexpr (EPI) {
-            if (p.cd == 1) {   // the few rows are x's
+            if (p.rows != 0) {   // the few rows are x's
                 with_activation(p.epi.activation, [&](auto act) {
                     finish4<decltype(act)::value>(p.epi, s0 + kq, d0, p.d - d0, mineacc, bias, res);
                 });
@@ -386,6 +387,7 @@ __global__ void __launch_bounds__(64 * kWaves) pam_skinny_kernel(SkinnyParams p)
 
 hipError_t launch_pam_skinny(bool rows, bool bf16, const GemmParams &g, int64_t batch, hipStream_t stream) {
     SkinnyParams p{};
+    p.rows = rows;
     // rows: op(A)'s few rows against B's; otherwise B's few rows (op(B)'s
     // columns) against A's (PAM is commutative), and C is written by columns.
     p.X = rows ? g.A : g.B;
