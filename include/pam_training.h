@@ -33,7 +33,8 @@ extern "C" {
  *   GELU_TANH  z s(2 sqrt(2/pi) (z + 0.044715 z^3)), s(u) = 1 / (1 + exp(-u))
  *   SILU       z s(z)
  * NaN gives NaN; an infinite z gives the limit or, of the smooth ones at
- * -inf, NaN where the formula does (GELU, SILU).
+ * -inf, NaN where the formula does.  Results from 2^-126 on are there, however far
+ * z is; of the slopes f'(z) those below 2^-118 may be zero.
  */
 #ifdef __cplusplus
 typedef enum : int32_t {
