@@ -167,9 +167,12 @@ pam_status_t pam_grad_norm(const pam_step_tensor_t *tensors, int64_t count, pam_
  * float32 by itself, as
  *   avg = fl(fl(avg beta1) + fl(g' (1 - beta1))),
  *   sq  = fl(fl(sq beta2) + fl(fl(g' (1 - beta2)) g')),
- * so that the codes are the same wherever they are computed.  A NaN or an
- * infinity among a block's new averages makes the block's averages of that kind
- * NaN or infinite.
+ * so that the codes are the same wherever they are computed.  With states in 8
+ * and in 32 bits, what is below 2^-126 counts as zero, among operands and among
+ * the results of each operation: from a fresh state and beta2 = 0.999, sq (and in 8
+ * bits its code) is 0 for a gradient below 3.4e-18, and p steps by avg / eps there,
+ * which for eps == 0 is infinite.  A NaN or an infinity among a block's new
+ * averages makes the block's averages of that kind NaN or infinite.
  *
  * A tensor of 0 values is passed over.  The tensors may not share memory.
  */

@@ -1,7 +1,8 @@
 """Plain definitions of the layer-and-step operators (NumPy): the activations and
 their slopes, a linear layer around a PAM product, the gradient of what it adds,
 the gradients' norm, and the AdamW step.  Everything is float64 but the 8-bit
-states' codes, whose definition rounds each operation to float32."""
+states' codes, whose definition rounds each operation to float32 and takes what is
+below 2^-126 for zero."""
 from __future__ import annotations
 
 import math
@@ -112,12 +113,18 @@ def random_bits(seed, step, tensor, n):
             (h >> np.uint64(16)) * np.uint64(16) + np.uint64(8))
 
 
+def normal(x):
+    """x in float32, what is below 2^-126 as a zero of its sign."""
+    x = np.asarray(x, np.float32)
+    return np.where(np.abs(x) < np.float32(2.0 ** -126), np.copysign(np.float32(0), x), x)
+
+
 def code_value(code, scales, most):
     """The float32 values of codes (most: 127 of avg, 255 of sq)."""
     size = code & most
     f = np.where(size > 0, (size.astype(np.uint32) + np.uint32(1016 - most)) << np.uint32(20), 0).astype(np.uint32)
     with np.errstate(invalid="ignore"):
-        x = f.view(np.float32) * np.repeat(scales, BLOCK)[:len(code)]
+        x = normal(f.view(np.float32) * np.repeat(normal(scales), BLOCK)[:len(code)])
     return np.where(code > most, -x, x).astype(np.float32)
 
 
@@ -140,12 +147,12 @@ def adamw8(p, g, avg, sq, avg_scale, sq_scale, step, lr, betas, eps, weight_deca
     """(p, avg, sq, avg_scale, sq_scale, the step alone) of one tensor after a
     step with 8-bit states; limit: the float32 factor of the gradient."""
     f = np.float32
-    g = np.asarray(g, f)
+    g = normal(g)
     with np.errstate(invalid="ignore", over="ignore"):
         if limit is not None:
-            g = g * f(limit)
-        m = code_value(avg, avg_scale, 127) * f(betas[0]) + g * f(1 - betas[0])
-        v = code_value(sq, sq_scale, 255) * f(betas[1]) + g * f(1 - betas[1]) * g
+            g = normal(g * f(limit))
+        m = normal(normal(code_value(avg, avg_scale, 127) * f(betas[0])) + normal(g * f(1 - betas[0])))
+        v = normal(normal(code_value(sq, sq_scale, 255) * f(betas[1])) + normal(normal(g * f(1 - betas[1])) * g))
         assert m.dtype == v.dtype == f
         r1, r2 = random_bits(seed, step, tensor, len(g))
         code, scale = code_of(np.abs(m), 127, r1)
