@@ -328,11 +328,17 @@ def adamw_step(params, grads, avgs, sqs, step, lr: float = 1e-3, betas=(0.9, 0.9
     when the kernels run (a captured step counts on when the graph also adds 1
     to it).  ``norm`` is ``grad_norm``'s result (or any float32 tensor of one
     element)."""
-    torch = _torch()
     for name, tensors in (("params", params), ("grads", grads), ("avgs", avgs), ("sqs", sqs)):
         if tensors is None:
             raise TypeError(f"{name} must be a list or tuple of tensors")
-    count, tensors, bf16, eight, first = _step_tensors(params, grads, avgs, sqs, avg_scales, sq_scales, copies)
+    packed = _step_tensors(params, grads, avgs, sqs, avg_scales, sq_scales, copies)
+    _adamw(packed, step, lr, betas, eps, weight_decay, norm, max_norm, seed)
+
+
+def _adamw(packed, step, lr, betas, eps, weight_decay, norm, max_norm, seed) -> None:
+    """adamw_step over _step_tensors' lists."""
+    torch = _torch()
+    count, tensors, bf16, eight, first = packed
     for name, t in (("norm", norm), ("step", step if isinstance(step, torch.Tensor) else None)):
         if t is None:
             continue
