@@ -291,7 +291,9 @@ def _dims(A, B, trans_a: bool, trans_b: bool):
 
 
 def _ld(t) -> int:
-    return max(t.stride(-2) if t.numel() > 0 else t.shape[-1], 1)
+    """A matrix's leading dimension.  Rows that overlap (an expanded dimension's: 0)
+    keep theirs, which the library refuses."""
+    return t.stride(-2) if t.shape[-2] > 1 and t.numel() > 0 else max(t.shape[-1], 1)
 
 
 def gemm(A, B, trans_a: bool = False, trans_b: bool = False, out=None, mantissa_bits: int = 23):
