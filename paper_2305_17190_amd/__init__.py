@@ -200,7 +200,7 @@ def _require(t, name: str, ndim: int, bf16_ok: bool = False):
         raise PamError(f"{name} must be a HIP (cuda) tensor; the PAM library has no CPU path")
     if t.dim() != ndim:
         raise ValueError(f"{name} must have {ndim} dimensions, got {t.dim()}")
-    if t.numel() > 0 and t.stride(-1) != 1:
+    if t.numel() > 0 and t.shape[-1] > 1 and t.stride(-1) != 1:   # a single column's is never taken
         raise ValueError(f"{name} must have a contiguous last dimension")
 
 
