@@ -3,6 +3,8 @@ not run)."""
 import pytest
 
 import linear_probe as probe
+import paper_2305_17190_amd as pam
+from long_sum_cases import CASES
 
 
 @pytest.mark.parametrize("m", [2, 33, 500, 4096, 65536])
@@ -24,3 +26,27 @@ def test_one_output_is_one_row_of_weights(m, k, bf16, ldy):
 def test_the_shorter_side_is_few(m, k, n, of_x):
     launches, count = probe.linear(m, k, n)
     assert count == 1 and launches[0].name == "few rows" and bool(launches[0].few_rows_of_a) == of_x
+
+
+@pytest.mark.parametrize("m,k,n,form", CASES)
+@pytest.mark.parametrize("bf16", [False, True])
+def test_long_sums_take_the_form_meant(m, k, n, form, bf16):
+    """Running sums in the workspace (at most 512 MiB of them, more tiles in several
+    launches), under the plan of the product."""
+    tile, kgroups, split, whole, launches = form
+    plan = pam.plan(m, n, k)
+    assert (plan[:2], plan[3], plan[2] > 1, plan[2] == 1 or plan[4] > 0) == form[:4]
+    tiles = -(-m // tile[0]) * -(-n // tile[1])
+    items = tiles if not split else plan[4] + (tiles - plan[4]) * plan[2]
+    sums = items * kgroups * tile[0] * tile[1] * 4
+    layer, product = probe.workspace(m, n, k)
+    assert layer == -(-product // 256) * 256 + min(sums, 512 << 20)
+    got, count = probe.linear(m, k, n, bf16)
+    assert [x.name for x in got] == ["tiled"] * launches + ["reduce"] * split
+    assert -(-sums // (512 << 20)) == launches and count == launches + split
+
+
+@pytest.mark.parametrize("m,k,n", [(4096, 1024, 1024), (8192, 512, 2048), (8, 4096, 512), (1773, 197, 770)])
+def test_short_sums_take_no_memory(m, k, n):
+    layer, product = probe.workspace(m, n, k)
+    assert layer == -(-product // 256) * 256
