@@ -230,6 +230,8 @@ class PAMLinear(torch.nn.Module):
     """A linear layer whose products are PAM (forward and approximate-derivative backward),
     with an activation and, in a call, a residual (``pam_linear``)."""
 
+    activation = None   # of layers that were saved whole before there was one
+
     def __init__(self, in_features: int, out_features: int, bias: bool = True, device=None,
                  mantissa_bits: int = 23, derivative: str = "approximate", activation: str = None):
         super().__init__()
