@@ -153,8 +153,10 @@ pam_status_t pam_grad_norm(const pam_step_tensor_t *tensors, int64_t count, pam_
  *   sq  = beta2 sq + (1 - beta2) g'^2
  *   p   = p (1 - lr weight_decay)
  *         - lr / (1 - beta1^t) avg / (sqrt(sq) / sqrt(1 - beta2^t) + eps)
- * t = step, or *step_device where that is not NULL (one int64, read when the
- * kernel runs, so that a captured step counts on).  p takes the averages
+ * t = step, or *step_device where that is not NULL (one int64 from 1 on, read when
+ * the kernel runs, so that a captured step counts on; 1 - beta^t is then computed in
+ * float32 there, and p may differ from that of the same `step` in its last bits: by
+ * a dozen units of 2^-24 of what it moves by, and its rounding).  p takes the averages
  * before they are rounded to 8 bits.
  *
  * Rounding to 8 bits is stochastic: with f the float32 encoding of |value| /
@@ -162,7 +164,8 @@ pam_status_t pam_grad_norm(const pam_step_tensor_t *tensors, int64_t count, pam_
  * at least 1 where the value is not 0; r = 16 h + 8, h the low (avg) or high
  * (sq) 16 bits of mix(i + mix(mix(seed + t 0x9E3779B9) + j)) for element i of
  * tensor j, all of 32 bits,
- *   mix(x): x = (x ^ x >> 16) 0x7FEB352D; x = (x ^ x >> 15) 0x846CA68B; x ^ x >> 16.
+ *   mix(x): x = (x ^ x >> 16) 0x7FEB352D; x = (x ^ x >> 15) 0x846CA68B; x ^ x >> 16
+ * (published by C. Wellons, "Prospecting for Hash Functions", 2018).
  * Each operation on the way from the old codes to the new ones is rounded to
  * float32 by itself, as
  *   avg = fl(fl(avg beta1) + fl(g' (1 - beta1))),

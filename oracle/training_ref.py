@@ -99,6 +99,7 @@ def adamw(p, g, avg, sq, step, lr, betas, eps, weight_decay, limit=1.0):
 # 8-bit states ---------------------------------------------------------------
 
 def mix(x):
+    """A hash of 32 bits: C. Wellons, "Prospecting for Hash Functions", 2018."""
     x = np.asarray(x, np.uint64) & np.uint64(0xFFFFFFFF)
     for shift, factor in ((16, 0x7FEB352D), (15, 0x846CA68B)):
         x = ((x ^ (x >> np.uint64(shift))) * np.uint64(factor)) & np.uint64(0xFFFFFFFF)

@@ -13,7 +13,10 @@ Every product runs in the library's HIP kernels (``pam.gemm`` / ``pam.bmm``);
 the bias gradient is an ordinary sum (no multiplication).  With an activation or
 a residual, Y = f(X .^ W^T + b) + R, what the layer adds runs in its product's
 launches (``pam.linear``), and dZ = dY f'(Z) and db in a pass of their own
-(``pam.activation_grad``); dX and dW are then products with dZ.  ``pam_linear``
+(``pam.activation_grad``); dX and dW are then products with dZ.  A layer with a
+bias alone keeps ``pam.gemm`` with the bias added to its result, and torch's sum
+as db: the results it has always had (beyond 1024 terms those of ``pam.linear``
+differ in their last bits).  ``pam_linear``
 and ``PAMLinear`` also offer Table 1's exact derivative
 (``derivative="exact"``): dX[i,k] = sum_j dY[i,j] d(X[i,k] .^ W[j,k])/dX[i,k]
 and dW likewise, through ``pam.exact_grad``.  With

@@ -3,8 +3,8 @@
 // many tensors.  All are bound by reading and writing each value once; a large
 // copy runs at 4.9 TB/s on these cards, reading and writing streams at up to 6.2.
 // Measured (passes in a row): the gradient of 16384 x 4096 float32 values 129 us (6.2
-// TB/s), bfloat16 71 us (5.7), 8192 x 2048 float32 39.5 us (5.1, the sums' launch 4
-// of it); the norm of 188 M float32 values 113 us (6.7 TB/s); the step over them 857
+// TB/s), bfloat16 71 us (5.7), 8192 x 2048 float32 45 us (4.5, the sums' launch 4 of
+// it; on the same buffers again, which the cache holds in part, 36); the norm of 188 M float32 values 113 us (6.7 TB/s); the step over them 857
 // us (6.1 TB/s), with 8-bit states 535 us (5.6); the norm and the step of a decoder's
 // 25.7 M parameters, gradients and copies bfloat16, 133 us (5.8).
 
@@ -141,7 +141,8 @@ template <typename T, typename Z, bool NT> __global__ void __launch_bounds__(kGr
                 };
                 // Several rows at once where the few there are make up a thread's time
                 // (64 x 512 6.5 -> 5.2 us); where memory does, one by one (8192 x 2048
-                // 39.5 us, by two 41.2, by four 46.8).
+                // 45.5 us, by two 45.8, by four 53.5; on the same buffers again 36.2, 37.1
+                // and 40.2).
                 constexpr int kRows = 4;
                 if (p.bands == 1)
                     for (; r + (kRows - 1) * at_once < end; r += kRows * at_once)
@@ -268,6 +269,8 @@ struct Rates {
     uint32_t key;     // of the tensor's random bits
 };
 
+// The mixer of two multiplications that C. Wellons found by search and published
+// ("Prospecting for Hash Functions", 2018).
 __device__ __forceinline__ uint32_t mix(uint32_t x) {
     x = (x ^ (x >> 16)) * 0x7FEB352Du;
     x = (x ^ (x >> 15)) * 0x846CA68Bu;
@@ -279,7 +282,8 @@ __device__ __forceinline__ Rates rates_of(const StepParams &p, int tensor) {
     int64_t step = p.step;
     if (p.step_device != nullptr) {
         step = *p.step_device;
-        // The exponents in float64, the rest in float32: every wave does this.
+        // The exponents in float64, the rest in float32, for every wave does this: within a
+        // dozen units of 2^-24 of the host's rates.
         r.step_size = p.step_size / -expm1f((float)((double)step * p.log_beta1));
         r.sq_factor = 1.0f / sqrtf(-expm1f((float)((double)step * p.log_beta2)));
     }

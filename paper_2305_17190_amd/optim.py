@@ -46,7 +46,10 @@ class AdamW(torch.optim.Optimizer):
     gradients in a byte a value, and 8 bytes a block of 256, in place of 8
     bytes a value; their rounding is stochastic, by ``seed``.  A parameter
     without a gradient is passed over.  ``step`` counts on the host: inside a
-    captured graph use ``pam.adamw_step`` with a step on the device."""
+    captured graph use ``pam.adamw_step`` with a step on the device, and for
+    bfloat16 copies of the parameters its ``copies``.  A step that is refused
+    (parameters not contiguous or of another type or device, rates that are none)
+    changes no parameter."""
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
                  max_norm: float = None, state_bits: int = 32, seed: int = 0):
