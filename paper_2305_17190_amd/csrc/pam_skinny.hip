@@ -30,9 +30,9 @@
 // 0.1% of them among the weights 32 x 4096 x 4096 took 491 us, now 58 us).  The test
 // for S1 is lost where the wide operand holds zeros or tiny normals: with a tenth of
 // the weights zero 8 x 4096 x 4096 in bfloat16 takes 16.4 us (13.8 without zeros; 15.1
-// with ranges of both operands for every chunk), in float32 18.4 us (18.1; 18.2).  bfloat16
-// operands widen to the same encodings, so their product equals the float32 one
-// bit for bit.
+// with ranges of both operands for every chunk), in float32 18.4 us (18.1; 18.2).
+// bfloat16 operands widen to the same encodings, so their product equals the
+// float32 one bit for bit.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>

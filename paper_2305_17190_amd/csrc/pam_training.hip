@@ -4,9 +4,10 @@
 // copy runs at 4.9 TB/s on these cards, reading and writing streams at up to 6.2.
 // Measured (passes in a row): the gradient of 16384 x 4096 float32 values 129 us (6.2
 // TB/s), bfloat16 71 us (5.7), 8192 x 2048 float32 45 us (4.5, the sums' launch 4 of
-// it; on the same buffers again, which the cache holds in part, 36); the norm of 188 M float32 values 113 us (6.7 TB/s); the step over them 857
-// us (6.1 TB/s), with 8-bit states 535 us (5.6); the norm and the step of a decoder's
-// 25.7 M parameters, gradients and copies bfloat16, 133 us (5.8).
+// it; on the same buffers again, which the cache holds in part, 36); the norm of 188 M
+// float32 values 113 us (6.7 TB/s); the step over them 857 us (6.1 TB/s), with 8-bit
+// states 535 us (5.6); the norm and the step of a decoder's 25.7 M parameters,
+// gradients and copies bfloat16, 131 us (5.9).
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>

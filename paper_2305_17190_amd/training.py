@@ -326,8 +326,8 @@ def adamw_step(params, grads, avgs, sqs, step, lr: float = 1e-3, betas=(0.9, 0.9
 
     ``step`` is t: an integer from 1 on, or a one-element int64 HIP tensor, read
     when the kernels run (a captured step counts on when the graph also adds 1
-    to it; its parameters may differ from the integer's in their last bits).  ``norm`` is ``grad_norm``'s result (or any float32 tensor of one
-    element)."""
+    to it; its parameters may differ from the integer's in their last bits).
+    ``norm`` is ``grad_norm``'s result (or any float32 tensor of one element)."""
     for name, tensors in (("params", params), ("grads", grads), ("avgs", avgs), ("sqs", sqs)):
         if tensors is None:
             raise TypeError(f"{name} must be a list or tuple of tensors")
